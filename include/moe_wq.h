@@ -361,6 +361,66 @@ int moe_combine(const void *y_perm, int y_dtype, const int32_t *inv_perm,
                 const float *expert_scale, const int32_t *active_rows, int T, int k, int d,
                 void *out, int out_dtype, void *stream);
 
+/*
+ * Microscaled 4-bit floating point (OCP MX, "MXFP4"): e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) with a power-of-two scale
+ * per block of 32 values along K.  A matrix of `rows` rows of K values is
+ *   codes  [rows, K/2] bytes, even k in the low nibble (code = sign * 8 + index into the list above)
+ *   scales [ceil(K/128), rows, 4] bytes: byte b of group g is block 4 g + b; s stands for 2^(s - 127), 255 for a block that is not a number
+ *          (bytes of blocks past K are written as 0 and never read)
+ * Expert weights (E, K, N) are E such matrices of N rows, an output channel each: codes [E, N, K/2], scales [E, ceil(K/128), N, 4].
+ * Quantisation: with amax the largest magnitude of a block, s = floor(log2(amax)) - 2 + 127, at least 0; a value becomes the code nearest to
+ * v / 2^(s - 127), ties to the even code, at most 6.  An all-zero block has s = 0; a block that holds an infinity or a NaN s = 255, codes 0.
+ *
+ * moe_mx4_quantize_rows: x [R, K] MOE_F16 | MOE_BF16 | MOE_F32, x_stride elements from row to row (>= K, rows 16-byte aligned).
+ * moe_mx4_quantize_experts: w fp32 [E, K, N] as for moe_quantize_experts; a slice of experts gives the same bytes.
+ * moe_mx4_dequantize: out [matrices, rows, K] in out_dtype = code * scale (rounded where out_dtype cannot hold it); for rows matrices = 1, for experts
+ *   matrices = E and rows = N.
+ * All require K % 64 == 0, experts N % 32 == 0.
+ */
+int moe_mx4_quantize_rows(const void *x, int x_dtype, int R, int K, int64_t x_stride, void *codes, void *scales, void *stream);
+int moe_mx4_quantize_experts(const float *w, int E, int K, int N, void *codes, void *scales, void *stream);
+int moe_mx4_dequantize(const void *codes, const void *scales, int matrices, int rows, int K, void *out, int out_dtype, void *stream);
+
+/*
+ * The experts' products on such weights and rows, in the matrix cores' own 4-bit form (products of codes are exact, sums fp32):
+ *   moe_grouped_gemm_mx4: y[r] = act(a[r] @ W[e]^T + bias[e]) for every expert e and each of its rows r
+ *     a_codes / a_scales: a_rows rows of K values; row r is a[perm_src[r] / k], or a[r] when perm_src is NULL (then a_rows >= R)
+ *     expert_offsets [E+1] (device) as for moe_grouped_ffn_wq; rows at or past expert_offsets[E] are not written
+ *     bias [E, N] fp16 or NULL; activation MOE_ACT_RELU | MOE_ACT_GELU or -1 for none; y [R, N] in y_dtype
+ *   moe_grouped_ffn_mx4: h[r] = act(mx4(x[perm_src[r] / k]) @ W1[e]^T + b1[e]), y[r] = mx4(h[r]) @ W2[e]^T + b2[e]
+ *     x [T, d] act_dtype (any of the three); both roundings to the 4-bit format are moe_mx4_quantize_rows' (h from its fp32 value); y_perm [R, d] y_dtype
+ *     workspace: the 4-bit forms of x and h (moe_grouped_ffn_mx4_workspace_bytes, 16-byte aligned)
+ * max_rows_per_expert: an upper bound on the rows of one expert or 0; it only takes part in the choice of kernels.
+ * Requires K, d, F % 64 == 0, N % 32 == 0, E <= 4096.
+ */
+int moe_grouped_gemm_mx4(const void *a_codes, const void *a_scales, int a_rows, const int32_t *perm_src, int k, const int32_t *expert_offsets,
+                         int R, int E, int max_rows_per_expert, int K, int N, const void *w_codes, const void *w_scales, const void *bias,
+                         int activation, void *y, int y_dtype, void *stream);
+size_t moe_grouped_ffn_mx4_workspace_bytes(int T, int R, int d, int F);
+int moe_grouped_ffn_mx4(const void *x, int act_dtype, int T, const int32_t *perm_src, int k, const int32_t *expert_offsets, int R, int E,
+                        int max_rows_per_expert, int d, int F, int activation, const void *w1_codes, const void *w1_scales, const void *b1,
+                        const void *w2_codes, const void *w2_scales, const void *b2, void *y_perm, int y_dtype, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * Tuning a router: its load-balance loss with per-expert counts, the gate scales as functions of the logits, and the gradient of both.
+ * With p = softmax(logits) (fp32; a token whose logits are all -infinity has p = 0), c_e the assignments of expert e, A their number, N the tokens with
+ * an assignment and P_e the mean of p_te over those tokens:
+ *   loss = coef * E * sum_e (c_e / A) P_e
+ *   expert_scale[t,j] = p[t, expert_idx[t,j]], divided by the sum over the token's k when renormalize != 0 and k > 1
+ * An entry of expert_idx outside [0, E) (the gate's E marks a pruned row) is no assignment: counted nowhere, scale 0, no gradient; a token without one
+ * takes no part.  No assignments at all: loss 0.
+ *   logits [T,E] dtype; expert_idx [T,k]; loss [1] fp32, counts [E] int32, prob_mean [E] fp32 (P), expert_scale [T,k] fp32,
+ *   weight [E] fp32: d loss / d p_te, the same for every token, which is all that the backward pass needs of the forward one
+ *   backward: dloss [1] fp32 and dscale [T,k] fp32, gradients of loss and of expert_scale, each may be NULL (zero); dlogits [T,E] in dtype.
+ * Counts take no gradient.  Limits: 1 <= k <= 8, k <= E <= 1024.  Sums are added in a fixed order.
+ */
+size_t moe_balance_loss_workspace_bytes(int T, int E);
+int moe_balance_loss(const void *logits, int dtype, const int32_t *expert_idx, int T, int E, int k, int renormalize, float coef, float *loss,
+                     int32_t *counts, float *prob_mean, float *expert_scale, float *weight, void *workspace, size_t workspace_bytes, void *stream);
+int moe_balance_loss_backward(const void *logits, int dtype, const int32_t *expert_idx, int T, int E, int k, int renormalize, const float *weight,
+                              const float *dloss, const float *dscale, void *dlogits, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

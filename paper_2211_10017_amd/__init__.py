@@ -10,3 +10,6 @@ from .layer import MoEExpertLayer  # noqa: E402,F401
 from .binding import (MoeError, moe_combine, moe_gate_topk, moe_grouped_ffn_wq,  # noqa: E402,F401
                       moe_grouped_ffn_wq_workspace_bytes, moe_permute, moe_permute_workspace_bytes,
                       moe_quantize_experts)
+from .binding import (moe_balance_loss, moe_balance_loss_backward, moe_grouped_ffn_mx4,  # noqa: E402,F401
+                      moe_grouped_ffn_mx4_workspace_bytes, moe_grouped_gemm_mx4, moe_mx4_dequantize, moe_mx4_quantize_experts,
+                      moe_mx4_quantize_rows)

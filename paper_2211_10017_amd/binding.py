@@ -25,7 +25,10 @@ EXPORTS = ["moe_last_error", "moe_last_ffn_kernels", "moe_device_info", "moe_abi
            "moe_grouped_ffn_wq_unsorted_supported", "moe_grouped_ffn_wq_unsorted_pays", "moe_grouped_ffn_wq_unsorted",
            "moe_grouped_ffn_wq_gated_supported", "moe_grouped_ffn_wq_gated_pays", "moe_grouped_ffn_wq_gated",
            "moe_grouped_ffn_wq_sliced_workspace_bytes", "moe_grouped_ffn_wq_sliced_pays", "moe_grouped_ffn_wq_sliced",
-           "moe_grouped_ffn_wq_noalloc_max_bytes", "moe_grouped_ffn_wq_noalloc"]
+           "moe_grouped_ffn_wq_noalloc_max_bytes", "moe_grouped_ffn_wq_noalloc",
+           "moe_mx4_quantize_rows", "moe_mx4_quantize_experts", "moe_mx4_dequantize", "moe_grouped_gemm_mx4",
+           "moe_grouped_ffn_mx4_workspace_bytes", "moe_grouped_ffn_mx4",
+           "moe_balance_loss_workspace_bytes", "moe_balance_loss", "moe_balance_loss_backward"]
 
 LAYER_MAX_EXPERTS = 256   # experts of a whole layer call: moe_gate_topk's limit (moe_permute: 1024, the FFN: 4096)
 
@@ -107,6 +110,25 @@ def load():
     lib.moe_grouped_gemm_wq.argtypes = [vp, vp, i, i, i, i, i, i, i, vp, vp, vp, i, vp]
     lib.moe_combine.restype = i
     lib.moe_combine.argtypes = [vp, i, vp, vp, vp, i, i, i, vp, i, vp]
+    i64, f = ctypes.c_int64, ctypes.c_float
+    lib.moe_mx4_quantize_rows.restype = i
+    lib.moe_mx4_quantize_rows.argtypes = [vp, i, i, i, i64, vp, vp, vp]
+    lib.moe_mx4_quantize_experts.restype = i
+    lib.moe_mx4_quantize_experts.argtypes = [vp, i, i, i, vp, vp, vp]
+    lib.moe_mx4_dequantize.restype = i
+    lib.moe_mx4_dequantize.argtypes = [vp, vp, i, i, i, vp, i, vp]
+    lib.moe_grouped_gemm_mx4.restype = i
+    lib.moe_grouped_gemm_mx4.argtypes = [vp, vp, i, vp, i, vp, i, i, i, i, i, vp, vp, vp, i, vp, i, vp]
+    lib.moe_grouped_ffn_mx4_workspace_bytes.restype = sz
+    lib.moe_grouped_ffn_mx4_workspace_bytes.argtypes = [i, i, i, i]
+    lib.moe_grouped_ffn_mx4.restype = i
+    lib.moe_grouped_ffn_mx4.argtypes = [vp, i, i, vp, i, vp, i, i, i, i, i, i, vp, vp, vp, vp, vp, vp, vp, i, vp, sz, vp]
+    lib.moe_balance_loss_workspace_bytes.restype = sz
+    lib.moe_balance_loss_workspace_bytes.argtypes = [i, i]
+    lib.moe_balance_loss.restype = i
+    lib.moe_balance_loss.argtypes = [vp, i, vp, i, i, i, i, f, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.moe_balance_loss_backward.restype = i
+    lib.moe_balance_loss_backward.argtypes = [vp, i, vp, i, i, i, i, vp, vp, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -424,3 +446,170 @@ def moe_grouped_ffn_wq_sliced(x, expert_idx, expert_scale, E: int, d: int, F: in
         _DT[out_dtype], _ptr(perm_src), _ptr(inv_perm), _ptr(offsets), _ptr(workspace), workspace.numel(), _stream())
     _check(rc, "moe_grouped_ffn_wq_sliced")
     return out, perm_src, inv_perm, offsets
+
+
+# ---- microscaled 4-bit floating point (codes [.., R, K/2] and scales [.., ceil(K/128), R, 4], include/moe_wq.h) ----------------------
+
+_FLOATS = (torch.float16, torch.bfloat16, torch.float32)
+
+
+def moe_mx4_shapes(rows: int, K: int):
+    """Shapes of the codes and the scales of `rows` rows of K values."""
+    return (rows, K // 2), (-(-K // 128), rows, 4)
+
+
+def _mx4_like(codes, scales, name):
+    """(matrices or None, rows, K) of codes and scales that belong together."""
+    if codes.dim() not in (2, 3) or codes.shape[-1] % 32:
+        raise MoeError("%s codes must be [R, K/2] or [E, N, K/2] with K %% 64 == 0, not %s" % (name, tuple(codes.shape)))
+    rows, K = codes.shape[-2], codes.shape[-1] * 2
+    if tuple(scales.shape) != tuple(codes.shape[:-2]) + moe_mx4_shapes(rows, K)[1] or scales.device != codes.device:
+        raise MoeError("%s scales must be [.., ceil(K/128), rows, 4] beside codes %s, not %s" % (name, tuple(codes.shape), tuple(scales.shape)))
+    return (codes.shape[0] if codes.dim() == 3 else None), rows, K
+
+
+def moe_mx4_quantize_rows(x, out=None):
+    """x [R, K] (rows may be strided) -> (codes uint8 [R, K/2], scales uint8 [ceil(K/128), R, 4])."""
+    if x.dim() != 2 or not x.is_cuda or x.dtype not in _FLOATS or (x.numel() and x.stride(1) != 1):
+        raise MoeError("x must be a [R, K] CUDA tensor of fp16, bf16 or fp32 whose rows are contiguous")
+    R, K = x.shape
+    stride = x.stride(0) if R > 1 else K
+    if out is None:
+        cs, ss = moe_mx4_shapes(R, K)
+        codes, scales = torch.empty(cs, dtype=torch.uint8, device=x.device), torch.empty(ss, dtype=torch.uint8, device=x.device)
+    else:
+        codes, scales = out
+        if _mx4_like(codes, scales, "out")[1:] != (R, K):
+            raise MoeError("out does not fit x")
+    rc = load().moe_mx4_quantize_rows(ctypes.c_void_p(x.data_ptr()), _DT[x.dtype], R, K, stride, _ptr(codes, torch.uint8, "codes"),
+                                      _ptr(scales, torch.uint8, "scales"), _stream())
+    _check(rc, "moe_mx4_quantize_rows")
+    return codes, scales
+
+
+def moe_mx4_quantize_experts(w, out=None):
+    """w fp32 [E, K, N] -> (codes uint8 [E, N, K/2], scales uint8 [E, ceil(K/128), N, 4])."""
+    E, K, N = w.shape
+    if out is None:
+        cs, ss = moe_mx4_shapes(N, K)
+        codes, scales = torch.empty((E,) + cs, dtype=torch.uint8, device=w.device), torch.empty((E,) + ss, dtype=torch.uint8, device=w.device)
+    else:
+        codes, scales = out
+        if _mx4_like(codes, scales, "out") != (E, N, K):
+            raise MoeError("out does not fit w")
+    rc = load().moe_mx4_quantize_experts(_ptr(w, torch.float32, "w"), E, K, N, _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), _stream())
+    _check(rc, "moe_mx4_quantize_experts")
+    return codes, scales
+
+
+def moe_mx4_dequantize(codes, scales, dtype=torch.bfloat16, out=None):
+    """The values that codes [.., R, K/2] and scales [.., ceil(K/128), R, 4] stand for, [.., R, K]."""
+    matrices, rows, K = _mx4_like(codes, scales, "the")
+    if out is None:
+        out = torch.empty(tuple(codes.shape[:-1]) + (K,), dtype=dtype, device=codes.device)
+    elif tuple(out.shape) != tuple(codes.shape[:-1]) + (K,):
+        raise MoeError("out must be %s" % (tuple(codes.shape[:-1]) + (K,),))
+    rc = load().moe_mx4_dequantize(_ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), 1 if matrices is None else matrices, rows, K,
+                                   _ptr(out, _FLOATS, "out"), _DT[out.dtype], _stream())
+    _check(rc, "moe_mx4_dequantize")
+    return out
+
+
+def _mx4_experts(codes, scales, expert_offsets, bias, name):
+    E, N, K = _mx4_like(codes, scales, name)
+    if E is None or expert_offsets.numel() != E + 1 or (bias is not None and tuple(bias.shape) != (E, N)):
+        raise MoeError("%s must be [E, N, K/2] beside E + 1 offsets and a bias [E, N]" % name)
+    return E, N, K
+
+
+def moe_grouped_gemm_mx4(a_codes, a_scales, expert_offsets, w_codes, w_scales, bias=None, activation=None, perm_src=None, k: int = 1,
+                         y_dtype=torch.float16, y=None, max_rows_per_expert: int = 0):
+    """y[r] = act(a[perm_src[r] / k] @ W[e]^T + bias[e]) for the rows r of every expert e; rows behind the last expert's are not written."""
+    E, N, K = _mx4_experts(w_codes, w_scales, expert_offsets, bias, "w")
+    matrices, rows, Ka = _mx4_like(a_codes, a_scales, "a")
+    if matrices is not None or Ka != K:
+        raise MoeError("a must be [R, K/2] with the weights' K = %d" % K)
+    R = rows if perm_src is None else perm_src.numel()
+    if y is None:
+        y = torch.empty((R, N), dtype=y_dtype, device=a_codes.device)
+    elif tuple(y.shape) != (R, N):
+        raise MoeError("y must be %s" % ((R, N),))
+    rc = load().moe_grouped_gemm_mx4(
+        _ptr(a_codes, torch.uint8, "a_codes"), _ptr(a_scales, torch.uint8, "a_scales"), rows, _ptr(perm_src, torch.int32, "perm_src"), k,
+        _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E, max_rows_per_expert, K, N, _ptr(w_codes, torch.uint8, "w_codes"),
+        _ptr(w_scales, torch.uint8, "w_scales"), _ptr(bias, torch.float16, "bias"), -1 if activation is None else ACTIVATIONS[activation],
+        _ptr(y, _FLOATS, "y"), _DT[y.dtype], _stream())
+    _check(rc, "moe_grouped_gemm_mx4")
+    return y
+
+
+def moe_grouped_ffn_mx4_workspace_bytes(T: int, R: int, d: int, F: int) -> int:
+    return int(load().moe_grouped_ffn_mx4_workspace_bytes(T, R, d, F))
+
+
+def moe_grouped_ffn_mx4(x, expert_offsets, w1_codes, w1_scales, w2_codes, w2_scales, b1=None, b2=None, perm_src=None, k: int = 1, y_dtype=None,
+                        y_perm=None, activation: str = "relu", max_rows_per_expert: int = 0, workspace=None):
+    """Expert FFN on 4-bit weights: x [T, d] -> y_perm [R, d], R = perm_src's length (T without one); rows behind the last expert's are not written."""
+    T, d = x.shape
+    E, F, K1 = _mx4_experts(w1_codes, w1_scales, expert_offsets, b1, "w1")
+    E2, d2, K2 = _mx4_experts(w2_codes, w2_scales, expert_offsets, b2, "w2")
+    if (E2, d2, K2, K1) != (E, d, F, d):
+        raise MoeError("w1 must be [E, F, d/2] and w2 [E, d, F/2] with x's d = %d" % d)
+    R = T if perm_src is None else perm_src.numel()
+    if y_perm is None:
+        y_perm = torch.empty((R, d), dtype=y_dtype or x.dtype, device=x.device)
+    elif tuple(y_perm.shape) != (R, d):
+        raise MoeError("y_perm must be %s" % ((R, d),))
+    if workspace is None:
+        workspace = torch.empty(moe_grouped_ffn_mx4_workspace_bytes(T, R, d, F), dtype=torch.uint8, device=x.device)
+    rc = load().moe_grouped_ffn_mx4(
+        _ptr(x, _FLOATS, "x"), _DT[x.dtype], T, _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E,
+        max_rows_per_expert, d, F, ACTIVATIONS[activation], _ptr(w1_codes, torch.uint8, "w1_codes"), _ptr(w1_scales, torch.uint8, "w1_scales"),
+        _ptr(b1, torch.float16, "b1"), _ptr(w2_codes, torch.uint8, "w2_codes"), _ptr(w2_scales, torch.uint8, "w2_scales"), _ptr(b2, torch.float16, "b2"),
+        _ptr(y_perm, _FLOATS, "y_perm"), _DT[y_perm.dtype], _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    _check(rc, "moe_grouped_ffn_mx4")
+    return y_perm
+
+
+# ---- the router's balance loss -------------------------------------------------------------------------------------------------------
+
+def _check_balance(logits, expert_idx):
+    if logits.dim() != 2 or expert_idx.dim() != 2 or expert_idx.shape[0] != logits.shape[0]:
+        raise MoeError("logits must be [T, E] and expert_idx [T, k]")
+
+
+def moe_balance_loss_workspace_bytes(T: int, E: int) -> int:
+    return int(load().moe_balance_loss_workspace_bytes(T, E))
+
+
+def moe_balance_loss(logits, expert_idx, coef: float = 0.01, renormalize: bool = True, workspace=None):
+    """(loss [], counts int32 [E], prob_mean [E], expert_scale [T, k], weight [E]); weight is what moe_balance_loss_backward takes."""
+    _check_balance(logits, expert_idx)
+    (T, E), k, dev = logits.shape, expert_idx.shape[1], logits.device
+    loss, prob_mean, weight = (torch.empty(s, dtype=torch.float32, device=dev) for s in ((), (E,), (E,)))
+    counts = torch.empty(E, dtype=torch.int32, device=dev)
+    scale = torch.empty((T, k), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = torch.empty(moe_balance_loss_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
+    rc = load().moe_balance_loss(_ptr(logits, _FLOATS, "logits"), _DT[logits.dtype], _ptr(expert_idx, torch.int32, "expert_idx"), T, E, k, int(renormalize),
+                                 coef, _ptr(loss), _ptr(counts), _ptr(prob_mean), _ptr(scale), _ptr(weight), _ptr(workspace, torch.uint8, "workspace"),
+                                 workspace.numel(), _stream())
+    _check(rc, "moe_balance_loss")
+    return loss, counts, prob_mean, scale, weight
+
+
+def moe_balance_loss_backward(logits, expert_idx, weight, dloss=None, dscale=None, renormalize: bool = True, out=None):
+    """Gradient of moe_balance_loss's loss and expert_scale with respect to the logits, in their type."""
+    _check_balance(logits, expert_idx)
+    (T, E), k = logits.shape, expert_idx.shape[1]
+    if weight.numel() != E or (dloss is not None and dloss.numel() != 1) or (dscale is not None and tuple(dscale.shape) != (T, k)):
+        raise MoeError("weight must be [E], dloss one number and dscale [T, k]")
+    if out is None:
+        out = torch.empty_like(logits)
+    elif out.shape != logits.shape:
+        raise MoeError("out must have the shape of logits")
+    rc = load().moe_balance_loss_backward(_ptr(logits, _FLOATS, "logits"), _DT[logits.dtype], _ptr(expert_idx, torch.int32, "expert_idx"), T, E, k,
+                                          int(renormalize), _ptr(weight, torch.float32, "weight"), _ptr(dloss, torch.float32, "dloss"),
+                                          _ptr(dscale, torch.float32, "dscale"), _ptr(out, logits.dtype, "out"), _stream())
+    _check(rc, "moe_balance_loss_backward")
+    return out

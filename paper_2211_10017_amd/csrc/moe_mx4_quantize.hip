@@ -1,0 +1,194 @@
+// moe_mx4_quantize_rows, moe_mx4_quantize_experts, moe_mx4_dequantize: values to and from the microscaled 4-bit format.
+#include <type_traits>
+
+#include "moe_mx4_common.h"
+
+namespace moe {
+
+__device__ inline uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Eight neighbouring values of a row as fp32.
+template <int DT>
+__device__ inline void load_eight(const void *base, size_t at, float (&v)[8])
+{
+    if constexpr (DT == MOE_F32) {
+        const f32x4_t *q = reinterpret_cast<const f32x4_t *>(reinterpret_cast<const float *>(base) + at);
+        const f32x4_t a = q[0], b = q[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    } else {
+        const u32x4_t w = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const uint16_t *>(base) + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint16_t b = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+            v[i] = DT == MOE_BF16 ? __uint_as_float((uint32_t)b << 16) : (float)__builtin_bit_cast(_Float16, b);
+        }
+    }
+}
+
+// Sixteen lanes hold 128 values of a row, eight each: the largest magnitude of a block is that of four neighbouring lanes, and every lane of
+// the sixteen gets the four scale bytes as the dword that is stored.
+__device__ inline uint32_t sixteen_lane_scales(uint32_t amax, uint32_t &byte)
+{
+    amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0xb1, 0xf, 0xf, true));      // quad_perm 1,0,3,2
+    amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0x4e, 0xf, 0xf, true));      // quad_perm 2,3,0,1
+    byte = mx_scale_byte(amax);
+    const int lane = threadIdx.x & 63, quad = (lane >> 2) & 3;
+    uint32_t d = byte << (8 * quad);
+    d |= __shfl_xor(d, 4);
+    d |= __shfl_xor(d, 8);
+    return d;
+}
+
+// Rows: a wavefront takes four rows by 128 values at a time, sixteen lanes a row, so that loads are whole lines and the scales of a block's
+// sixteen rows one 64-byte piece.  Memory-bound: reads K values of a row once, writes 17/32 byte each.
+template <int DT>
+__global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const void *__restrict__ x, int R, int K, long stride, int per,
+                                                                uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
+{
+    const int tid = threadIdx.x, part = tid & 15;
+    const int G = mx_groups(K), chunks = (G + per - 1) / per;
+    const int row = (int)(blockIdx.x / chunks) * 16 + (tid >> 4), g0 = (int)(blockIdx.x % chunks) * per;
+    const bool live = row < R;
+    for (int g = g0; g < min(g0 + per, G); ++g) {
+        const int k = g * kMxGroup + part * 8;
+        float v[8] = {};
+        if (live && k < K) load_eight<DT>(x, (size_t)row * stride + k, v);
+        uint32_t amax = 0, byte;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = max(amax, abs_bits(v[i]));
+        const uint32_t d = sixteen_lane_scales(amax, byte);
+        if (!live) continue;
+        if (k < K) *reinterpret_cast<uint32_t *>(codes + (size_t)row * (K / 2) + k / 2) = mx_codes(v, byte);
+        if (part == 0) *reinterpret_cast<uint32_t *>(scales + ((size_t)g * R + row) * 4) = d;
+    }
+}
+
+// Experts: w is [K, N] with N contiguous and a block runs along K: a lane owns a channel and walks down 128 values of it, so that loads are
+// whole lines and so are a wavefront's scales.
+__global__ __launch_bounds__(256) void mx4_quantize_experts_kernel(const float *__restrict__ w, int K, int N, uint8_t *__restrict__ codes,
+                                                                   uint8_t *__restrict__ scales)
+{
+    const int G = mx_groups(K), ncol = (N + 255) / 256;
+    const int g = (int)(blockIdx.x / ncol % G), n = (int)(blockIdx.x % ncol) * 256 + threadIdx.x;
+    const size_t e = blockIdx.x / ncol / G;
+    if (n >= N) return;
+    w += (e * K + (size_t)g * kMxGroup) * N + n;
+    uint32_t d = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        if (g * kMxGroup + b * kMxBlock >= K) break;
+        float v[32];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = w[(size_t)(b * 32 + i) * N];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) amax = max(amax, abs_bits(v[i]));
+        const uint32_t byte = mx_scale_byte(amax);
+        d |= byte << (8 * b);
+        u32x4_t c;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float t[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
+            c[q] = mx_codes(t, byte);
+        }
+        *reinterpret_cast<u32x4_t *>(codes + (e * N + n) * (size_t)(K / 2) + g * 64 + b * 16) = c;
+    }
+    *reinterpret_cast<uint32_t *>(scales + ((e * G + g) * (size_t)N + n) * 4) = d;
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, long rows, int per_matrix,
+                                                             int K, void *__restrict__ out)
+{
+    const int part = threadIdx.x & 15, G = mx_groups(K);
+    const long row = (long)(blockIdx.x / G) * 16 + (threadIdx.x >> 4);
+    const int g = (int)(blockIdx.x % G), k = g * kMxGroup + part * 8;
+    if (row >= rows || k >= K) return;
+    const long m = row / per_matrix, n = row % per_matrix;
+    const uint32_t c = *reinterpret_cast<const uint32_t *>(codes + (size_t)row * (K / 2) + k / 2);
+    const uint32_t byte = scales[(((size_t)m * G + g) * per_matrix + n) * 4 + (part >> 2)];
+    const float s = mx_scale_value(byte);
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3)};
+    const size_t at = (size_t)row * K + k;
+    if constexpr (DT == MOE_F32) {
+        f32x4_t *q = reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(out) + at);
+        q[0] = f32x4_t{p[0][0] * s, p[0][1] * s, p[1][0] * s, p[1][1] * s};
+        q[1] = f32x4_t{p[2][0] * s, p[2][1] * s, p[3][0] * s, p[3][1] * s};
+    } else {
+        u32x4_t w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = p[i][0] * s, hi = p[i][1] * s;
+            if (DT == MOE_BF16) w[i] = (uint32_t)to_bf16_rne(lo) | ((uint32_t)to_bf16_rne(hi) << 16);
+            else w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16);
+        }
+        *reinterpret_cast<u32x4_t *>(reinterpret_cast<uint16_t *>(out) + at) = w;
+    }
+}
+
+constexpr double kMostBlocks = 0xffffff;          // of 256 threads: a launch takes fewer than 2^32 threads
+
+int launch_mx4_quantize_rows(const void *x, int dtype, int R, int K, long stride, uint8_t *codes, uint8_t *scales, hipStream_t s)
+{
+    const int G = mx_groups(K), per = (long)R * G >= 16384 ? 4 : 1;
+    const long blocks = (long)((R + 15) / 16) * ((G + per - 1) / per);
+    if (blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "moe_mx4_quantize_rows: %ld workgroups exceed one launch", blocks);
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, R, K, stride, per, codes, scales); };
+    if (dtype == MOE_F16) run(&mx4_quantize_rows_kernel<MOE_F16>);
+    else if (dtype == MOE_BF16) run(&mx4_quantize_rows_kernel<MOE_BF16>);
+    else run(&mx4_quantize_rows_kernel<MOE_F32>);
+    return check_launch("moe_mx4_quantize_rows");
+}
+
+}  // namespace moe
+
+extern "C" int moe_mx4_quantize_rows(const void *x, int x_dtype, int R, int K, int64_t x_stride, void *codes, void *scales, void *stream)
+{
+    using namespace moe;
+    const char *what = "moe_mx4_quantize_rows";
+    if (R < 0 || K <= 0 || K % 64) return fail(MOE_ERR_INVALID_ARG, "%s: need R >= 0 and K a positive multiple of 64", what);
+    if (x_dtype < 0 || x_dtype > 2) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
+    if (R == 0) return MOE_OK;                                  // empty buffers may be NULL
+    if (!x || !codes || !scales) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned16(x) || !aligned16(codes) || !aligned16(scales)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
+    if (x_stride < K || x_stride % (x_dtype == MOE_F32 ? 4 : 8)) return fail(MOE_ERR_INVALID_ARG, "%s: rows of x must be K values or more and 16-byte aligned", what);
+    return launch_mx4_quantize_rows(x, x_dtype, R, K, x_stride, (uint8_t *)codes, (uint8_t *)scales, as_stream(stream));
+}
+
+extern "C" int moe_mx4_quantize_experts(const float *w, int E, int K, int N, void *codes, void *scales, void *stream)
+{
+    using namespace moe;
+    const char *what = "moe_mx4_quantize_experts";
+    if (E < 0 || K <= 0 || N <= 0 || K % 64 || N % 32) return fail(MOE_ERR_INVALID_ARG, "%s: need E >= 0, K %% 64 == 0 and N %% 32 == 0", what);
+    if (E == 0) return MOE_OK;
+    if (!w || !codes || !scales) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned16(w) || !aligned16(codes) || !aligned16(scales)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
+    const double blocks = (double)E * mx_groups(K) * ((N + 255) / 256);
+    if (blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "%s: %.0f workgroups exceed one launch", what, blocks);
+    hipLaunchKernelGGL(mx4_quantize_experts_kernel, dim3((unsigned)blocks), dim3(256), 0, as_stream(stream), w, K, N, (uint8_t *)codes, (uint8_t *)scales);
+    return check_launch(what);
+}
+
+extern "C" int moe_mx4_dequantize(const void *codes, const void *scales, int matrices, int rows, int K, void *out, int out_dtype, void *stream)
+{
+    using namespace moe;
+    const char *what = "moe_mx4_dequantize";
+    if (matrices < 0 || rows < 0 || K <= 0 || K % 64) return fail(MOE_ERR_INVALID_ARG, "%s: need matrices, rows >= 0 and K a positive multiple of 64", what);
+    if (out_dtype < 0 || out_dtype > 2) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
+    if (matrices == 0 || rows == 0) return MOE_OK;
+    if (!codes || !scales || !out) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned16(codes) || !aligned16(scales) || !aligned16(out)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
+    const long all = (long)matrices * rows;
+    const double blocks = (double)((all + 15) / 16) * mx_groups(K);
+    if (blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "%s: %.0f workgroups exceed one launch", what, blocks);
+    auto run = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, as_stream(stream), (const uint8_t *)codes, (const uint8_t *)scales, all, rows, K, out);
+    };
+    if (out_dtype == MOE_F16) run(&mx4_dequantize_kernel<MOE_F16>);
+    else if (out_dtype == MOE_BF16) run(&mx4_dequantize_kernel<MOE_BF16>);
+    else run(&mx4_dequantize_kernel<MOE_F32>);
+    return check_launch(what);
+}
