@@ -19,7 +19,7 @@ TILED = ["moe_ffn_tiled_4.hip", "moe_ffn_tiled_4_exact.hip", "moe_ffn_tiled_8.hi
 
 SOURCES = ["moe_errors.hip", "moe_quantize.hip", "moe_gate.hip", "moe_permute.hip", "moe_ffn.hip", "moe_ffn_tiled.hip", "moe_ffn_tiled_4.hip", "moe_ffn_tiled_4_exact.hip",
            "moe_ffn_tiled_8.hip", "moe_ffn_tiled_8_exact.hip", "moe_ffn_ring_4.hip", "moe_ffn_ring_8.hip", "moe_ffn_stream.hip", "moe_ffn_decode.hip",
-           "moe_combine.hip", "moe_mx4.hip", "moe_mx4_quantize.hip", "moe_mx4_stream.hip", "moe_balance.hip"]
+           "moe_combine.hip", "moe_mx4.hip", "moe_mx4_quantize.hip", "moe_mx4_stream.hip", "moe_mx4_tiled.hip", "moe_balance.hip"]
 
 # packed-fp32 VALU forms are switched off for every translation unit of this library
 HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-I" + INCLUDE, "-I" + CSRC,

@@ -8,13 +8,6 @@ namespace moe {
 // Accumulator of one tile: weights are the matrix instruction's first operand, so a lane holds one row (lane & 31) and, with h = lane >> 5, the
 // channels 8 q + 4 h + i, q, i = 0..3, of the slab: a block of 32 channels of a row is in two lanes, and quantising the result for the next
 // product takes one exchange between them.
-// As activate(), but a NaN stays one (fmaxf would make it 0, and a row with a NaN in it would come out as numbers).
-__device__ inline float mx_activate(float v, int act)
-{
-    if (act == MOE_ACT_RELU) return v < 0.0f ? 0.0f : v;
-    return activate(v, act);
-}
-
 template <int OUT>      // MOE_F16, MOE_BF16, MOE_F32, or -1: the 4-bit format
 __device__ __forceinline__ void mx_store_tile(const MxArgs &p, const float16_t &acc, int e, int n0, int row, bool live)
 {
@@ -30,9 +23,12 @@ __device__ __forceinline__ void mx_store_tile(const MxArgs &p, const float16_t &
             for (int i = 0; i < 4; ++i) v[4 * q + i] += (float)__builtin_bit_cast(_Float16, (uint16_t)(b[i >> 1] >> (16 * (i & 1))));
         }
     }
-    if (p.act != MOE_ACT_NONE) {
+    if (p.act == MOE_ACT_RELU) {            // (not fmaxf, which would make a 0 of a NaN, and numbers of a row that holds one)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = mx_activate(v[i], p.act);
+        for (int i = 0; i < 16; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+    } else if (p.act == MOE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = gelu(v[i]);
     }
     if constexpr (OUT < 0) {
         uint32_t amax = 0;

@@ -70,6 +70,8 @@ __global__ __launch_bounds__(256) void mx4_stream_kernel(MxArgs p)
 
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
 {
+    const int mean = (p.R + p.E - 1) / p.E;
+    if (mean > 24) return launch_mx4_tiled(p, mean <= 64 ? 64 : mean <= 128 ? 128 : 256, s);
     const long slots = (long)p.R / 32 + (p.E < p.R ? p.E : p.R);
     const long wgs = (slots * (p.N / 32) + kXcds - 1) / kXcds * kXcds;         // upper bound of the work items, whole rounds of XCDs
     if (wgs > 0xffffff) return fail(MOE_ERR_UNSUPPORTED, "moe_grouped_gemm_mx4: %ld workgroups exceed one launch", wgs);
