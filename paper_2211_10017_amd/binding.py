@@ -460,28 +460,36 @@ def moe_mx4_shapes(rows: int, K: int):
 
 def _mx4_like(codes, scales, name):
     """(matrices or None, rows, K) of codes and scales that belong together."""
-    if codes.dim() not in (2, 3) or codes.shape[-1] % 32:
-        raise MoeError("%s codes must be [R, K/2] or [E, N, K/2] with K %% 64 == 0, not %s" % (name, tuple(codes.shape)))
-    rows, K = codes.shape[-2], codes.shape[-1] * 2
-    if tuple(scales.shape) != tuple(codes.shape[:-2]) + moe_mx4_shapes(rows, K)[1] or scales.device != codes.device:
-        raise MoeError("%s scales must be [.., ceil(K/128), rows, 4] beside codes %s, not %s" % (name, tuple(codes.shape), tuple(scales.shape)))
-    return (codes.shape[0] if codes.dim() == 3 else None), rows, K
+    cs = codes.shape
+    if len(cs) == 2:
+        (rows, half), matrices = cs, None
+        want = (-(-half // 64), rows, 4)
+    elif len(cs) == 3:
+        matrices, rows, half = cs
+        want = (matrices, -(-half // 64), rows, 4)
+    else:
+        half = 1
+    if half % 32:
+        raise MoeError("%s codes must be [R, K/2] or [E, N, K/2] with K %% 64 == 0, not %s" % (name, tuple(cs)))
+    if scales.shape != want:
+        raise MoeError("%s scales must be [.., ceil(K/128), rows, 4] beside codes %s, not %s" % (name, tuple(cs), tuple(scales.shape)))
+    return matrices, rows, 2 * half
 
 
 def moe_mx4_quantize_rows(x, out=None):
     """x [R, K] (rows may be strided) -> (codes uint8 [R, K/2], scales uint8 [ceil(K/128), R, 4])."""
-    if x.dim() != 2 or not x.is_cuda or x.dtype not in _FLOATS or (x.numel() and x.stride(1) != 1):
+    if x.dim() != 2 or not x.is_cuda or x.dtype not in _FLOATS or (x.shape[1] > 1 and x.stride(1) != 1):
         raise MoeError("x must be a [R, K] CUDA tensor of fp16, bf16 or fp32 whose rows are contiguous")
     R, K = x.shape
     stride = x.stride(0) if R > 1 else K
     if out is None:
-        cs, ss = moe_mx4_shapes(R, K)
-        codes, scales = torch.empty(cs, dtype=torch.uint8, device=x.device), torch.empty(ss, dtype=torch.uint8, device=x.device)
+        dev = x.device
+        codes, scales = torch.empty(R, K // 2, dtype=torch.uint8, device=dev), torch.empty(-(-K // 128), R, 4, dtype=torch.uint8, device=dev)
     else:
         codes, scales = out
         if _mx4_like(codes, scales, "out")[1:] != (R, K):
             raise MoeError("out does not fit x")
-    rc = load().moe_mx4_quantize_rows(ctypes.c_void_p(x.data_ptr()), _DT[x.dtype], R, K, stride, _ptr(codes, torch.uint8, "codes"),
+    rc = load().moe_mx4_quantize_rows(x.data_ptr(), _DT[x.dtype], R, K, stride, _ptr(codes, torch.uint8, "codes"),
                                       _ptr(scales, torch.uint8, "scales"), _stream())
     _check(rc, "moe_mx4_quantize_rows")
     return codes, scales
@@ -506,7 +514,8 @@ def moe_mx4_dequantize(codes, scales, dtype=torch.bfloat16, out=None):
     """The values that codes [.., R, K/2] and scales [.., ceil(K/128), R, 4] stand for, [.., R, K]."""
     matrices, rows, K = _mx4_like(codes, scales, "the")
     if out is None:
-        out = torch.empty(tuple(codes.shape[:-1]) + (K,), dtype=dtype, device=codes.device)
+        out = (torch.empty(rows, K, dtype=dtype, device=codes.device) if matrices is None
+               else torch.empty(matrices, rows, K, dtype=dtype, device=codes.device))
     elif tuple(out.shape) != tuple(codes.shape[:-1]) + (K,):
         raise MoeError("out must be %s" % (tuple(codes.shape[:-1]) + (K,),))
     rc = load().moe_mx4_dequantize(_ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), 1 if matrices is None else matrices, rows, K,
@@ -517,7 +526,7 @@ def moe_mx4_dequantize(codes, scales, dtype=torch.bfloat16, out=None):
 
 def _mx4_experts(codes, scales, expert_offsets, bias, name):
     E, N, K = _mx4_like(codes, scales, name)
-    if E is None or expert_offsets.numel() != E + 1 or (bias is not None and tuple(bias.shape) != (E, N)):
+    if E is None or expert_offsets.numel() != E + 1 or (bias is not None and bias.shape != (E, N)):
         raise MoeError("%s must be [E, N, K/2] beside E + 1 offsets and a bias [E, N]" % name)
     return E, N, K
 
@@ -531,8 +540,8 @@ def moe_grouped_gemm_mx4(a_codes, a_scales, expert_offsets, w_codes, w_scales, b
         raise MoeError("a must be [R, K/2] with the weights' K = %d" % K)
     R = rows if perm_src is None else perm_src.numel()
     if y is None:
-        y = torch.empty((R, N), dtype=y_dtype, device=a_codes.device)
-    elif tuple(y.shape) != (R, N):
+        y = torch.empty(R, N, dtype=y_dtype, device=a_codes.device)
+    elif y.shape != (R, N):
         raise MoeError("y must be %s" % ((R, N),))
     rc = load().moe_grouped_gemm_mx4(
         _ptr(a_codes, torch.uint8, "a_codes"), _ptr(a_scales, torch.uint8, "a_scales"), rows, _ptr(perm_src, torch.int32, "perm_src"), k,
@@ -557,12 +566,13 @@ def moe_grouped_ffn_mx4(x, expert_offsets, w1_codes, w1_scales, w2_codes, w2_sca
         raise MoeError("w1 must be [E, F, d/2] and w2 [E, d, F/2] with x's d = %d" % d)
     R = T if perm_src is None else perm_src.numel()
     if y_perm is None:
-        y_perm = torch.empty((R, d), dtype=y_dtype or x.dtype, device=x.device)
-    elif tuple(y_perm.shape) != (R, d):
+        y_perm = torch.empty(R, d, dtype=y_dtype or x.dtype, device=x.device)
+    elif y_perm.shape != (R, d):
         raise MoeError("y_perm must be %s" % ((R, d),))
+    lib = load()
     if workspace is None:
-        workspace = torch.empty(moe_grouped_ffn_mx4_workspace_bytes(T, R, d, F), dtype=torch.uint8, device=x.device)
-    rc = load().moe_grouped_ffn_mx4(
+        workspace = torch.empty(lib.moe_grouped_ffn_mx4_workspace_bytes(T, R, d, F), dtype=torch.uint8, device=x.device)
+    rc = lib.moe_grouped_ffn_mx4(
         _ptr(x, _FLOATS, "x"), _DT[x.dtype], T, _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E,
         max_rows_per_expert, d, F, ACTIVATIONS[activation], _ptr(w1_codes, torch.uint8, "w1_codes"), _ptr(w1_scales, torch.uint8, "w1_scales"),
         _ptr(b1, torch.float16, "b1"), _ptr(w2_codes, torch.uint8, "w2_codes"), _ptr(w2_scales, torch.uint8, "w2_scales"), _ptr(b2, torch.float16, "b2"),
@@ -586,14 +596,15 @@ def moe_balance_loss(logits, expert_idx, coef: float = 0.01, renormalize: bool =
     """(loss [], counts int32 [E], prob_mean [E], expert_scale [T, k], weight [E]); weight is what moe_balance_loss_backward takes."""
     _check_balance(logits, expert_idx)
     (T, E), k, dev = logits.shape, expert_idx.shape[1], logits.device
-    loss, prob_mean, weight = (torch.empty(s, dtype=torch.float32, device=dev) for s in ((), (E,), (E,)))
+    lib, f32 = load(), torch.float32
+    loss, prob_mean, weight = (torch.empty((), dtype=f32, device=dev), torch.empty(E, dtype=f32, device=dev), torch.empty(E, dtype=f32, device=dev))
     counts = torch.empty(E, dtype=torch.int32, device=dev)
-    scale = torch.empty((T, k), dtype=torch.float32, device=dev)
+    scale = torch.empty(T, k, dtype=f32, device=dev)
     if workspace is None:
-        workspace = torch.empty(moe_balance_loss_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
-    rc = load().moe_balance_loss(_ptr(logits, _FLOATS, "logits"), _DT[logits.dtype], _ptr(expert_idx, torch.int32, "expert_idx"), T, E, k, int(renormalize),
-                                 coef, _ptr(loss), _ptr(counts), _ptr(prob_mean), _ptr(scale), _ptr(weight), _ptr(workspace, torch.uint8, "workspace"),
-                                 workspace.numel(), _stream())
+        workspace = torch.empty(lib.moe_balance_loss_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
+    rc = lib.moe_balance_loss(_ptr(logits, _FLOATS, "logits"), _DT[logits.dtype], _ptr(expert_idx, torch.int32, "expert_idx"), T, E, k, int(renormalize),
+                              coef, loss.data_ptr(), counts.data_ptr(), prob_mean.data_ptr(), scale.data_ptr(), weight.data_ptr(),
+                              _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
     _check(rc, "moe_balance_loss")
     return loss, counts, prob_mean, scale, weight
 
@@ -602,7 +613,7 @@ def moe_balance_loss_backward(logits, expert_idx, weight, dloss=None, dscale=Non
     """Gradient of moe_balance_loss's loss and expert_scale with respect to the logits, in their type."""
     _check_balance(logits, expert_idx)
     (T, E), k = logits.shape, expert_idx.shape[1]
-    if weight.numel() != E or (dloss is not None and dloss.numel() != 1) or (dscale is not None and tuple(dscale.shape) != (T, k)):
+    if weight.numel() != E or (dloss is not None and dloss.numel() != 1) or (dscale is not None and dscale.shape != (T, k)):
         raise MoeError("weight must be [E], dloss one number and dscale [T, k]")
     if out is None:
         out = torch.empty_like(logits)

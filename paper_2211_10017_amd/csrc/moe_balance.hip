@@ -16,7 +16,7 @@
 
 namespace moe {
 
-constexpr int kBalanceThreads = 512, kBalanceMostBlocks = 256, kBalanceMostExperts = 1024, kBalanceMostK = 8;
+constexpr int kBalanceMostBlocks = 256, kBalanceMostExperts = 1024, kBalanceMostK = 8;
 
 struct BalanceArgs {
     const void *logits;         // [T, E]
@@ -24,8 +24,9 @@ struct BalanceArgs {
     int T, E, k, renorm, L;     // L: lanes of a token, a power of two
     float coef;
     float *scale;               // [T, k]
-    float *part;                // [blocks, E] sums of p
-    int32_t *part_count;        // [blocks, E + 1]: assignments, and tokens with one
+    float *part;                // [blocks, E rounded up to four] sums of p
+    int32_t *part_count;        // the same, assignments
+    int32_t *part_live;         // [blocks] tokens with an assignment
     float *loss, *prob_mean, *weight;
     int32_t *counts;
     // backward
@@ -33,25 +34,47 @@ struct BalanceArgs {
     void *dlogits;
 };
 
-// V neighbouring logits at column c of token t as fp32; -infinity past the end.
-template <int DT, int V>
-__device__ inline void load_logits(const BalanceArgs &a, int t, int c, float (&v)[V])
+template <int DT>
+__device__ inline float to_f32(uint32_t bits)
 {
-    const size_t at = (size_t)t * a.E + c;
-    if constexpr (V == 1) {
-        if constexpr (DT == MOE_F32) v[0] = reinterpret_cast<const float *>(a.logits)[at];
-        else if constexpr (DT == MOE_F16) v[0] = (float)reinterpret_cast<const _Float16 *>(a.logits)[at];
-        else v[0] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(a.logits)[at] << 16);
-    } else if constexpr (DT == MOE_F32) {
-        const float4 q = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(a.logits) + at);
-        v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
-    } else {
-        const uint2 q = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(a.logits) + at);
-        const uint16_t b[4] = {(uint16_t)q.x, (uint16_t)(q.x >> 16), (uint16_t)q.y, (uint16_t)(q.y >> 16)};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = DT == MOE_BF16 ? __uint_as_float((uint32_t)b[i] << 16) : (float)__builtin_bit_cast(_Float16, b[i]);
-    }
+    if (DT == MOE_F32) return __uint_as_float(bits);
+    if (DT == MOE_F16) return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+    return __uint_as_float(bits << 16);
 }
+
+// What a lane holds of a token: V neighbouring logits in each of S steps, as they lie in memory, and the token's experts.  Requested one token ahead.
+template <int DT, int V, int S>
+struct TokenLoad {
+    static constexpr int W = V == 1 ? 1 : DT == MOE_F32 ? 4 : 2;      // words of a step
+    uint32_t raw[S][W];
+    int e[kBalanceMostK];
+
+    __device__ inline void request(const BalanceArgs &a, int t, int lane_in)
+    {
+#pragma unroll
+        for (int j = 0; j < kBalanceMostK; ++j)
+            if (j < a.k) e[j] = a.idx[(size_t)t * a.k + j];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int c = V * (lane_in + a.L * s);
+            const size_t at = (size_t)t * a.E + min(c, a.E - V);      // (past the end: what the last lane holds, which value() leaves out)
+            if constexpr (V == 1) raw[s][0] = DT == MOE_F32 ? reinterpret_cast<const uint32_t *>(a.logits)[at] : reinterpret_cast<const uint16_t *>(a.logits)[at];
+            else if constexpr (DT == MOE_F32) {
+                const uint4 q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const float *>(a.logits) + at);
+                raw[s][0] = q.x, raw[s][1] = q.y, raw[s][2] = q.z, raw[s][3] = q.w;
+            } else {
+                const uint2 q = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(a.logits) + at);
+                raw[s][0] = q.x, raw[s][1] = q.y;
+            }
+        }
+    }
+    __device__ inline float value(const BalanceArgs &a, int s, int i, int lane_in) const
+    {
+        if (V * (lane_in + a.L * s) >= a.E) return -INFINITY;
+        if (V == 1 || DT == MOE_F32) return to_f32<DT>(raw[s][i]);
+        return to_f32<DT>(i & 1 ? raw[s][i >> 1] >> 16 : raw[s][i >> 1] & 0xffffu);
+    }
+};
 
 template <int DT, int V>
 __device__ inline void store_logits(const BalanceArgs &a, int t, int c, const float (&v)[V])
@@ -67,34 +90,33 @@ __device__ inline void store_logits(const BalanceArgs &a, int t, int c, const fl
     else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(a.dlogits) + at) = make_uint2(b[0] | (uint32_t)b[1] << 16, b[2] | (uint32_t)b[3] << 16);
 }
 
-__device__ inline float lanes_max(float v, int L)
+// op over the L lanes of a token, in the vector unit's own lane permutations up to sixteen of them.
+template <class Op>
+__device__ inline float over_lanes(float v, int L, Op op)
 {
-    for (int o = 1; o < L; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ inline float lanes_sum(float v, int L)
-{
-    for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o);
+    auto dpp = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    using std::integral_constant;
+    if (L > 1) v = op(v, dpp(integral_constant<int, 0xb1>{}));        // quad_perm 1,0,3,2
+    if (L > 2) v = op(v, dpp(integral_constant<int, 0x4e>{}));        // quad_perm 2,3,0,1
+    if (L > 4) v = op(v, dpp(integral_constant<int, 0x141>{}));       // row_half_mirror
+    if (L > 8) v = op(v, dpp(integral_constant<int, 0x140>{}));       // row_mirror
+    if (L > 16) v = op(v, __shfl_xor(v, 16));
+    if (L > 32) v = op(v, __shfl_xor(v, 32));
     return v;
 }
 
-// Softmax of a token over its L lanes: p[s][i] of column V (lane_in + L s) + i.  A token whose logits are all -infinity has nothing to choose: p = 0.
-// (A NaN or +infinity among them makes its p NaN.)
+// Softmax of a token over its L lanes: p[s][i] of column V (lane_in + L s) + i, and what makes a probability of any other logit of it: exp(z - base) inv.
+// A token whose logits are all -infinity has nothing to choose: p = 0.  (A NaN or +infinity among them makes its p NaN.)
 template <int DT, int V, int S>
-__device__ inline void token_softmax(const BalanceArgs &a, int t, int lane_in, float (&p)[S][V])
+__device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V, S> &x, int lane_in, float (&p)[S][V], float &base, float &inv)
 {
     float m = -INFINITY;
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int c = V * (lane_in + a.L * s);
+    for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int i = 0; i < V; ++i) p[s][i] = -INFINITY;
-        if (c < a.E) load_logits<DT, V>(a, t, c, p[s]);
-#pragma unroll
-        for (int i = 0; i < V; ++i) m = fmaxf(m, p[s][i]);
-    }
-    m = lanes_max(m, a.L);
-    const float base = m == -INFINITY ? 0.0f : m;
+        for (int i = 0; i < V; ++i) p[s][i] = x.value(a, s, i, lane_in), m = fmaxf(m, p[s][i]);
+    m = over_lanes(m, a.L, [](float u, float v) { return fmaxf(u, v); });
+    base = m == -INFINITY ? 0.0f : m;
     float sum = 0.0f;
 #pragma unroll
     for (int s = 0; s < S; ++s)
@@ -103,68 +125,75 @@ __device__ inline void token_softmax(const BalanceArgs &a, int t, int lane_in, f
             p[s][i] = expf(p[s][i] - base);
             sum += p[s][i];
         }
-    sum = lanes_sum(sum, a.L);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    sum = over_lanes(sum, a.L, [](float u, float v) { return u + v; });
+    inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int i = 0; i < V; ++i) p[s][i] *= inv;
 }
 
-// p of expert e, which one of the token's lanes holds, for all of them.
-template <int V, int S>
-__device__ inline float of_expert(const float (&p)[S][V], int e, int lane_in, int L)
+// Logit of expert e (the first one for a slot without an expert).
+template <int DT>
+__device__ inline float logit_of(const BalanceArgs &a, int t, int e)
 {
-    const int lane = threadIdx.x & 63, col = e / V, owner = col % L;
-    float mine = 0.0f;
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (s * L + lane_in == col && i == e % V) mine = p[s][i];
-    return __shfl(mine, (lane & ~(L - 1)) + owner);
+    const size_t at = (size_t)t * a.E + (e >= 0 && e < a.E ? e : 0);
+    return to_f32<DT>(DT == MOE_F32 ? reinterpret_cast<const uint32_t *>(a.logits)[at] : reinterpret_cast<const uint16_t *>(a.logits)[at]);
+}
+
+// The tokens of a thread's L lanes, one after the other, the next one's loads ahead of the work on this one: f(token, whether it is there, loads).
+template <int DT, int V, int S, class F>
+__device__ inline void for_tokens(const BalanceArgs &a, int lane_in, F f)
+{
+    const int per = blockDim.x / a.L, mine = threadIdx.x / a.L;
+    const long step = (long)gridDim.x * per;
+    auto at = [&](long t) { return (int)(t < a.T ? t : a.T - 1); };
+    long t = (long)blockIdx.x * per + mine;
+    const long end = (long)blockIdx.x * per;                       // (the block's first token: its loop ends for all of its threads at once)
+    TokenLoad<DT, V, S> now, next;
+    now.request(a, at(t), lane_in);
+    for (long first = end; first < a.T; first += step, t += step) {
+        next.request(a, at(t + step), lane_in);
+        f(at(t), t < a.T, now);
+        now = next;
+    }
 }
 
 template <int DT, int V, int S>
-__global__ __launch_bounds__(kBalanceThreads) void balance_forward_kernel(BalanceArgs a)
+__global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
 {
-    __shared__ float sums[kBalanceThreads / 64][kBalanceMostExperts];
+    extern __shared__ float sums[];                             // [wavefronts][E]
     __shared__ int32_t cnt[kBalanceMostExperts + 1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, L = a.L, lane_in = lane & (L - 1);
-    for (int i = tid; i <= a.E; i += kBalanceThreads) cnt[i] = 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x / 64, L = a.L, lane_in = lane & (L - 1);
+    for (int i = tid; i <= a.E; i += blockDim.x) cnt[i] = 0;
     __syncthreads();
     float acc[S][V] = {};
-    const int per = kBalanceThreads / L;                       // tokens of a block at a time
-    for (long t0 = (long)blockIdx.x * per; t0 < a.T; t0 += (long)gridDim.x * per) {
-        const bool here = t0 + tid / L < a.T;
-        const int t = here ? (int)(t0 + tid / L) : a.T - 1;
-        float p[S][V];
-        token_softmax<DT, V, S>(a, t, lane_in, p);
+    for_tokens<DT, V, S>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S> &x) {
+        float chosen[kBalanceMostK], total = 0.0f, base, inv, p[S][V];
+#pragma unroll
+        for (int j = 0; j < kBalanceMostK; ++j)
+            if (j < a.k) chosen[j] = logit_of<DT>(a, t, x.e[j]);
+        token_softmax<DT, V, S>(a, x, lane_in, p, base, inv);
         bool live = false;
-        float chosen[kBalanceMostK], total = 0.0f;
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j) {
             if (j >= a.k) break;
-            const int e = a.idx[(size_t)t * a.k + j];
-            const bool used = e >= 0 && e < a.E;
-            const float v = of_expert<V, S>(p, used ? e : 0, lane_in, L);
-            chosen[j] = used ? v : 0.0f;
+            const bool used = x.e[j] >= 0 && x.e[j] < a.E;
+            chosen[j] = used ? expf(chosen[j] - base) * inv : 0.0f;
             total += chosen[j];
             live |= used;
-            if (here && used && lane_in == 0) atomicAdd(&cnt[e], 1);
+            if (here && used && lane_in == 0) atomicAdd(&cnt[x.e[j]], 1);
         }
         if (here && live && lane_in == 0) atomicAdd(&cnt[a.E], 1);
-        const float div = a.renorm && a.k > 1 ? (total != 0.0f ? total : 1.0f) : 1.0f;
+        const float div = a.renorm && a.k > 1 && total != 0.0f ? total : 1.0f;
 #pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j) {
-            if (j >= a.k) break;
-            if (here && lane_in == 0) a.scale[(size_t)t * a.k + j] = chosen[j] / div;
-        }
+        for (int j = 0; j < kBalanceMostK; ++j)
+            if (j < a.k && here && lane_in == 0) a.scale[(size_t)t * a.k + j] = chosen[j] / div;
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[s][i] += here && live ? p[s][i] : 0.0f;
-    }
+    });
     // the lanes of a wavefront that hold the same experts, then the wavefronts
 #pragma unroll
     for (int s = 0; s < S; ++s)
@@ -173,77 +202,91 @@ __global__ __launch_bounds__(kBalanceThreads) void balance_forward_kernel(Balanc
             float v = acc[s][i];
             for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o);
             const int c = V * (lane_in + L * s) + i;
-            if (lane < L && c < a.E) sums[wave][c] = v;
+            if (lane < L && c < a.E) sums[wave * a.E + c] = v;
         }
     __syncthreads();
-    for (int c = tid; c <= a.E; c += kBalanceThreads) {
-        if (c < a.E) {
-            float v = 0.0f;
-            for (int w = 0; w < kBalanceThreads / 64; ++w) v += sums[w][c];
-            a.part[(size_t)blockIdx.x * a.E + c] = v;
-        }
-        a.part_count[(size_t)blockIdx.x * (a.E + 1) + c] = cnt[c];
+    const int pitch = (a.E + 3) & ~3;
+    for (int c = tid; c < pitch; c += blockDim.x) {
+        float v = 0.0f;
+        if (c < a.E)
+            for (int w = 0; w < waves; ++w) v += sums[w * a.E + c];
+        a.part[(size_t)blockIdx.x * pitch + c] = v;
+        a.part_count[(size_t)blockIdx.x * pitch + c] = c < a.E ? cnt[c] : 0;
     }
+    if (tid == 0) a.part_live[blockIdx.x] = cnt[a.E];
 }
 
-// The blocks' sums of an expert, in their order, and what follows from them; one block.
+// The blocks' sums of every expert, in a fixed order, and what follows from them; one block.  Four experts per thread, and as many strands of blocks
+// beside each other as threads allow.
 __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a, int blocks)
 {
-    __shared__ float fs[1024];
-    __shared__ int32_t is[1024];
-    __shared__ float pc[kBalanceMostExperts];
-    __shared__ int32_t cc[kBalanceMostExperts + 1];
-    const int tid = threadIdx.x;
-    // one expert per thread, in as many strands of blocks as threads allow
+    __shared__ float4 fs[1024];
+    __shared__ int4 is[1024];
+    __shared__ int32_t assigned[16], tokens[16];
+    __shared__ float losses[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pitch = (a.E + 3) & ~3, quads = pitch / 4;
     int cols = 1;
-    while (cols < a.E + 1 && cols < 1024) cols <<= 1;
-    const int strands = 1024 / cols, strand = tid / cols;
-    for (int c0 = 0; c0 <= a.E; c0 += cols) {
-        const int c = c0 + tid % cols;
-        float v = 0.0f;
-        int32_t n = 0;
-        if (c <= a.E)
-            for (int b = strand; b < blocks; b += strands) {
-                if (c < a.E) v += a.part[(size_t)b * a.E + c];
-                n += a.part_count[(size_t)b * (a.E + 1) + c];
-            }
-        fs[tid] = v, is[tid] = n;
-        __syncthreads();
-        if (strand == 0 && c <= a.E) {
-            for (int s = 1; s < strands; ++s) v += fs[s * cols + tid], n += is[s * cols + tid];
-            if (c < a.E) pc[c] = v;
-            cc[c] = n;
+    while (cols < quads) cols <<= 1;                            // (at most 256)
+    const int strands = 1024 / cols, strand = tid / cols, q = tid % cols;
+    float4 v = make_float4(0, 0, 0, 0);
+    int4 n = make_int4(0, 0, 0, 0);
+    if (q < quads) {
+#pragma unroll 4
+        for (int b = strand; b < blocks; b += strands) {
+            const float4 f = reinterpret_cast<const float4 *>(a.part + (size_t)b * pitch)[q];
+            const int4 i = reinterpret_cast<const int4 *>(a.part_count + (size_t)b * pitch)[q];
+            v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+            n.x += i.x, n.y += i.y, n.z += i.z, n.w += i.w;
         }
-        __syncthreads();
     }
-    int32_t total = 0;
-    for (int c = tid; c < a.E; c += 1024) total += cc[c];
-    is[tid] = total;
+    int live = tid < blocks ? a.part_live[tid] : 0;             // (at most 256 blocks)
+    for (int o = 1; o < 64; o <<= 1) live += __shfl_xor(live, o);
+    fs[tid] = v, is[tid] = n;
+    if (lane == 0) tokens[wave] = live;
+    for (int half = strands / 2; half; half >>= 1) {
+        __syncthreads();
+        if (strand < half) {
+            const float4 f = fs[tid + half * cols];
+            const int4 i = is[tid + half * cols];
+            v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+            n.x += i.x, n.y += i.y, n.z += i.z, n.w += i.w;
+            fs[tid] = v, is[tid] = n;
+        }
+    }
     __syncthreads();
-    for (int o = 512; o; o >>= 1) {
-        if (tid < o) is[tid] += is[tid + o];
-        __syncthreads();
-    }
-    const float A = (float)max(is[0], 1), N = (float)max(cc[a.E], 1);
+    const bool mine = strand == 0 && q < quads;
+    int total = mine ? n.x + n.y + n.z + n.w : 0;
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+    if (lane == 0) assigned[wave] = total;
+    __syncthreads();
+    int A = 0, N = 0;
+    for (int w = 0; w < 16; ++w) A += assigned[w], N += tokens[w];
+    const float fa = (float)max(A, 1), fn = (float)max(N, 1);
     float loss = 0.0f;
-    for (int c = tid; c < a.E; c += 1024) {
-        const float w = a.coef * (float)a.E * ((float)cc[c] / A);
-        loss += w * (pc[c] / N);
-        a.counts[c] = cc[c], a.prob_mean[c] = pc[c] / N, a.weight[c] = w / N;
+    if (mine) {
+        const float ps[4] = {v.x, v.y, v.z, v.w};
+        const int ns[4] = {n.x, n.y, n.z, n.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = 4 * q + i;
+            if (c >= a.E) break;
+            const float w = a.coef * (float)a.E * ((float)ns[i] / fa), mean = ps[i] / fn;
+            loss += w * mean;
+            a.counts[c] = ns[i], a.prob_mean[c] = mean, a.weight[c] = w / fn;
+        }
     }
-    fs[tid] = loss;
+    for (int o = 1; o < 64; o <<= 1) loss += __shfl_xor(loss, o);
+    if (lane == 0) losses[wave] = loss;
     __syncthreads();
-    for (int o = 512; o; o >>= 1) {
-        if (tid < o) fs[tid] += fs[tid + o];
-        __syncthreads();
-    }
-    if (tid == 0) *a.loss = fs[0];
+    if (tid) return;
+    for (int w = 1; w < 16; ++w) loss += losses[w];
+    *a.loss = loss;
 }
 
 template <int DT, int V, int S>
-__global__ __launch_bounds__(kBalanceThreads) void balance_backward_kernel(BalanceArgs a)
+__global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
 {
-    const int tid = threadIdx.x, lane = tid & 63, L = a.L, lane_in = lane & (L - 1);
+    const int lane_in = threadIdx.x & (a.L - 1), L = a.L;
     const float dloss = a.dloss ? *a.dloss : 0.0f;
     float w[S][V];
 #pragma unroll
@@ -253,35 +296,33 @@ __global__ __launch_bounds__(kBalanceThreads) void balance_backward_kernel(Balan
             const int c = V * (lane_in + L * s) + i;
             w[s][i] = c < a.E ? dloss * a.weight[c] : 0.0f;
         }
-    const int per = kBalanceThreads / L;
-    for (long t0 = (long)blockIdx.x * per; t0 < a.T; t0 += (long)gridDim.x * per) {
-        const bool here = t0 + tid / L < a.T;
-        const int t = here ? (int)(t0 + tid / L) : a.T - 1;
-        float p[S][V];
-        token_softmax<DT, V, S>(a, t, lane_in, p);
-        int e[kBalanceMostK];
-        float s[kBalanceMostK], ds[kBalanceMostK], total = 0.0f;
+    const bool renorm = a.renorm && a.k > 1;
+    for_tokens<DT, V, S>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S> &x) {
+        float sc[kBalanceMostK], ds[kBalanceMostK], total = 0.0f, base, inv, p[S][V];
+#pragma unroll
+        for (int j = 0; j < kBalanceMostK; ++j) {
+            if (j >= a.k) break;
+            sc[j] = logit_of<DT>(a, t, x.e[j]);
+            ds[j] = a.dscale ? a.dscale[(size_t)t * a.k + j] : 0.0f;
+        }
+        token_softmax<DT, V, S>(a, x, lane_in, p, base, inv);
         bool live = false;
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j) {
             if (j >= a.k) break;
-            e[j] = a.idx[(size_t)t * a.k + j];
-            const bool used = e[j] >= 0 && e[j] < a.E;
-            if (!used) e[j] = -1;
-            const float v = of_expert<V, S>(p, used ? e[j] : 0, lane_in, L);
-            s[j] = used ? v : 0.0f;
-            ds[j] = used && a.dscale ? a.dscale[(size_t)t * a.k + j] : 0.0f;
-            total += s[j];
+            const bool used = x.e[j] >= 0 && x.e[j] < a.E;
+            sc[j] = used ? expf(sc[j] - base) * inv : 0.0f;
+            if (!used) ds[j] = 0.0f;
+            total += sc[j];
             live |= used;
         }
-        const bool renorm = a.renorm && a.k > 1;
         const float div = renorm && total != 0.0f ? total : 1.0f;
         float mean = 0.0f;                                    // sum_j s_j ds_j
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j) {
             if (j >= a.k) break;
-            s[j] /= div;
-            mean += s[j] * ds[j];
+            sc[j] /= div;
+            mean += sc[j] * ds[j];
         }
         // Renormalised scales are a softmax over the chosen experts: s_j (ds_j - sum_i s_i ds_i), which, as the s_i add up to one, is
         // s_j sum_i s_i (ds_j - ds_i): nothing is lost where the ds are nearly the same.
@@ -293,19 +334,17 @@ __global__ __launch_bounds__(kBalanceThreads) void balance_backward_kernel(Balan
             if (renorm) {
                 d = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kBalanceMostK; ++i) {
-                    if (i >= a.k) break;
-                    d += s[i] * (ds[j] - ds[i]);
-                }
+                for (int i = 0; i < kBalanceMostK; ++i)
+                    if (i < a.k) d += sc[i] * (ds[j] - ds[i]);
             }
-            gate[j] = s[j] * d;
+            gate[j] = sc[j] * d;
         }
         float pw = 0.0f;
 #pragma unroll
         for (int q = 0; q < S; ++q)
 #pragma unroll
             for (int i = 0; i < V; ++i) pw += p[q][i] * w[q][i];
-        pw = lanes_sum(pw, L);
+        pw = over_lanes(pw, L, [](float u, float v) { return u + v; });
         const float off = renorm ? pw : pw + mean;            // what every expert's gradient loses, times its p
 #pragma unroll
         for (int q = 0; q < S; ++q) {
@@ -317,16 +356,17 @@ __global__ __launch_bounds__(kBalanceThreads) void balance_backward_kernel(Balan
 #pragma unroll
                 for (int j = 0; j < kBalanceMostK; ++j) {
                     if (j >= a.k) break;
-                    if (e[j] == c + i) g[i] += gate[j];
+                    if (x.e[j] == c + i) g[i] += gate[j];
                 }
                 if (!live) g[i] = 0.0f;
             }
             if (here && c < a.E) store_logits<DT, V>(a, t, c, g);
         }
-    }
+    });
 }
 
-// Lanes of a token and steps, by E: four neighbouring logits a lane where rows allow it.
+// Lanes of a token and steps, by E: four neighbouring logits a lane where rows allow it; sixteen lanes, which exchange without LDS, as long as a lane then holds
+// no more than four steps.
 struct BalanceShape { int V, S, L; };
 static BalanceShape balance_shape(int E)
 {
@@ -334,15 +374,18 @@ static BalanceShape balance_shape(int E)
     b.V = E % 4 == 0 ? 4 : 1;
     const int cols = E / b.V;
     b.L = 1;
-    while (b.L < cols && b.L < 64) b.L <<= 1;
+    while (b.L < cols && (b.L < 16 || (b.L < 64 && b.L * 4 < cols))) b.L <<= 1;
     b.S = 1;
     while (b.S * b.L < cols) b.S <<= 1;
     return b;
 }
 
-static int balance_blocks(int T, int L)
+// Threads of a forward block: its wavefronts' sums take 64 KB of LDS at most together with the counts.
+static int balance_threads(int E) { return E <= 512 ? 1024 : 512; }
+
+static int balance_blocks(int T, int E)
 {
-    const long per = kBalanceThreads / L, want = ((long)T + per - 1) / per;
+    const long per = balance_threads(E) / balance_shape(E).L, want = ((long)T + per - 1) / per;
     return (int)(want < kBalanceMostBlocks ? want : kBalanceMostBlocks);
 }
 
@@ -386,8 +429,8 @@ extern "C" size_t moe_balance_loss_workspace_bytes(int T, int E)
 {
     using namespace moe;
     if (T < 0 || E < 1 || E > kBalanceMostExperts) return 0;
-    const size_t blocks = balance_blocks(T, balance_shape(E).L);
-    return round_up(blocks * E * 4, 16) + blocks * (E + 1) * 4 + 16;
+    const size_t blocks = balance_blocks(T, E), pitch = round_up(E, 4);
+    return blocks * (2 * pitch * 4 + 4) + 16;
 }
 
 extern "C" int moe_balance_loss(const void *logits, int dtype, const int32_t *expert_idx, int T, int E, int k, int renormalize, float coef, float *loss,
@@ -401,15 +444,17 @@ extern "C" int moe_balance_loss(const void *logits, int dtype, const int32_t *ex
     if (!workspace || workspace_bytes < need) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned16(workspace)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     const BalanceShape b = balance_shape(E);
-    const int blocks = balance_blocks(T, b.L);
+    const int blocks = balance_blocks(T, E), threads = balance_threads(E);
     hipStream_t s = as_stream(stream);
     BalanceArgs a{};
     a.logits = logits, a.idx = expert_idx, a.T = T, a.E = E, a.k = k, a.renorm = renormalize, a.L = b.L, a.coef = coef, a.scale = expert_scale;
-    a.part = (float *)workspace, a.part_count = (int32_t *)((uint8_t *)workspace + round_up((size_t)blocks * E * 4, 16));
+    const size_t all = (size_t)blocks * round_up(E, 4);
+    a.part = (float *)workspace, a.part_count = (int32_t *)workspace + all, a.part_live = (int32_t *)workspace + 2 * all;
     a.loss = loss, a.counts = counts, a.prob_mean = prob_mean, a.weight = weight;
     if (blocks)
         with_shape(dtype, b, [&](auto dt, auto v, auto st) {
-            hipLaunchKernelGGL((balance_forward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value>), dim3(blocks), dim3(kBalanceThreads), 0, s, a);
+            hipLaunchKernelGGL((balance_forward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value>), dim3(blocks), dim3(threads),
+                               threads / 64 * E * 4, s, a);
         });
     if (int rc = check_launch(what)) return rc;
     hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(1024), 0, s, a, blocks);
@@ -426,13 +471,13 @@ extern "C" int moe_balance_loss_backward(const void *logits, int dtype, const in
     if (!weight || !dlogits) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(dlogits)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     const BalanceShape b = balance_shape(E);
-    const long want = ((long)T * b.L + kBalanceThreads - 1) / kBalanceThreads;
+    const long want = ((long)T * b.L + 511) / 512;
     BalanceArgs a{};
     a.logits = logits, a.idx = expert_idx, a.T = T, a.E = E, a.k = k, a.renorm = renormalize, a.L = b.L;
     a.weight = const_cast<float *>(weight), a.dloss = dloss, a.dscale = dscale, a.dlogits = dlogits;
     with_shape(dtype, b, [&](auto dt, auto v, auto st) {
         hipLaunchKernelGGL((balance_backward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value>), dim3((unsigned)(want < 2048 ? want : 2048)),
-                           dim3(kBalanceThreads), 0, as_stream(stream), a);
+                           dim3(512), 0, as_stream(stream), a);
     });
     return check_launch(what);
 }
