@@ -7,7 +7,7 @@
 // Both directions are bound by reading the logits (and the backward by writing their gradient), small batches by their launches.  A token's logits are
 // spread over L lanes of a wavefront, V neighbouring ones per lane and step, so that a lane keeps the sums of its own experts in registers over all
 // of its tokens; a block's sums meet in LDS and the blocks' in a second launch, in the order of the blocks: no floating-point atomics, the same bits
-// every time.  (A launch of one block does both.)
+// every time.  (A launch of one block does without.)
 #include <math.h>
 
 #include <type_traits>
@@ -42,8 +42,9 @@ __device__ inline float to_f32(uint32_t bits)
     return __uint_as_float(bits << 16);
 }
 
+// FULL: the lanes and steps of a token hold its E logits and nothing besides, as they do for powers of two from eight on.
 // What a lane holds of a token: V neighbouring logits in each of S steps, as they lie in memory, and the token's experts.  Requested one token ahead.
-template <int DT, int V, int S>
+template <int DT, int V, int S, bool FULL>
 struct TokenLoad {
     static constexpr int W = V == 1 ? 1 : DT == MOE_F32 ? 4 : 2;      // words of a step
     uint32_t raw[S][W];
@@ -57,7 +58,7 @@ struct TokenLoad {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const int c = V * (lane_in + a.L * s);
-            const size_t at = (size_t)t * a.E + min(c, a.E - V);      // (past the end: what the last lane holds, which value() leaves out)
+            const size_t at = (size_t)t * a.E + (FULL ? c : min(c, a.E - V));      // (past the end: what the last lane holds, which value() leaves out)
             if constexpr (V == 1) raw[s][0] = DT == MOE_F32 ? reinterpret_cast<const uint32_t *>(a.logits)[at] : reinterpret_cast<const uint16_t *>(a.logits)[at];
             else if constexpr (DT == MOE_F32) {
                 const uint4 q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const float *>(a.logits) + at);
@@ -70,7 +71,7 @@ struct TokenLoad {
     }
     __device__ inline float value(const BalanceArgs &a, int s, int i, int lane_in) const
     {
-        if (V * (lane_in + a.L * s) >= a.E) return -INFINITY;
+        if (!FULL && V * (lane_in + a.L * s) >= a.E) return -INFINITY;
         if (V == 1 || DT == MOE_F32) return to_f32<DT>(raw[s][i]);
         return to_f32<DT>(i & 1 ? raw[s][i >> 1] >> 16 : raw[s][i >> 1] & 0xffffu);
     }
@@ -90,6 +91,10 @@ __device__ inline void store_logits(const BalanceArgs &a, int t, int c, const fl
     else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(a.dlogits) + at) = make_uint2(b[0] | (uint32_t)b[1] << 16, b[2] | (uint32_t)b[3] << 16);
 }
 
+// e^x, x <= 0, in the exponential instruction: off by a unit of its own and by 2^-24 of the argument, 1.2e-6 where e^x = 2e-9.  (expf: both directions of
+// 131072 tokens by 256 experts 141 us, a good part of it vector instructions.)
+__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
 // op over the L lanes of a token, in the vector unit's own lane permutations up to sixteen of them.
 template <class Op>
 __device__ inline float over_lanes(float v, int L, Op op)
@@ -105,10 +110,10 @@ __device__ inline float over_lanes(float v, int L, Op op)
     return v;
 }
 
-// Softmax of a token over its L lanes: p[s][i] of column V (lane_in + L s) + i, and what makes a probability of any other logit of it: exp(z - base) inv.
-// A token whose logits are all -infinity has nothing to choose: p = 0.  (A NaN or +infinity among them makes its p NaN.)
-template <int DT, int V, int S>
-__device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V, S> &x, int lane_in, float (&p)[S][V], float &base, float &inv)
+// Softmax of a token over its L lanes: p[s][i] inv is that of column V (lane_in + L s) + i, and exp_of(z - base) inv that of any logit z of it.
+// A token whose logits are all -infinity has nothing to choose: inv = 0.  (A NaN or +infinity among them makes its p NaN.)
+template <int DT, int V, int S, bool FULL>
+__device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V, S, FULL> &x, int lane_in, float (&p)[S][V], float &base, float &inv)
 {
     float m = -INFINITY;
 #pragma unroll
@@ -122,15 +127,11 @@ __device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V
     for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            p[s][i] = expf(p[s][i] - base);
+            p[s][i] = exp_of(p[s][i] - base);
             sum += p[s][i];
         }
     sum = over_lanes(sum, a.L, [](float u, float v) { return u + v; });
     inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int i = 0; i < V; ++i) p[s][i] *= inv;
 }
 
 // Logit of expert e (the first one for a slot without an expert).
@@ -142,7 +143,7 @@ __device__ inline float logit_of(const BalanceArgs &a, int t, int e)
 }
 
 // The tokens of a thread's L lanes, one after the other, the next one's loads ahead of the work on this one: f(token, whether it is there, loads).
-template <int DT, int V, int S, class F>
+template <int DT, int V, int S, bool FULL, class F>
 __device__ inline void for_tokens(const BalanceArgs &a, int lane_in, F f)
 {
     const int per = blockDim.x / a.L, mine = threadIdx.x / a.L;
@@ -150,7 +151,8 @@ __device__ inline void for_tokens(const BalanceArgs &a, int lane_in, F f)
     auto at = [&](long t) { return (int)(t < a.T ? t : a.T - 1); };
     long t = (long)blockIdx.x * per + mine;
     const long end = (long)blockIdx.x * per;                       // (the block's first token: its loop ends for all of its threads at once)
-    TokenLoad<DT, V, S> now, next;
+    if (a.T == 0) return;
+    TokenLoad<DT, V, S, FULL> now, next;
     now.request(a, at(t), lane_in);
     for (long first = end; first < a.T; first += step, t += step) {
         next.request(a, at(t + step), lane_in);
@@ -159,7 +161,39 @@ __device__ inline void for_tokens(const BalanceArgs &a, int lane_in, F f)
     }
 }
 
-template <int DT, int V, int S>
+// What follows from the sums of all tokens: thread q < quads of one block has those of experts 4 q .. 4 q + 3, N the number of tokens with an assignment.
+__device__ inline void balance_end(const BalanceArgs &a, const float (&ps)[4], const int (&ns)[4], int q, bool mine, int N)
+{
+    __shared__ int32_t assigned[16];
+    __shared__ float losses[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x / 64;
+    int total = mine ? ns[0] + ns[1] + ns[2] + ns[3] : 0;
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+    if (lane == 0) assigned[wave] = total;
+    __syncthreads();
+    int A = 0;
+    for (int w = 0; w < waves; ++w) A += assigned[w];
+    const float fa = (float)max(A, 1), fn = (float)max(N, 1);
+    float loss = 0.0f;
+    if (mine) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = 4 * q + i;
+            if (c >= a.E) break;
+            const float w = a.coef * (float)a.E * ((float)ns[i] / fa), mean = ps[i] / fn;
+            loss += w * mean;
+            a.counts[c] = ns[i], a.prob_mean[c] = mean, a.weight[c] = w / fn;
+        }
+    }
+    for (int o = 1; o < 64; o <<= 1) loss += __shfl_xor(loss, o);
+    if (lane == 0) losses[wave] = loss;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < waves; ++w) loss += losses[w];
+    *a.loss = loss;
+}
+
+template <int DT, int V, int S, bool FULL>
 __global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
 {
     extern __shared__ float sums[];                             // [wavefronts][E]
@@ -168,18 +202,18 @@ __global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
     for (int i = tid; i <= a.E; i += blockDim.x) cnt[i] = 0;
     __syncthreads();
     float acc[S][V] = {};
-    for_tokens<DT, V, S>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S> &x) {
+    for_tokens<DT, V, S, FULL>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL> &x) {
         float chosen[kBalanceMostK], total = 0.0f, base, inv, p[S][V];
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j)
             if (j < a.k) chosen[j] = logit_of<DT>(a, t, x.e[j]);
-        token_softmax<DT, V, S>(a, x, lane_in, p, base, inv);
+        token_softmax<DT, V, S, FULL>(a, x, lane_in, p, base, inv);
         bool live = false;
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j) {
             if (j >= a.k) break;
             const bool used = x.e[j] >= 0 && x.e[j] < a.E;
-            chosen[j] = used ? expf(chosen[j] - base) * inv : 0.0f;
+            chosen[j] = used ? exp_of(chosen[j] - base) * inv : 0.0f;
             total += chosen[j];
             live |= used;
             if (here && used && lane_in == 0) atomicAdd(&cnt[x.e[j]], 1);
@@ -189,10 +223,17 @@ __global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j)
             if (j < a.k && here && lane_in == 0) a.scale[(size_t)t * a.k + j] = chosen[j] / div;
+        if (__all(here && live)) {
 #pragma unroll
-        for (int s = 0; s < S; ++s)
+            for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[s][i] += here && live ? p[s][i] : 0.0f;
+                for (int i = 0; i < V; ++i) acc[s][i] = fmaf(p[s][i], inv, acc[s][i]);
+        } else {                                                // (not by a factor of 0: a pruned token's p may be NaN)
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[s][i] += here && live ? p[s][i] * inv : 0.0f;
+        }
     });
     // the lanes of a wavefront that hold the same experts, then the wavefronts
 #pragma unroll
@@ -206,6 +247,21 @@ __global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
         }
     __syncthreads();
     const int pitch = (a.E + 3) & ~3;
+    if (gridDim.x == 1) {
+        float ps[4] = {};
+        int ns[4] = {};
+        const bool mine = 4 * tid < a.E;                        // (at most 256 threads of 512 or more)
+        if (mine)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = 4 * tid + i;
+                if (c >= a.E) break;
+                for (int w = 0; w < waves; ++w) ps[i] += sums[w * a.E + c];
+                ns[i] = cnt[c];
+            }
+        balance_end(a, ps, ns, tid, mine, cnt[a.E]);
+        return;
+    }
     for (int c = tid; c < pitch; c += blockDim.x) {
         float v = 0.0f;
         if (c < a.E)
@@ -222,8 +278,7 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a, int
 {
     __shared__ float4 fs[1024];
     __shared__ int4 is[1024];
-    __shared__ int32_t assigned[16], tokens[16];
-    __shared__ float losses[16];
+    __shared__ int32_t tokens[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pitch = (a.E + 3) & ~3, quads = pitch / 4;
     int cols = 1;
     while (cols < quads) cols <<= 1;                            // (at most 256)
@@ -254,36 +309,14 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a, int
         }
     }
     __syncthreads();
-    const bool mine = strand == 0 && q < quads;
-    int total = mine ? n.x + n.y + n.z + n.w : 0;
-    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
-    if (lane == 0) assigned[wave] = total;
-    __syncthreads();
-    int A = 0, N = 0;
-    for (int w = 0; w < 16; ++w) A += assigned[w], N += tokens[w];
-    const float fa = (float)max(A, 1), fn = (float)max(N, 1);
-    float loss = 0.0f;
-    if (mine) {
-        const float ps[4] = {v.x, v.y, v.z, v.w};
-        const int ns[4] = {n.x, n.y, n.z, n.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = 4 * q + i;
-            if (c >= a.E) break;
-            const float w = a.coef * (float)a.E * ((float)ns[i] / fa), mean = ps[i] / fn;
-            loss += w * mean;
-            a.counts[c] = ns[i], a.prob_mean[c] = mean, a.weight[c] = w / fn;
-        }
-    }
-    for (int o = 1; o < 64; o <<= 1) loss += __shfl_xor(loss, o);
-    if (lane == 0) losses[wave] = loss;
-    __syncthreads();
-    if (tid) return;
-    for (int w = 1; w < 16; ++w) loss += losses[w];
-    *a.loss = loss;
+    int N = 0;
+    for (int w = 0; w < 16; ++w) N += tokens[w];
+    const float ps[4] = {v.x, v.y, v.z, v.w};
+    const int ns[4] = {n.x, n.y, n.z, n.w};
+    balance_end(a, ps, ns, q, strand == 0 && q < quads, N);
 }
 
-template <int DT, int V, int S>
+template <int DT, int V, int S, bool FULL>
 __global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
 {
     const int lane_in = threadIdx.x & (a.L - 1), L = a.L;
@@ -297,7 +330,7 @@ __global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
             w[s][i] = c < a.E ? dloss * a.weight[c] : 0.0f;
         }
     const bool renorm = a.renorm && a.k > 1;
-    for_tokens<DT, V, S>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S> &x) {
+    for_tokens<DT, V, S, FULL>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL> &x) {
         float sc[kBalanceMostK], ds[kBalanceMostK], total = 0.0f, base, inv, p[S][V];
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j) {
@@ -305,13 +338,13 @@ __global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
             sc[j] = logit_of<DT>(a, t, x.e[j]);
             ds[j] = a.dscale ? a.dscale[(size_t)t * a.k + j] : 0.0f;
         }
-        token_softmax<DT, V, S>(a, x, lane_in, p, base, inv);
+        token_softmax<DT, V, S, FULL>(a, x, lane_in, p, base, inv);
         bool live = false;
 #pragma unroll
         for (int j = 0; j < kBalanceMostK; ++j) {
             if (j >= a.k) break;
             const bool used = x.e[j] >= 0 && x.e[j] < a.E;
-            sc[j] = used ? expf(sc[j] - base) * inv : 0.0f;
+            sc[j] = used ? exp_of(sc[j] - base) * inv : 0.0f;
             if (!used) ds[j] = 0.0f;
             total += sc[j];
             live |= used;
@@ -344,7 +377,7 @@ __global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
         for (int q = 0; q < S; ++q)
 #pragma unroll
             for (int i = 0; i < V; ++i) pw += p[q][i] * w[q][i];
-        pw = over_lanes(pw, L, [](float u, float v) { return u + v; });
+        pw = inv * over_lanes(pw, L, [](float u, float v) { return u + v; });
         const float off = renorm ? pw : pw + mean;            // what every expert's gradient loses, times its p
 #pragma unroll
         for (int q = 0; q < S; ++q) {
@@ -352,7 +385,7 @@ __global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
             float g[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                g[i] = p[q][i] * (w[q][i] - off);
+                g[i] = p[q][i] * inv * (w[q][i] - off);
 #pragma unroll
                 for (int j = 0; j < kBalanceMostK; ++j) {
                     if (j >= a.k) break;
@@ -383,23 +416,28 @@ static BalanceShape balance_shape(int E)
 // Threads of a forward block: its wavefronts' sums take 64 KB of LDS at most together with the counts.
 static int balance_threads(int E) { return E <= 512 ? 1024 : 512; }
 
+// Blocks of the forward launch.  Up to four rounds of tokens stay in one block, which then needs no second launch to join the blocks' sums (4 us).
 static int balance_blocks(int T, int E)
 {
-    const long per = balance_threads(E) / balance_shape(E).L, want = ((long)T + per - 1) / per;
+    const long per = balance_threads(E) / balance_shape(E).L, want = T <= 4 * per ? 1 : ((long)T + per - 1) / per;
     return (int)(want < kBalanceMostBlocks ? want : kBalanceMostBlocks);
 }
 
-// Calls f(element type, V, S) as compile-time numbers.
+// Calls f(element type, V, S, FULL) as compile-time numbers.
 template <class F>
-static void with_shape(int dtype, const BalanceShape &b, F f)
+static void with_shape(int dtype, int E, const BalanceShape &b, F f)
 {
     auto steps = [&](auto dt) {
-        auto go = [&](auto v, auto s) { f(dt, v, s); };
+        auto go = [&](auto v, auto s) { f(dt, v, s, std::false_type{}); };
         using std::integral_constant;
         if (b.V == 4) {
-            if (b.S == 1) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-            else if (b.S == 2) go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-            else go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+            auto four = [&](auto full) {
+                if (b.S == 1) f(dt, integral_constant<int, 4>{}, integral_constant<int, 1>{}, full);
+                else if (b.S == 2) f(dt, integral_constant<int, 4>{}, integral_constant<int, 2>{}, full);
+                else f(dt, integral_constant<int, 4>{}, integral_constant<int, 4>{}, full);
+            };
+            if (E == 4 * b.L * b.S) four(std::true_type{});
+            else four(std::false_type{});
         } else {
             if (b.S == 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
             else if (b.S == 2) go(integral_constant<int, 1>{}, integral_constant<int, 2>{});
@@ -451,11 +489,11 @@ extern "C" int moe_balance_loss(const void *logits, int dtype, const int32_t *ex
     const size_t all = (size_t)blocks * round_up(E, 4);
     a.part = (float *)workspace, a.part_count = (int32_t *)workspace + all, a.part_live = (int32_t *)workspace + 2 * all;
     a.loss = loss, a.counts = counts, a.prob_mean = prob_mean, a.weight = weight;
-    if (blocks)
-        with_shape(dtype, b, [&](auto dt, auto v, auto st) {
-            hipLaunchKernelGGL((balance_forward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value>), dim3(blocks), dim3(threads),
+    with_shape(dtype, E, b, [&](auto dt, auto v, auto st, auto full) {
+        hipLaunchKernelGGL((balance_forward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value, decltype(full)::value>), dim3(blocks), dim3(threads),
                                threads / 64 * E * 4, s, a);
-        });
+    });
+    if (blocks == 1) return check_launch(what);
     if (int rc = check_launch(what)) return rc;
     hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(1024), 0, s, a, blocks);
     return check_launch(what);
@@ -475,8 +513,8 @@ extern "C" int moe_balance_loss_backward(const void *logits, int dtype, const in
     BalanceArgs a{};
     a.logits = logits, a.idx = expert_idx, a.T = T, a.E = E, a.k = k, a.renorm = renormalize, a.L = b.L;
     a.weight = const_cast<float *>(weight), a.dloss = dloss, a.dscale = dscale, a.dlogits = dlogits;
-    with_shape(dtype, b, [&](auto dt, auto v, auto st) {
-        hipLaunchKernelGGL((balance_backward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value>), dim3((unsigned)(want < 2048 ? want : 2048)),
+    with_shape(dtype, E, b, [&](auto dt, auto v, auto st, auto full) {
+        hipLaunchKernelGGL((balance_backward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value, decltype(full)::value>), dim3((unsigned)(want < 2048 ? want : 2048)),
                            dim3(512), 0, as_stream(stream), a);
     });
     return check_launch(what);

@@ -1,86 +1,157 @@
-// Grouped product of 4-bit rows and 4-bit experts for few rows per expert.
+// Grouped product of 4-bit rows and 4-bit experts for few rows per expert: a launch that streams weights.
+#include <type_traits>
+
 #include "moe_mx4_epilogue.h"
 
 namespace moe {
 
-// Block: four wavefronts, one item of up to 32 rows of an expert by 32 channels; the wavefronts take every fourth 256 values of K and their sums meet
-// in LDS, added in the order of the wavefronts.  Codes go from memory to registers as the matrix instruction wants them: of 256 values lane (r, h)
-// takes the 64 bytes that are blocks 4 h .. 4 h + 3 of its channel (or row), so the two lanes of a channel read a whole line, and step j multiplies
-// block 4 h + j of both operands: any pairing of blocks with steps will do as long as it is the same on both sides, and with this one
-// the scales of a lane's four steps are one dword.
-constexpr int kStreamWaves = 4;
+// Block: WAVES wavefronts, one item of up to 32 rows of an expert by NS slabs of 32 channels; the wavefronts split K, 256 values (a line of a channel's
+// codes) at a time, CPW of them each per pass, and their sums meet in LDS, added in the order of the wavefronts.  Weights go from memory into the
+// wavefront's own part of LDS, eight channels' whole lines per load: requested first, before the block knows its rows, so that the chain of index and rows
+// runs under them.  (Weights straight into registers, a channel's sixteen bytes per lane, touch 64 places per load: 29 us instead of 16.7 for 70 MB.)
+// Rows' codes, of which there are few and which come from L2, and scales go into registers.
+//
+// Of 256 values lane (r, h) takes blocks 4 h .. 4 h + 3 of its channel (or row), and step j multiplies block 4 h + j of both operands: any pairing of
+// blocks with steps will do as long as it is the same on both sides, and with this one the scales of a lane's four steps are one dword.
+template <int WAVES, int NS, int CPW>
+struct MxStream {
+    static constexpr int kWave = NS * CPW * 4096;
+    static constexpr int kLds = WAVES * kWave;          // (the partial sums, 4 KB per wavefront and slab, fit as well)
+};
 
-template <int OUT>
-__global__ __launch_bounds__(256) void mx4_stream_kernel(MxArgs p)
+template <int WAVES, int NS, int CPW, int OUT>
+__global__ __launch_bounds__(64 * WAVES) void mx4_stream_kernel(MxArgs p)
 {
-    __shared__ f32x4_t part[kStreamWaves][4][64];
+    extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 31, h = lane >> 5;
-    const int K = p.K, N = p.N, G = mx_groups(K), blocks = K / kMxBlock;
+    const int K = p.K, N = p.N, G = mx_groups(K), blocks = K / kMxBlock, chunks = (blocks + 7) / 8;
     int e, col, row0, rows;
-    if (!find_item(p.offsets, p.E, p.R, 32, N / 32, blockIdx.x, &e, &col, &row0, &rows)) return;
+    if (!find_item(p.offsets, p.E, p.R, 32, (N + 32 * NS - 1) / (32 * NS), blockIdx.x, &e, &col, &row0, &rows)) return;
     e = __builtin_amdgcn_readfirstlane(e), col = __builtin_amdgcn_readfirstlane(col);
     row0 = __builtin_amdgcn_readfirstlane(row0), rows = __builtin_amdgcn_readfirstlane(rows);
-    const int n = col * 32 + r, out_row = row0 + min(r, rows - 1);             // (lanes past the rows repeat the last one)
+    const int n0 = col * 32 * NS;
+    const uint8_t *w = p.w + (size_t)e * N * (K / 2);
+    const uint32_t *ws = reinterpret_cast<const uint32_t *>(p.ws) + (size_t)e * G * N;
+    uint8_t *mine = lds + wave * MxStream<WAVES, NS, CPW>::kWave;
+
+    // (channels past N: the last slab again, not stored; chunks past K: whatever LDS holds, times rows of zeros)
+    auto slab = [&](int s) { return min(n0 + 32 * s, N - 32); };
+    auto request = [&](int pass) {
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) {
+            const int c = (pass * CPW + i) * WAVES + wave;
+            if (c >= chunks) break;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int row = 8 * t + (lane >> 3), b = min(8 * c + ((lane & 7) ^ ((row >> 1) & 7)), blocks - 1);
+                    load_to_lds16<true>(w + (size_t)(slab(s) + row) * (K / 2) + (size_t)b * 16, reinterpret_cast<uint16_t *>(mine + ((i * NS + s) * 4 + t) * 1024));
+                }
+        }
+    };
+    request(0);
+    const int out_row = row0 + min(r, rows - 1);             // (lanes past the rows repeat the last one)
     const int a_row = p.a_src ? min(max(p.a_src[out_row] / p.a_div, 0), p.a_rows - 1) : out_row;
-    const uint8_t *w = p.w + ((size_t)e * N + n) * (K / 2), *a = p.a + (size_t)a_row * (K / 2);
-    const uint32_t *ws = reinterpret_cast<const uint32_t *>(p.ws) + (size_t)e * G * N + n;
+    const uint8_t *a = p.a + (size_t)a_row * (K / 2);
     const uint32_t *as = reinterpret_cast<const uint32_t *>(p.as) + a_row;
 
-    float16_t acc = {};
-    for (int c = wave; c * 256 < K; c += kStreamWaves) {
-        const int b0 = 8 * c + 4 * h, g = 2 * c + h;                           // this lane's blocks and their group of scales
-        u32x4_t wq[4] = {}, aq[4] = {};
-        uint32_t wsc = 0, asc = 0;
+    float16_t acc[NS] = {};
+    for (int pass = 0; pass * CPW * WAVES < chunks; ++pass) {
+        if (pass) request(pass);
+        u32x4_t aq[CPW][4];
+        uint32_t asc[CPW], wsc[CPW][NS];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (b0 + j < blocks) {
-                wq[j] = *reinterpret_cast<const u32x4_t *>(w + (size_t)(b0 + j) * 16);
-                aq[j] = *reinterpret_cast<const u32x4_t *>(a + (size_t)(b0 + j) * 16);
+        for (int i = 0; i < CPW; ++i) {
+            const int b0 = 8 * ((pass * CPW + i) * WAVES + wave) + 4 * h;          // this lane's blocks, and their group of scales
+            const int g = min(b0 / 4, G - 1);
+            // scales of blocks that are not there may hold anything; the rows' codes are zero there
+            const uint32_t mask = b0 + 4 <= blocks ? 0xffffffffu : b0 < blocks ? (1u << (8 * (blocks - b0))) - 1 : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                aq[i][j] = u32x4_t{};
+                if (b0 + j < blocks) aq[i][j] = *reinterpret_cast<const u32x4_t *>(a + (size_t)(b0 + j) * 16);
             }
-        if (b0 < blocks) wsc = ws[(size_t)g * N], asc = as[(size_t)g * p.a_rows];
-        if (b0 + 4 > blocks) {                                                 // scales of blocks that are not there may hold anything
-            const uint32_t mask = b0 < blocks ? (1u << (8 * (blocks - b0))) - 1 : 0;
-            wsc &= mask, asc &= mask;
-        }
-#define MX_STEP(J)                                                                                                                                     \
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(i32x8_t{(int)wq[J][0], (int)wq[J][1], (int)wq[J][2], (int)wq[J][3], 0, 0, 0, 0},            \
-                                                          i32x8_t{(int)aq[J][0], (int)aq[J][1], (int)aq[J][2], (int)aq[J][3], 0, 0, 0, 0}, acc, 4, 4, \
-                                                          J, (int)wsc, J, (int)asc)
-        MX_STEP(0);
-        MX_STEP(1);
-        MX_STEP(2);
-        MX_STEP(3);
-#undef MX_STEP
-    }
+            asc[i] = as[(size_t)g * p.a_rows] & mask;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) part[wave][q][lane] = f32x4_t{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+            for (int s = 0; s < NS; ++s) wsc[i][s] = ws[(size_t)g * N + slab(s) + r] & mask;
+        }
+        wait_loads<0>();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < CPW; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                u32x4_t wq[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    wq[j] = *reinterpret_cast<const u32x4_t *>(mine + (i * NS + s) * 4096 + r * 128 + (((4 * h + j) ^ ((r >> 1) & 7)) * 16));
+                auto step = [&](auto j_c) {
+                    constexpr int J = decltype(j_c)::value;
+                    acc[s] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                        i32x8_t{(int)wq[J][0], (int)wq[J][1], (int)wq[J][2], (int)wq[J][3], 0, 0, 0, 0},
+                        i32x8_t{(int)aq[i][J][0], (int)aq[i][J][1], (int)aq[i][J][2], (int)aq[i][J][3], 0, 0, 0, 0}, acc[s], 4, 4, J, (int)wsc[i][s], J, (int)asc[i]);
+                };
+                step(std::integral_constant<int, 0>{});
+                step(std::integral_constant<int, 1>{});
+                step(std::integral_constant<int, 2>{});
+                step(std::integral_constant<int, 3>{});
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the next pass's weights take the place of these)
+    }
     __syncthreads();
-    if (wave) return;
+    f32x4_t *part = reinterpret_cast<f32x4_t *>(lds);               // [wavefront][slab][q][lane]
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            part[((wave * NS + s) * 4 + q) * 64 + lane] = f32x4_t{acc[s][4 * q], acc[s][4 * q + 1], acc[s][4 * q + 2], acc[s][4 * q + 3]};
+    __syncthreads();
+    if (wave >= NS || n0 + 32 * wave >= N) return;
+    float16_t sum;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        f32x4_t s = part[0][q][lane];
+        f32x4_t v = part[(wave * 4 + q) * 64 + lane];
 #pragma unroll
-        for (int t = 1; t < kStreamWaves; ++t) s += part[t][q][lane];
+        for (int t = 1; t < WAVES; ++t) v += part[((t * NS + wave) * 4 + q) * 64 + lane];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[4 * q + i] = s[i];
+        for (int i = 0; i < 4; ++i) sum[4 * q + i] = v[i];
     }
-    mx_store_tile<OUT>(p, acc, e, col * 32, row0 + r, r < rows);
+    mx_store_tile<OUT>(p, sum, e, n0 + 32 * wave, row0 + r, r < rows);
 }
 
+template <int WAVES, int NS, int CPW>
+static int launch_stream(const MxArgs &p, hipStream_t s)
+{
+    using S = MxStream<WAVES, NS, CPW>;
+    const long slots = (long)p.R / 32 + (p.E < p.R ? p.E : p.R);
+    const long wgs = (slots * ((p.N + 32 * NS - 1) / (32 * NS)) + kXcds - 1) / kXcds * kXcds;      // upper bound of the work items, whole rounds of XCDs
+    if (wgs * WAVES > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "moe_grouped_gemm_mx4: %ld workgroups exceed one launch", wgs);
+    auto run = [&](auto out) {
+        constexpr int OUT = decltype(out)::value;
+        static std::atomic<uint64_t> raised;
+        if (S::kLds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(&mx4_stream_kernel<WAVES, NS, CPW, OUT>), S::kLds, raised);
+        hipLaunchKernelGGL((mx4_stream_kernel<WAVES, NS, CPW, OUT>), dim3((unsigned)wgs), dim3(64 * WAVES), S::kLds, s, p);
+    };
+    if (p.out_scales) run(std::integral_constant<int, -1>{});
+    else if (p.out_dtype == MOE_F16) run(std::integral_constant<int, MOE_F16>{});
+    else if (p.out_dtype == MOE_BF16) run(std::integral_constant<int, MOE_BF16>{});
+    else run(std::integral_constant<int, MOE_F32>{});
+    return check_launch("moe_grouped_gemm_mx4");
+}
+
+// Wavefronts and slabs of a block (kernel times, 4 KB of LDS per wavefront and slab; what counts is how many bytes a compute unit has in flight, so small blocks,
+// and how often a block's chain of index and rows is paid for, so not too small ones):
+//  - K up to 1024: four wavefronts, one slab (64 tokens, two of 32 experts, 1024 x 4096: 16.7 us, two slabs 16.8, four 18.1; 40 tokens, one each, 12.4 / 13.2 / 13.7);
+//  - longer K: eight wavefronts, two slabs where that makes two blocks per compute unit (4096 x 16384, 64 experts, 64 tokens: 285 us = 6.9 TB/s, one slab 311, 64 KB
+//    per four wavefronts 433; 2048 x 8192, 32 experts: 57 and 64), else one (16 tokens, fc2 of 4096 x 1024: 10.1 and 12.0).
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
 {
     const int mean = (p.R + p.E - 1) / p.E;
     if (mean > 24) return launch_mx4_tiled(p, mean <= 64 ? 64 : mean <= 128 ? 128 : 256, s);
-    const long slots = (long)p.R / 32 + (p.E < p.R ? p.E : p.R);
-    const long wgs = (slots * (p.N / 32) + kXcds - 1) / kXcds * kXcds;         // upper bound of the work items, whole rounds of XCDs
-    if (wgs > 0xffffff) return fail(MOE_ERR_UNSUPPORTED, "moe_grouped_gemm_mx4: %ld workgroups exceed one launch", wgs);
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, p); };
-    if (p.out_scales) run(&mx4_stream_kernel<-1>);
-    else if (p.out_dtype == MOE_F16) run(&mx4_stream_kernel<MOE_F16>);
-    else if (p.out_dtype == MOE_BF16) run(&mx4_stream_kernel<MOE_BF16>);
-    else run(&mx4_stream_kernel<MOE_F32>);
-    return check_launch("moe_grouped_gemm_mx4");
+    if (p.K <= 1024) return launch_stream<4, 1, 1>(p, s);
+    return decode_active_experts(p.R, p.E) * (p.N / 64) >= 450 ? launch_stream<8, 2, 1>(p, s) : launch_stream<8, 1, 1>(p, s);
 }
 
 }  // namespace moe
