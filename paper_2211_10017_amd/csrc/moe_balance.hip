@@ -16,7 +16,7 @@
 
 namespace moe {
 
-constexpr int kBalanceMostBlocks = 256, kBalanceMostExperts = 1024, kBalanceMostK = 8;
+constexpr int kBalanceThreads = 512, kBalanceMostBlocks = 256, kBalanceMostExperts = 1024, kBalanceMostK = 8;
 
 struct BalanceArgs {
     const void *logits;         // [T, E]
@@ -42,33 +42,49 @@ __device__ inline float to_f32(uint32_t bits)
     return __uint_as_float(bits << 16);
 }
 
-// FULL: the lanes and steps of a token hold its E logits and nothing besides, as they do for powers of two from eight on.
-// What a lane holds of a token: V neighbouring logits in each of S steps, as they lie in memory, and the token's experts.  Requested one token ahead.
-template <int DT, int V, int S, bool FULL>
+// FULL: the lanes and steps of a token hold its E logits and nothing besides, as they do for powers of two from eight on.  KM: the most experts of a token (with eight
+// for all, a token's scalar work is most of it: 131072 tokens by 256 experts, two each, forward 43 us).
+// What a lane holds of a token: V neighbouring logits in each of S steps, as they lie in memory, the token's experts, their logits and the gradients of their
+// scales.  Requested one token ahead, the experts, which the others' addresses depend on, two.
+template <int DT, int V, int S, bool FULL, int KM>
 struct TokenLoad {
     static constexpr int W = V == 1 ? 1 : DT == MOE_F32 ? 4 : 2;      // words of a step
-    uint32_t raw[S][W];
-    int e[kBalanceMostK];
+    uint32_t raw[S][W], chosen[KM];
+    int e[KM];
+    float ds[KM];
 
-    __device__ inline void request(const BalanceArgs &a, int t, int lane_in)
+    __device__ inline void request_experts(const BalanceArgs &a, int t)
     {
 #pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j)
+        for (int j = 0; j < KM; ++j)
             if (j < a.k) e[j] = a.idx[(size_t)t * a.k + j];
+    }
+    __device__ inline void request(const BalanceArgs &a, int t, int lane_in)
+    {
+        const uint32_t *z32 = reinterpret_cast<const uint32_t *>(a.logits);
+        const uint16_t *z16 = reinterpret_cast<const uint16_t *>(a.logits);
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const int c = V * (lane_in + a.L * s);
             const size_t at = (size_t)t * a.E + (FULL ? c : min(c, a.E - V));      // (past the end: what the last lane holds, which value() leaves out)
-            if constexpr (V == 1) raw[s][0] = DT == MOE_F32 ? reinterpret_cast<const uint32_t *>(a.logits)[at] : reinterpret_cast<const uint16_t *>(a.logits)[at];
+            if constexpr (V == 1) raw[s][0] = DT == MOE_F32 ? z32[at] : z16[at];
             else if constexpr (DT == MOE_F32) {
-                const uint4 q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const float *>(a.logits) + at);
+                const uint4 q = *reinterpret_cast<const uint4 *>(z32 + at);
                 raw[s][0] = q.x, raw[s][1] = q.y, raw[s][2] = q.z, raw[s][3] = q.w;
             } else {
-                const uint2 q = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(a.logits) + at);
+                const uint2 q = *reinterpret_cast<const uint2 *>(z16 + at);
                 raw[s][0] = q.x, raw[s][1] = q.y;
             }
         }
+#pragma unroll
+        for (int j = 0; j < KM; ++j) {
+            if (j >= a.k) break;
+            const size_t at = (size_t)t * a.E + (used(a, j) ? e[j] : 0);
+            chosen[j] = DT == MOE_F32 ? z32[at] : z16[at];
+            if (a.dscale) ds[j] = a.dscale[(size_t)t * a.k + j];
+        }
     }
+    __device__ inline bool used(const BalanceArgs &a, int j) const { return e[j] >= 0 && e[j] < a.E; }
     __device__ inline float value(const BalanceArgs &a, int s, int i, int lane_in) const
     {
         if (!FULL && V * (lane_in + a.L * s) >= a.E) return -INFINITY;
@@ -112,8 +128,8 @@ __device__ inline float over_lanes(float v, int L, Op op)
 
 // Softmax of a token over its L lanes: p[s][i] inv is that of column V (lane_in + L s) + i, and exp_of(z - base) inv that of any logit z of it.
 // A token whose logits are all -infinity has nothing to choose: inv = 0.  (A NaN or +infinity among them makes its p NaN.)
-template <int DT, int V, int S, bool FULL>
-__device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V, S, FULL> &x, int lane_in, float (&p)[S][V], float &base, float &inv)
+template <int DT, int V, int S, bool FULL, int KM>
+__device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V, S, FULL, KM> &x, int lane_in, float (&p)[S][V], float &base, float &inv)
 {
     float m = -INFINITY;
 #pragma unroll
@@ -134,30 +150,30 @@ __device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V
     inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 }
 
-// Logit of expert e (the first one for a slot without an expert).
-template <int DT>
-__device__ inline float logit_of(const BalanceArgs &a, int t, int e)
-{
-    const size_t at = (size_t)t * a.E + (e >= 0 && e < a.E ? e : 0);
-    return to_f32<DT>(DT == MOE_F32 ? reinterpret_cast<const uint32_t *>(a.logits)[at] : reinterpret_cast<const uint16_t *>(a.logits)[at]);
-}
-
 // The tokens of a thread's L lanes, one after the other, the next one's loads ahead of the work on this one: f(token, whether it is there, loads).
-template <int DT, int V, int S, bool FULL, class F>
+// (Two tokens a turn, so that what is loaded need not be moved, which would wait for it.)
+template <int DT, int V, int S, bool FULL, int KM, class F>
 __device__ inline void for_tokens(const BalanceArgs &a, int lane_in, F f)
 {
     const int per = blockDim.x / a.L, mine = threadIdx.x / a.L;
     const long step = (long)gridDim.x * per;
     auto at = [&](long t) { return (int)(t < a.T ? t : a.T - 1); };
-    long t = (long)blockIdx.x * per + mine;
-    const long end = (long)blockIdx.x * per;                       // (the block's first token: its loop ends for all of its threads at once)
     if (a.T == 0) return;
-    TokenLoad<DT, V, S, FULL> now, next;
-    now.request(a, at(t), lane_in);
-    for (long first = end; first < a.T; first += step, t += step) {
+    TokenLoad<DT, V, S, FULL, KM> x, y;
+    long first = (long)blockIdx.x * per, t = first + mine;         // (the block's first token: its loop ends for all of its threads at once)
+    x.request_experts(a, at(t));
+    y.request_experts(a, at(t + step));
+    x.request(a, at(t), lane_in);
+    auto turn = [&](TokenLoad<DT, V, S, FULL, KM> &now, TokenLoad<DT, V, S, FULL, KM> &next) {
         next.request(a, at(t + step), lane_in);
         f(at(t), t < a.T, now);
-        now = next;
+        now.request_experts(a, at(t + 2 * step));
+        first += step, t += step;
+    };
+    while (first < a.T) {
+        turn(x, y);
+        if (first >= a.T) break;
+        turn(y, x);
     }
 }
 
@@ -193,8 +209,8 @@ __device__ inline void balance_end(const BalanceArgs &a, const float (&ps)[4], c
     *a.loss = loss;
 }
 
-template <int DT, int V, int S, bool FULL>
-__global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
+template <int DT, int V, int S, bool FULL, int KM>
+__global__ __launch_bounds__(kBalanceThreads) void balance_forward_kernel(BalanceArgs a)
 {
     extern __shared__ float sums[];                             // [wavefronts][E]
     __shared__ int32_t cnt[kBalanceMostExperts + 1];
@@ -202,27 +218,26 @@ __global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
     for (int i = tid; i <= a.E; i += blockDim.x) cnt[i] = 0;
     __syncthreads();
     float acc[S][V] = {};
-    for_tokens<DT, V, S, FULL>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL> &x) {
-        float chosen[kBalanceMostK], total = 0.0f, base, inv, p[S][V];
-#pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j)
-            if (j < a.k) chosen[j] = logit_of<DT>(a, t, x.e[j]);
-        token_softmax<DT, V, S, FULL>(a, x, lane_in, p, base, inv);
+    for_tokens<DT, V, S, FULL, KM>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL, KM> &x) {
+        float chosen[KM], total = 0.0f, base, inv, p[S][V];
+        token_softmax<DT, V, S, FULL, KM>(a, x, lane_in, p, base, inv);
         bool live = false;
 #pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j) {
+        for (int j = 0; j < KM; ++j) {
             if (j >= a.k) break;
-            const bool used = x.e[j] >= 0 && x.e[j] < a.E;
-            chosen[j] = used ? exp_of(chosen[j] - base) * inv : 0.0f;
+            const bool used = x.used(a, j);
+            chosen[j] = used ? exp_of(to_f32<DT>(x.chosen[j]) - base) * inv : 0.0f;
             total += chosen[j];
             live |= used;
             if (here && used && lane_in == 0) atomicAdd(&cnt[x.e[j]], 1);
         }
         if (here && live && lane_in == 0) atomicAdd(&cnt[a.E], 1);
-        const float div = a.renorm && a.k > 1 && total != 0.0f ? total : 1.0f;
+        const float norm = a.renorm && a.k > 1 && total != 0.0f ? 1.0f / total : 1.0f;
+        if (here && lane_in == 0) {
 #pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j)
-            if (j < a.k && here && lane_in == 0) a.scale[(size_t)t * a.k + j] = chosen[j] / div;
+            for (int j = 0; j < KM; ++j)
+                if (j < a.k) a.scale[(size_t)t * a.k + j] = chosen[j] * norm;
+        }
         if (__all(here && live)) {
 #pragma unroll
             for (int s = 0; s < S; ++s)
@@ -250,7 +265,7 @@ __global__ __launch_bounds__(1024) void balance_forward_kernel(BalanceArgs a)
     if (gridDim.x == 1) {
         float ps[4] = {};
         int ns[4] = {};
-        const bool mine = 4 * tid < a.E;                        // (at most 256 threads of 512 or more)
+        const bool mine = 4 * tid < a.E;                        // (at most 256 threads)
         if (mine)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -316,8 +331,8 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a, int
     balance_end(a, ps, ns, q, strand == 0 && q < quads, N);
 }
 
-template <int DT, int V, int S, bool FULL>
-__global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
+template <int DT, int V, int S, bool FULL, int KM>
+__global__ __launch_bounds__(kBalanceThreads) void balance_backward_kernel(BalanceArgs a)
 {
     const int lane_in = threadIdx.x & (a.L - 1), L = a.L;
     const float dloss = a.dloss ? *a.dloss : 0.0f;
@@ -330,44 +345,38 @@ __global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
             w[s][i] = c < a.E ? dloss * a.weight[c] : 0.0f;
         }
     const bool renorm = a.renorm && a.k > 1;
-    for_tokens<DT, V, S, FULL>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL> &x) {
-        float sc[kBalanceMostK], ds[kBalanceMostK], total = 0.0f, base, inv, p[S][V];
-#pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j) {
-            if (j >= a.k) break;
-            sc[j] = logit_of<DT>(a, t, x.e[j]);
-            ds[j] = a.dscale ? a.dscale[(size_t)t * a.k + j] : 0.0f;
-        }
-        token_softmax<DT, V, S, FULL>(a, x, lane_in, p, base, inv);
+    for_tokens<DT, V, S, FULL, KM>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL, KM> &x) {
+        float sc[KM], ds[KM], total = 0.0f, base, inv, p[S][V];
+        token_softmax<DT, V, S, FULL, KM>(a, x, lane_in, p, base, inv);
         bool live = false;
 #pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j) {
+        for (int j = 0; j < KM; ++j) {
             if (j >= a.k) break;
-            const bool used = x.e[j] >= 0 && x.e[j] < a.E;
-            sc[j] = used ? exp_of(sc[j] - base) * inv : 0.0f;
-            if (!used) ds[j] = 0.0f;
+            const bool used = x.used(a, j);
+            sc[j] = used ? exp_of(to_f32<DT>(x.chosen[j]) - base) * inv : 0.0f;
+            ds[j] = used && a.dscale ? x.ds[j] : 0.0f;
             total += sc[j];
             live |= used;
         }
-        const float div = renorm && total != 0.0f ? total : 1.0f;
+        const float norm = renorm && total != 0.0f ? 1.0f / total : 1.0f;
         float mean = 0.0f;                                    // sum_j s_j ds_j
 #pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j) {
+        for (int j = 0; j < KM; ++j) {
             if (j >= a.k) break;
-            sc[j] /= div;
+            sc[j] *= norm;
             mean += sc[j] * ds[j];
         }
         // Renormalised scales are a softmax over the chosen experts: s_j (ds_j - sum_i s_i ds_i), which, as the s_i add up to one, is
         // s_j sum_i s_i (ds_j - ds_i): nothing is lost where the ds are nearly the same.
-        float gate[kBalanceMostK];
+        float gate[KM];
 #pragma unroll
-        for (int j = 0; j < kBalanceMostK; ++j) {
+        for (int j = 0; j < KM; ++j) {
             if (j >= a.k) break;
             float d = ds[j];
             if (renorm) {
                 d = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kBalanceMostK; ++i)
+                for (int i = 0; i < KM; ++i)
                     if (i < a.k) d += sc[i] * (ds[j] - ds[i]);
             }
             gate[j] = sc[j] * d;
@@ -387,7 +396,7 @@ __global__ __launch_bounds__(512) void balance_backward_kernel(BalanceArgs a)
             for (int i = 0; i < V; ++i) {
                 g[i] = p[q][i] * inv * (w[q][i] - off);
 #pragma unroll
-                for (int j = 0; j < kBalanceMostK; ++j) {
+                for (int j = 0; j < KM; ++j) {
                     if (j >= a.k) break;
                     if (x.e[j] == c + i) g[i] += gate[j];
                 }
@@ -413,42 +422,37 @@ static BalanceShape balance_shape(int E)
     return b;
 }
 
-// Threads of a forward block: its wavefronts' sums take 64 KB of LDS at most together with the counts.
-static int balance_threads(int E) { return E <= 512 ? 1024 : 512; }
-
 // Blocks of the forward launch.  Up to four rounds of tokens stay in one block, which then needs no second launch to join the blocks' sums (4 us).
 static int balance_blocks(int T, int E)
 {
-    const long per = balance_threads(E) / balance_shape(E).L, want = T <= 4 * per ? 1 : ((long)T + per - 1) / per;
+    const long per = kBalanceThreads / balance_shape(E).L, want = T <= 4 * per ? 1 : ((long)T + per - 1) / per;
     return (int)(want < kBalanceMostBlocks ? want : kBalanceMostBlocks);
 }
 
-// Calls f(element type, V, S, FULL) as compile-time numbers.
+// Calls f(element type, V, S, FULL, KM) as compile-time numbers.
 template <class F>
-static void with_shape(int dtype, int E, const BalanceShape &b, F f)
+static void with_shape(int dtype, int E, int k, const BalanceShape &b, F f)
 {
-    auto steps = [&](auto dt) {
-        auto go = [&](auto v, auto s) { f(dt, v, s, std::false_type{}); };
+    auto shapes = [&](auto dt, auto full, auto km) {
         using std::integral_constant;
         if (b.V == 4) {
-            auto four = [&](auto full) {
-                if (b.S == 1) f(dt, integral_constant<int, 4>{}, integral_constant<int, 1>{}, full);
-                else if (b.S == 2) f(dt, integral_constant<int, 4>{}, integral_constant<int, 2>{}, full);
-                else f(dt, integral_constant<int, 4>{}, integral_constant<int, 4>{}, full);
-            };
-            if (E == 4 * b.L * b.S) four(std::true_type{});
-            else four(std::false_type{});
-        } else {
-            if (b.S == 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-            else if (b.S == 2) go(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-            else if (b.S == 4) go(integral_constant<int, 1>{}, integral_constant<int, 4>{});
-            else if (b.S == 8) go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
-            else go(integral_constant<int, 1>{}, integral_constant<int, 16>{});
+            if (b.S == 1) f(dt, integral_constant<int, 4>{}, integral_constant<int, 1>{}, full, km);
+            else if (b.S == 2) f(dt, integral_constant<int, 4>{}, integral_constant<int, 2>{}, full, km);
+            else f(dt, integral_constant<int, 4>{}, integral_constant<int, 4>{}, full, km);
+        } else if constexpr (!decltype(full)::value) {
+            if (b.S == 1) f(dt, integral_constant<int, 1>{}, integral_constant<int, 1>{}, full, km);
+            else if (b.S <= 4) f(dt, integral_constant<int, 1>{}, integral_constant<int, 4>{}, full, km);
+            else f(dt, integral_constant<int, 1>{}, integral_constant<int, 16>{}, full, km);
         }
     };
-    if (dtype == MOE_F16) steps(std::integral_constant<int, MOE_F16>{});
-    else if (dtype == MOE_BF16) steps(std::integral_constant<int, MOE_BF16>{});
-    else steps(std::integral_constant<int, MOE_F32>{});
+    auto types = [&](auto full, auto km) {
+        if (dtype == MOE_F16) shapes(std::integral_constant<int, MOE_F16>{}, full, km);
+        else if (dtype == MOE_BF16) shapes(std::integral_constant<int, MOE_BF16>{}, full, km);
+        else shapes(std::integral_constant<int, MOE_F32>{}, full, km);
+    };
+    if (k > 2) types(std::false_type{}, std::integral_constant<int, kBalanceMostK>{});
+    else if (E == 4 * b.L * b.S) types(std::true_type{}, std::integral_constant<int, 2>{});
+    else types(std::false_type{}, std::integral_constant<int, 2>{});
 }
 
 static int check_balance(const char *what, const void *logits, int dtype, const int32_t *idx, int T, int E, int k)
@@ -482,16 +486,16 @@ extern "C" int moe_balance_loss(const void *logits, int dtype, const int32_t *ex
     if (!workspace || workspace_bytes < need) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned16(workspace)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     const BalanceShape b = balance_shape(E);
-    const int blocks = balance_blocks(T, E), threads = balance_threads(E);
+    const int blocks = balance_blocks(T, E);
     hipStream_t s = as_stream(stream);
     BalanceArgs a{};
     a.logits = logits, a.idx = expert_idx, a.T = T, a.E = E, a.k = k, a.renorm = renormalize, a.L = b.L, a.coef = coef, a.scale = expert_scale;
     const size_t all = (size_t)blocks * round_up(E, 4);
     a.part = (float *)workspace, a.part_count = (int32_t *)workspace + all, a.part_live = (int32_t *)workspace + 2 * all;
     a.loss = loss, a.counts = counts, a.prob_mean = prob_mean, a.weight = weight;
-    with_shape(dtype, E, b, [&](auto dt, auto v, auto st, auto full) {
-        hipLaunchKernelGGL((balance_forward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value, decltype(full)::value>), dim3(blocks), dim3(threads),
-                               threads / 64 * E * 4, s, a);
+    with_shape(dtype, E, k, b, [&](auto dt, auto v, auto st, auto full, auto km) {
+        hipLaunchKernelGGL((balance_forward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value, decltype(full)::value, decltype(km)::value>), dim3(blocks), dim3(kBalanceThreads),
+                           kBalanceThreads / 64 * E * 4, s, a);
     });
     if (blocks == 1) return check_launch(what);
     if (int rc = check_launch(what)) return rc;
@@ -509,13 +513,13 @@ extern "C" int moe_balance_loss_backward(const void *logits, int dtype, const in
     if (!weight || !dlogits) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(dlogits)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     const BalanceShape b = balance_shape(E);
-    const long want = ((long)T * b.L + 511) / 512;
+    const long want = ((long)T * b.L + kBalanceThreads - 1) / kBalanceThreads;
     BalanceArgs a{};
     a.logits = logits, a.idx = expert_idx, a.T = T, a.E = E, a.k = k, a.renorm = renormalize, a.L = b.L;
     a.weight = const_cast<float *>(weight), a.dloss = dloss, a.dscale = dscale, a.dlogits = dlogits;
-    with_shape(dtype, E, b, [&](auto dt, auto v, auto st, auto full) {
-        hipLaunchKernelGGL((balance_backward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value, decltype(full)::value>), dim3((unsigned)(want < 2048 ? want : 2048)),
-                           dim3(512), 0, as_stream(stream), a);
+    with_shape(dtype, E, k, b, [&](auto dt, auto v, auto st, auto full, auto km) {
+        hipLaunchKernelGGL((balance_backward_kernel<decltype(dt)::value, decltype(v)::value, decltype(st)::value, decltype(full)::value, decltype(km)::value>), dim3((unsigned)(want < kBalanceMostBlocks ? want : kBalanceMostBlocks)),
+                           dim3(kBalanceThreads), 0, as_stream(stream), a);
     });
     return check_launch(what);
 }
