@@ -70,7 +70,7 @@ struct MxArgs {
 };
 
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s);
-int launch_mx4_tiled(const MxArgs &p, int bm, hipStream_t s);
+int launch_mx4_tiled(const MxArgs &p, hipStream_t s);
 int launch_mx4_quantize_rows(const void *x, int dtype, int R, int K, long stride, uint8_t *codes, uint8_t *scales, hipStream_t s);
 
 }  // namespace moe

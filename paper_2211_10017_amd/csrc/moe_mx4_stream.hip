@@ -146,10 +146,12 @@ static int launch_stream(const MxArgs &p, hipStream_t s)
 //  - K up to 1024: four wavefronts, one slab (64 tokens, two of 32 experts, 1024 x 4096: 16.7 us, two slabs 16.8, four 18.1; 40 tokens, one each, 12.4 / 13.2 / 13.7);
 //  - longer K: eight wavefronts, two slabs where that makes two blocks per compute unit (4096 x 16384, 64 experts, 64 tokens: 285 us = 6.9 TB/s, one slab 311, 64 KB
 //    per four wavefronts 433; 2048 x 8192, 32 experts: 57 and 64), else one (16 tokens, fc2 of 4096 x 1024: 10.1 and 12.0).
+// Row tiles from 25 rows per expert on (us, streaming / tiles: 384 tokens, two of 32 experts of 1024 x 4096, 24 rows, fc1 21.3 / 19.1, fc2 20.7 / 19.8, of 2048 x 8192 65 / 64
+// and 59 / 69; 32 rows 27.7 / 19.7 and 22.4 / 20.5; 16 rows 20.4 / 18.7 and 16.9 / 20.1).
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
 {
     const int mean = (p.R + p.E - 1) / p.E;
-    if (mean > 24) return launch_mx4_tiled(p, mean <= 64 ? 64 : mean <= 128 ? 128 : 256, s);
+    if (mean > 24) return launch_mx4_tiled(p, s);
     if (p.K <= 1024) return launch_stream<4, 1, 1>(p, s);
     return decode_active_experts(p.R, p.E) * (p.N / 64) >= 450 ? launch_stream<8, 2, 1>(p, s) : launch_stream<8, 1, 1>(p, s);
 }
