@@ -5,8 +5,10 @@ device pointers into its C entry points (loaded on first use, and failing loudly
 library has not been built).  ``workloads`` holds the seeded synthetic input generators.
 """
 
-from . import binding, layer, workloads  # noqa: E402,F401
+from . import binding, layer, mx4_layer, router, workloads  # noqa: E402,F401
 from .layer import MoEExpertLayer  # noqa: E402,F401
+from .mx4_layer import MoEMx4Layer  # noqa: E402,F401
+from .router import balance_loss  # noqa: E402,F401
 from .binding import (MoeError, moe_combine, moe_gate_topk, moe_grouped_ffn_wq,  # noqa: E402,F401
                       moe_grouped_ffn_wq_workspace_bytes, moe_permute, moe_permute_workspace_bytes,
                       moe_quantize_experts)

@@ -241,6 +241,14 @@ def moe_permute(expert_idx, x, E: int, out=None, workspace=None):
     return x_perm, perm_src, inv_perm, offsets
 
 
+def moe_permute_index(expert_idx, E: int, d: int, act_dtype, perm_src, inv_perm, expert_offsets, workspace):
+    """moe_permute without the copy of the rows, into buffers of the caller's."""
+    T, k = expert_idx.shape
+    rc = load().moe_permute(_ptr(expert_idx, torch.int32, "expert_idx"), None, _DT[act_dtype], T, k, E, d, None, _ptr(perm_src, torch.int32, "perm_src"),
+                            _ptr(inv_perm, torch.int32, "inv_perm"), _ptr(expert_offsets, torch.int32, "expert_offsets"), _ptr(workspace), workspace.numel(), _stream())
+    _check(rc, "moe_permute")
+
+
 def moe_grouped_ffn_wq_workspace_bytes(R: int, d: int, F: int, E: int, act_dtype) -> int:
     return int(load().moe_grouped_ffn_wq_workspace_bytes(R, d, F, E, _DT[act_dtype]))
 
