@@ -325,6 +325,18 @@ __device__ inline void load_to_lds16(const void *src, uint16_t *dst)
     else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(l) : "memory", "m0");
 }
 
+// The same from a wavefront's base and an offset per lane.
+__device__ inline void load_to_lds16_at(const void *base, uint32_t offset, void *dst)
+{
+    const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)dst;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(l) : "memory", "m0");
+}
+__device__ inline void load_to_lds4_at(const void *base, uint32_t offset, void *dst)
+{
+    const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)dst;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(l) : "memory", "m0");
+}
+
 // The same with 4 bytes per lane: lane l's bytes land at dst + 4 l.
 __device__ inline void load_to_lds4(const void *src, void *dst)
 {

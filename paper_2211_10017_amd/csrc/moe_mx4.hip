@@ -8,6 +8,7 @@ static int check_product(const char *what, int R, int E, int a_rows, int K, int 
     if (R < 0 || E < 0 || a_rows < 0 || K <= 0 || N <= 0 || K % 64 || N % 32)
         return fail(MOE_ERR_INVALID_ARG, "%s: need R, E and rows >= 0, K %% 64 == 0, N %% 32 == 0 (R=%d E=%d rows=%d K=%d N=%d)", what, R, E, a_rows, K, N);
     if (perm_src ? k < 1 : a_rows < R) return fail(MOE_ERR_INVALID_ARG, "%s: without perm_src there are as many rows as R, with it k >= 1", what);
+    if (a_rows > 0x3fffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are more than 2^30", what, a_rows);
     if (E > 4096) return fail(MOE_ERR_UNSUPPORTED, "%s: E = %d above 4096", what, E);
     return MOE_OK;
 }
@@ -63,13 +64,14 @@ extern "C" int moe_grouped_ffn_mx4(const void *x, int act_dtype, int T, const in
     hipStream_t s = as_stream(stream);
     uint8_t *xq = (uint8_t *)workspace, *xs = xq + round_up(mx_code_bytes(T, d), 256);
     uint8_t *hq = xs + round_up(mx_scale_bytes(T, d), 256), *hs = hq + round_up(mx_code_bytes(R, F), 256);
-    if (int rc = launch_mx4_quantize_rows(x, act_dtype, T, d, d, xq, xs, s)) return rc;
     MxArgs p{};
+    if (mx4_fuses_rows(R, E, F, act_dtype)) p.x = x, p.x_dtype = act_dtype;
+    else if (int rc = launch_mx4_quantize_rows(x, act_dtype, T, d, d, xq, xs, s)) return rc;
     p.a = xq, p.as = xs, p.a_rows = T, p.a_src = perm_src, p.a_div = k, p.offsets = expert_offsets;
     p.w = (const uint8_t *)w1_codes, p.ws = (const uint8_t *)w1_scales, p.bias = (const __half *)b1;
     p.out = hq, p.out_scales = hs, p.E = E, p.R = R, p.K = d, p.N = F, p.act = activation;
     if (int rc = launch_mx4_gemm(p, s)) return rc;
-    p.a = hq, p.as = hs, p.a_rows = R, p.a_src = nullptr, p.w = (const uint8_t *)w2_codes, p.ws = (const uint8_t *)w2_scales, p.bias = (const __half *)b2;
+    p.x = nullptr, p.a = hq, p.as = hs, p.a_rows = R, p.a_src = nullptr, p.w = (const uint8_t *)w2_codes, p.ws = (const uint8_t *)w2_scales, p.bias = (const __half *)b2;
     p.out = y_perm, p.out_scales = nullptr, p.out_dtype = y_dtype, p.K = F, p.N = d, p.act = MOE_ACT_NONE;
     return launch_mx4_gemm(p, s);
 }

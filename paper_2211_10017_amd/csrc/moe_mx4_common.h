@@ -56,6 +56,8 @@ __device__ inline float mx_scale_value(uint32_t byte)
 struct MxArgs {
     const uint8_t *a;         // codes [a_rows, K/2]
     const uint8_t *as;        // scales [ceil(K/128), a_rows, 4]
+    const void *x;            // or null: rows [a_rows, K] that are not quantised yet, in x_dtype (16 bits); only where mx4_fuses_rows says so
+    int x_dtype;
     int a_rows;
     const int32_t *a_src;     // [R] or null: row r is a[a_src[r] / a_div]
     int a_div;
@@ -70,6 +72,7 @@ struct MxArgs {
 };
 
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s);
+bool mx4_fuses_rows(int R, int E, int N, int x_dtype);
 int launch_mx4_tiled(const MxArgs &p, hipStream_t s);
 int launch_mx4_quantize_rows(const void *x, int dtype, int R, int K, long stride, uint8_t *codes, uint8_t *scales, hipStream_t s);
 

@@ -13,13 +13,48 @@ namespace moe {
 //
 // Of 256 values lane (r, h) takes blocks 4 h .. 4 h + 3 of its channel (or row), and step j multiplies block 4 h + j of both operands: any pairing of
 // blocks with steps will do as long as it is the same on both sides, and with this one the scales of a lane's four steps are one dword.
+//
+// XDT (MOE_F16 | MOE_BF16, or -1: codes): rows that are not quantised yet.  As a lane's operand is a whole block of its row, it quantises what it multiplies
+// without a word to any other, which saves a launch where there are few blocks to repeat it (mx4_fuses_rows).
+// A block of 32 16-bit values as codes, and its scale byte; the same bits as mx4_quantize_rows_kernel.
+template <int XDT>
+__device__ inline u32x4_t mx_quantize_block(const u32x4_t (&raw)[4], uint32_t &byte)
+{
+    typedef unsigned short us2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+    us2_t m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2_t, raw[i >> 2][i & 3] & 0x7fff7fffu));
+    const uint16_t top = m[0] > m[1] ? m[0] : m[1];
+    byte = mx_scale_byte(XDT == MOE_BF16 ? (uint32_t)top << 16 : __float_as_uint((float)__builtin_bit_cast(_Float16, top)));
+    const float s = mx_scale_operand(byte);
+    u32x4_t c;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t d = 0;
+        if constexpr (XDT == MOE_BF16) {
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][0]), s, 0);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][1]), s, 1);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][2]), s, 2);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][3]), s, 3);
+        } else {
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(d, bits_h2(raw[q][0]), s, 0);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(d, bits_h2(raw[q][1]), s, 1);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(d, bits_h2(raw[q][2]), s, 2);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(d, bits_h2(raw[q][3]), s, 3);
+        }
+        c[q] = byte == 255 ? 0u : d;
+    }
+    return c;
+}
+
 template <int WAVES, int NS, int CPW>
 struct MxStream {
     static constexpr int kWave = NS * CPW * 4096;
     static constexpr int kLds = WAVES * kWave;          // (the partial sums, 4 KB per wavefront and slab, fit as well)
 };
 
-template <int WAVES, int NS, int CPW, int OUT>
+template <int WAVES, int NS, int CPW, int OUT, int XDT>
 __global__ __launch_bounds__(64 * WAVES) void mx4_stream_kernel(MxArgs p)
 {
     extern __shared__ __align__(16) uint8_t lds[];
@@ -54,7 +89,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_stream_kernel(MxArgs p)
     request(0);
     const int out_row = row0 + min(r, rows - 1);             // (lanes past the rows repeat the last one)
     const int a_row = p.a_src ? min(max(p.a_src[out_row] / p.a_div, 0), p.a_rows - 1) : out_row;
-    const uint8_t *a = p.a + (size_t)a_row * (K / 2);
+    const uint8_t *a = XDT < 0 ? p.a + (size_t)a_row * (K / 2) : reinterpret_cast<const uint8_t *>(p.x) + (size_t)a_row * K * 2;
     const uint32_t *as = reinterpret_cast<const uint32_t *>(p.as) + a_row;
 
     float16_t acc[NS] = {};
@@ -68,12 +103,28 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_stream_kernel(MxArgs p)
             const int g = min(b0 / 4, G - 1);
             // scales of blocks that are not there may hold anything; the rows' codes are zero there
             const uint32_t mask = b0 + 4 <= blocks ? 0xffffffffu : b0 < blocks ? (1u << (8 * (blocks - b0))) - 1 : 0;
+            if constexpr (XDT < 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                aq[i][j] = u32x4_t{};
-                if (b0 + j < blocks) aq[i][j] = *reinterpret_cast<const u32x4_t *>(a + (size_t)(b0 + j) * 16);
+                for (int j = 0; j < 4; ++j) {
+                    aq[i][j] = u32x4_t{};
+                    if (b0 + j < blocks) aq[i][j] = *reinterpret_cast<const u32x4_t *>(a + (size_t)(b0 + j) * 16);
+                }
+                asc[i] = as[(size_t)g * p.a_rows] & mask;
+            } else {
+                u32x4_t raw[4][4] = {};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (b0 + j < blocks)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) raw[j][q] = *reinterpret_cast<const u32x4_t *>(a + (size_t)(b0 + j) * 64 + q * 16);
+                asc[i] = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t byte;
+                    aq[i][j] = mx_quantize_block<XDT>(raw[j], byte);
+                    asc[i] |= byte << (8 * j);
+                }
             }
-            asc[i] = as[(size_t)g * p.a_rows] & mask;
 #pragma unroll
             for (int s = 0; s < NS; ++s) wsc[i][s] = ws[(size_t)g * N + slab(s) + r] & mask;
         }
@@ -128,16 +179,19 @@ static int launch_stream(const MxArgs &p, hipStream_t s)
     const long slots = (long)p.R / 32 + (p.E < p.R ? p.E : p.R);
     const long wgs = (slots * ((p.N + 32 * NS - 1) / (32 * NS)) + kXcds - 1) / kXcds * kXcds;      // upper bound of the work items, whole rounds of XCDs
     if (wgs * WAVES > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "moe_grouped_gemm_mx4: %ld workgroups exceed one launch", wgs);
-    auto run = [&](auto out) {
-        constexpr int OUT = decltype(out)::value;
-        static std::atomic<uint64_t> raised;
-        if (S::kLds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(&mx4_stream_kernel<WAVES, NS, CPW, OUT>), S::kLds, raised);
-        hipLaunchKernelGGL((mx4_stream_kernel<WAVES, NS, CPW, OUT>), dim3((unsigned)wgs), dim3(64 * WAVES), S::kLds, s, p);
+    auto run = [&](auto out, auto x) {
+        constexpr int OUT = decltype(out)::value, XDT = decltype(x)::value;
+        hipLaunchKernelGGL((mx4_stream_kernel<WAVES, NS, CPW, OUT, XDT>), dim3((unsigned)wgs), dim3(64 * WAVES), S::kLds, s, p);
     };
-    if (p.out_scales) run(std::integral_constant<int, -1>{});
-    else if (p.out_dtype == MOE_F16) run(std::integral_constant<int, MOE_F16>{});
-    else if (p.out_dtype == MOE_BF16) run(std::integral_constant<int, MOE_BF16>{});
-    else run(std::integral_constant<int, MOE_F32>{});
+    static_assert(S::kLds <= 64 * 1024, "what a launch may ask for without more");
+    using std::integral_constant;
+    constexpr integral_constant<int, -1> codes{};
+    if (p.x && p.x_dtype == MOE_F16) run(codes, integral_constant<int, MOE_F16>{});
+    else if (p.x) run(codes, integral_constant<int, MOE_BF16>{});
+    else if (p.out_scales) run(codes, codes);
+    else if (p.out_dtype == MOE_F16) run(integral_constant<int, MOE_F16>{}, codes);
+    else if (p.out_dtype == MOE_BF16) run(integral_constant<int, MOE_BF16>{}, codes);
+    else run(integral_constant<int, MOE_F32>{}, codes);
     return check_launch("moe_grouped_gemm_mx4");
 }
 
@@ -148,12 +202,19 @@ static int launch_stream(const MxArgs &p, hipStream_t s)
 //    per four wavefronts 433; 2048 x 8192, 32 experts: 57 and 64), else one (16 tokens, fc2 of 4096 x 1024: 10.1 and 12.0).
 // Row tiles from 25 rows per expert on (us, streaming / tiles: 384 tokens, two of 32 experts of 1024 x 4096, 24 rows, fc1 21.3 / 19.1, fc2 20.7 / 19.8, of 2048 x 8192 65 / 64
 // and 59 / 69; 32 rows 27.7 / 19.7 and 22.4 / 20.5; 16 rows 20.4 / 18.7 and 16.9 / 20.1).
+static bool streams(int R, int E) { return (R + E - 1) / E <= 24; }
+
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
 {
-    const int mean = (p.R + p.E - 1) / p.E;
-    if (mean > 24) return launch_mx4_tiled(p, s);
+    if (!streams(p.R, p.E)) return launch_mx4_tiled(p, s);
     if (p.K <= 1024) return launch_stream<4, 1, 1>(p, s);
     return decode_active_experts(p.R, p.E) * (p.N / 64) >= 450 ? launch_stream<8, 2, 1>(p, s) : launch_stream<8, 1, 1>(p, s);
+}
+
+// Whether fc1 quantises its rows for itself: every block does so for the rows of its item, so only where there are few blocks.
+bool mx4_fuses_rows(int R, int E, int N, int x_dtype)
+{
+    return x_dtype != MOE_F32 && streams(R, E) && decode_active_experts(R, E) * (N / 32) <= 512;
 }
 
 }  // namespace moe

@@ -13,19 +13,19 @@ struct MxTile {
     static constexpr int W = WR * WC, BM = 32 * TM * WR, BN = 32 * TN * WC;
     static constexpr int kCodes = (BM + BN) * 64, kStage = kCodes + (BM + BN) * 4;
     static constexpr int NA = BM / 16 / W, NB = BN / 16 / W;             // code loads per wavefront and stage (16 rows each)
-    static constexpr int kChunks = (BM + BN) / 64, NC = (kChunks + W - 1) / W;      // scale loads (64 rows each): of the block, of a wavefront and stage
-    static constexpr int L = NA + NB + NC;
+    static constexpr int NCA = (BM / 64 + W - 1) / W, NCB = (BN / 64 + W - 1) / W;      // scale loads (64 rows each)
+    static constexpr int LA = NA + NCA, L = LA + NB + NCB;
     static constexpr int kLds = NST * kStage;
     static constexpr int kPerCu = 160 * 1024 / kLds < 1 ? 1 : 160 * 1024 / kLds;
     static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0, "loads are dealt evenly");
-    static_assert(NST >= 2 && (NST - 1) * L < 64 && kLds <= 160 * 1024, "a stage in use and one or more on their way");
+    static_assert(NST >= 2 && NST <= 3 && (NST - 1) * L < 64 && kLds <= 160 * 1024, "a stage in use and one or more on their way");
 };
 
 template <int WR, int WC, int TM, int TN, int NST, int OUT>
 __global__ __launch_bounds__(64 * WR * WC, TM *TN > 8 ? 1 : 2) void mx4_tile_kernel(MxArgs p)
 {
     using S = MxTile<WR, WC, TM, TN, NST>;
-    constexpr int W = S::W, BM = S::BM, BN = S::BN, NA = S::NA, NB = S::NB, NC = S::NC, L = S::L;
+    constexpr int W = S::W, BM = S::BM, BN = S::BN, NA = S::NA, NB = S::NB, NCA = S::NCA, NCB = S::NCB, LA = S::LA, L = S::L;
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
     const int r = lane & 31, h = lane >> 5;
@@ -40,38 +40,54 @@ __global__ __launch_bounds__(64 * WR * WC, TM *TN > 8 ? 1 : 2) void mx4_tile_ker
         const int out_row = row0 + min(i, rows - 1);
         return p.a_src ? min(max(p.a_src[out_row] / p.a_div, 0), p.a_rows - 1) : out_row;
     };
-    auto channel = [&](int i) { return min(col * BN + i, N - 1); };
     const int blk = (lane & 3) ^ ((lane >> 4) & 3);                     // the block of its row that this lane's loads bring
-    const uint8_t *a_ptr[NA], *b_ptr[NB], *s_ptr[NC];
-    long s_step[NC];
+    // Weights and scales: a base of the wavefront's and an offset per lane, so that going on to the next stage costs no vector instruction; rows, which may lie
+    // further apart than 32 bits reach, as pointers.
+    const int c0 = col * BN;
+    auto channel = [&](int i) { return (uint32_t)(min(c0 + i, N - 1) - c0); };
+    const uint8_t *w = p.w + ((size_t)e * N + c0) * (K / 2), *ws = p.ws + ((size_t)e * G * N + c0) * 4, *as = p.as;
+    uint32_t b_off[NB], bs_off[NCB], as_off[NCA];
+    const uint8_t *a_ptr[NA];
+    // (the second half of the last group may not be there: its lanes bring the first again)
+    auto back = [&](int s) { return 4 * s + blk < blocks ? 0 : 32; };
+    auto issue_weights = [&](int s, uint8_t *st) {                      // a stage's loads, to st in LDS
+        const int b = back(s);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) b_ptr[i] = p.w + ((size_t)e * N + channel((i * W + wave) * 16 + (lane >> 2))) * (K / 2) + blk * 16;
+        for (int i = 0; i < NB; ++i) load_to_lds16_at(w, b_off[i] - b, st + BM * 64 + (i * W + wave) * 1024);
+#pragma unroll
+        for (int i = 0; i < NCB; ++i) load_to_lds4_at(ws, bs_off[i], st + S::kCodes + BM * 4 + (i * W + wave) % (BN / 64) * 256);
+        w += 64, ws += (size_t)N * 4;
+    };
+    auto issue_rows = [&](int s, uint8_t *st) {
+        const int b = back(s);
+#pragma unroll
+        for (int i = 0; i < NA; ++i) load_to_lds16(a_ptr[i] - b, reinterpret_cast<uint16_t *>(st + (i * W + wave) * 1024)), a_ptr[i] += 64;
+#pragma unroll
+        for (int i = 0; i < NCA; ++i) load_to_lds4_at(as, as_off[i], st + S::kCodes + (i * W + wave) % (BM / 64) * 256);
+        as += (size_t)p.a_rows * 4;
+    };
+    // The first stages' weights are requested before the rows are known, so that the chain of index and rows runs under them.
+    // (A lane steps back only from blocks 2 and 3, so its offset stays positive.)
+#pragma unroll
+    for (int i = 0; i < NB; ++i) b_off[i] = channel((i * W + wave) * 16 + (lane >> 2)) * (uint32_t)(K / 2) + blk * 16;
+#pragma unroll
+    for (int i = 0; i < NCB; ++i) bs_off[i] = channel((i * W + wave) % (BN / 64) * 64 + lane) * 4;
+#pragma unroll
+    for (int s = 0; s < NST; ++s)
+        if (s < G) issue_weights(s, lds + s * S::kStage);
 #pragma unroll
     for (int i = 0; i < NA; ++i) a_ptr[i] = p.a + (size_t)source((i * W + wave) * 16 + (lane >> 2)) * (K / 2) + blk * 16;
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int c = (i * W + wave) % S::kChunks;
-        if (c < BM / 64) s_ptr[i] = p.as + (size_t)source(c * 64 + lane) * 4, s_step[i] = (long)p.a_rows * 4;
-        else s_ptr[i] = p.ws + ((size_t)e * G * N + channel((c - BM / 64) * 64 + lane)) * 4, s_step[i] = (long)N * 4;
-    }
-    int issued = 0;
-    auto issue = [&](int stage) {                                       // the loads of the next stage, to `stage` bytes into LDS
-        uint8_t *st = lds + stage;
-        const int back = 4 * issued + blk < blocks ? 0 : 32;            // (the second half of the last group may not be there)
+    for (int i = 0; i < NCA; ++i) as_off[i] = (uint32_t)source((i * W + wave) % (BM / 64) * 64 + lane) * 4;
 #pragma unroll
-        for (int i = 0; i < NA; ++i) load_to_lds16(a_ptr[i] - back, reinterpret_cast<uint16_t *>(st + (i * W + wave) * 1024)), a_ptr[i] += 64;
-#pragma unroll
-        for (int i = 0; i < NB; ++i) load_to_lds16(b_ptr[i] - back, reinterpret_cast<uint16_t *>(st + BM * 64 + (i * W + wave) * 1024)), b_ptr[i] += 64;
-#pragma unroll
-        for (int i = 0; i < NC; ++i) load_to_lds4(s_ptr[i], st + S::kCodes + (i * W + wave) % S::kChunks * 256), s_ptr[i] += s_step[i];
-        ++issued;
-    };
+    for (int s = 0; s < NST; ++s)
+        if (s < G) issue_rows(s, lds + s * S::kStage);
     auto run = [&](auto live_c) {
         constexpr int LIVE = decltype(live_c)::value;
         float16_t acc[LIVE][TN] = {};
         const int m0 = wr * LIVE * 32, n0 = wc * TN * 32;               // first row and channel of the wavefront
         u32x4_t a[2][LIVE], b[2][TN];
-        uint32_t as[LIVE], bs[TN], as_next[LIVE], bs_next[TN];
+        uint32_t asc[LIVE], bsc[TN], as_next[LIVE], bs_next[TN];
         const int swz = (r >> 2) & 3, at[2] = {(h ^ swz) * 16, ((2 + h) ^ swz) * 16};
         const uint8_t *a_lds = lds + (m0 + r) * 64, *b_lds = lds + BM * 64 + (n0 + r) * 64, *as_lds = lds + S::kCodes + (m0 + r) * 4, *bs_lds = lds + S::kCodes + (BM + n0 + r) * 4;
         auto read = [&](int stage, auto j_c) {                          // (stage: its place in LDS, in bytes)
@@ -89,9 +105,9 @@ __global__ __launch_bounds__(64 * WR * WC, TM *TN > 8 ? 1 : 2) void mx4_tile_ker
         };
         auto take_scales = [&]() {                                      // bytes 0 and 2 are then this lane's in steps 0 and 1
 #pragma unroll
-            for (int n = 0; n < TN; ++n) bs[n] = bs_next[n] >> (8 * h);
+            for (int n = 0; n < TN; ++n) bsc[n] = bs_next[n] >> (8 * h);
 #pragma unroll
-            for (int m = 0; m < LIVE; ++m) as[m] = as_next[m] >> (8 * h);
+            for (int m = 0; m < LIVE; ++m) asc[m] = as_next[m] >> (8 * h);
         };
         auto multiply = [&](auto j_c) {
             constexpr int J = decltype(j_c)::value;
@@ -101,36 +117,44 @@ __global__ __launch_bounds__(64 * WR * WC, TM *TN > 8 ? 1 : 2) void mx4_tile_ker
                 for (int n = 0; n < TN; ++n)
                     acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
                         i32x8_t{(int)b[J][n][0], (int)b[J][n][1], (int)b[J][n][2], (int)b[J][n][3], 0, 0, 0, 0},
-                        i32x8_t{(int)a[J][m][0], (int)a[J][m][1], (int)a[J][m][2], (int)a[J][m][3], 0, 0, 0, 0}, acc[m][n], 4, 4, 2 * J, (int)bs[n], 2 * J, (int)as[m]);
+                        i32x8_t{(int)a[J][m][0], (int)a[J][m][1], (int)a[J][m][2], (int)a[J][m][3], 0, 0, 0, 0}, acc[m][n], 4, 4, 2 * J, (int)bsc[n], 2 * J, (int)asc[m]);
         };
         constexpr std::integral_constant<int, 0> first{};
         constexpr std::integral_constant<int, 1> second{};
         // Every product's operands are read one step ahead of it: step 1's during step 0, the next stage's step 0 during step 1.  So stage s + 1 has to be
         // there in the middle of stage s; the stages after it may still be on their way.  The barrier there also says that everyone has read all of stage s,
-        // whose place is refilled.  (The scheduling barriers keep the products where they are: left to itself the compiler lines them up behind the
-        // barrier, where each wavefront then waits for all that it reads.)
-        if (G >= NST) wait_loads<(NST - 1) * L>();
+        // whose place is refilled.  (hold(): left to itself the compiler moves step 0's products behind the barrier, where they wait with step 1's.)
+        auto hold = [&]() {
+#pragma unroll
+            for (int m = 0; m < LIVE; ++m)
+#pragma unroll
+                for (int n = 0; n < TN; ++n) asm volatile("" : "+v"(acc[m][n]));
+        };
+        if (G >= NST) wait_loads<(NST - 2) * LA>();                     // (the first stages' weights came before all of their rows)
         else wait_loads<0>();
         __syncthreads();
         read(0, first);
         read_scales(0);
         int stage = 0;
-        for (int s = 0; s + 1 < G; ++s) {
+        auto iterate = [&](int s, auto more_c) {
             const int next = stage + S::kStage == NST * S::kStage ? 0 : stage + S::kStage;
             read(stage, second);
             take_scales();
             multiply(first);
-            __builtin_amdgcn_sched_barrier(0);
-            if (NST > 2 && s + NST <= G) wait_loads<(NST - 2) * L>();
+            hold();
+            if constexpr (decltype(more_c)::value) wait_loads<(NST - 2) * L>();
             else wait_loads<0>();
             __syncthreads();
             read(next, first);
             read_scales(next);
-            if (s + NST < G) issue(stage);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(more_c)::value) issue_weights(s + NST, lds + stage), issue_rows(s + NST, lds + stage);
             multiply(second);
+            hold();
             stage = next;
-        }
+        };
+        int s = 0;
+        for (; s + NST < G; ++s) iterate(s, std::true_type{});
+        for (; s + 1 < G; ++s) iterate(s, std::false_type{});
         if (4 * G - 2 < blocks) read(stage, second);
         take_scales();
         multiply(first);
@@ -149,9 +173,6 @@ __global__ __launch_bounds__(64 * WR * WC, TM *TN > 8 ? 1 : 2) void mx4_tile_ker
             }
         }
     };
-#pragma unroll
-    for (int s = 0; s < NST; ++s)
-        if (s < G) issue(s * S::kStage);
     if (TM == 1 || live == 1) run(std::integral_constant<int, 1>{});
     else if (live == 2) run(std::integral_constant<int, TM < 2 ? TM : 2>{});
     else if (live == 3) run(std::integral_constant<int, TM < 3 ? TM : 3>{});
@@ -178,10 +199,10 @@ static int launch_tile(const MxArgs &p, hipStream_t s)
     return check_launch("moe_grouped_gemm_mx4");
 }
 
-// Tiles of 128 rows by 256 channels, two blocks per compute unit, whose starts and ends overlap each other's loops (8192 tokens, two of 64 experts of 4096 x 16384: fc1 1013 us,
-// fc2 897; one block of 256 x 256 1056 and 868; 4096 tokens, two of 128 experts, 2048 x 8192, 287 and 337), and of 64 by 128 where that makes fewer than one
-// and a half of them per compute unit (997 tokens, two of 16 experts of 704 x 2880: 15.4 + 11.4 us, 22.0 + 28.5 in large ones; 768, two of 32, 4096 x 1024: 19.3 and 27.5;
-// left to large ones 1600, two of 32, 1024 x 4096: 26.1, small 33.7).
+// Tiles of 128 rows by 256 channels, two blocks per compute unit, whose starts and ends overlap each other's loops (8192 tokens, two of 64 experts of 4096 x 16384: fc1 942 us,
+// fc2 826; one block of 256 x 256 1065 and 786; 4096 tokens, two of 128 experts, 2048 x 8192, 281 and 359), and of 64 by 128 where that makes fewer than one
+// and a half of them per compute unit (997 tokens, two of 16 experts of 704 x 2880: 15.3 + 11.5 us, 20.9 + 24.1 in large ones; 768, two of 32, 4096 x 1024: 19.5 and 26.6;
+// left to large ones 1600, two of 32, 1024 x 4096: 25.5, small 32.4).
 int launch_mx4_tiled(const MxArgs &p, hipStream_t s)
 {
     return expected_row_tiles(p.R, p.E, 128) * ((p.N + 255) / 256) <= 384 ? launch_tile<2, 2, 1, 2, 3>(p, s) : launch_tile<1, 4, 4, 2, 3>(p, s);
