@@ -150,9 +150,9 @@ def _ptr(t, dtype=None, name="tensor"):
         return None
     if not t.is_cuda or not t.is_contiguous():
         raise MoeError("%s must be a contiguous CUDA tensor" % name)
-    if dtype is not None and t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+    if dtype is not None and t.dtype is not dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
         raise MoeError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 # What torch.cuda.current_stream() itself calls; not part of torch's interface, so a torch without them takes the long way.
@@ -168,7 +168,7 @@ def current_stream_handle() -> int:
 
 
 def _stream():
-    return ctypes.c_void_p(current_stream_handle())
+    return current_stream_handle()
 
 
 def moe_quantize_experts(w, bits: int, group_size: int = 0, want_canon: bool = True,
@@ -486,10 +486,14 @@ def _mx4_like(codes, scales, name):
 
 def moe_mx4_quantize_rows(x, out=None):
     """x [R, K] (rows may be strided) -> (codes uint8 [R, K/2], scales uint8 [ceil(K/128), R, 4])."""
-    if x.dim() != 2 or not x.is_cuda or x.dtype not in _FLOATS or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise MoeError("x must be a [R, K] CUDA tensor of fp16, bf16 or fp32 whose rows are contiguous")
-    R, K = x.shape
-    stride = x.stride(0) if R > 1 else K
+    dtype = _DT.get(x.dtype)
+    if dtype is None or x.dim() != 2 or not x.is_cuda:
+        raise MoeError("x must be a [R, K] CUDA tensor of fp16, bf16 or fp32")
+    (R, K), (stride, inner) = x.shape, x.stride()
+    if inner != 1 and K > 1:
+        raise MoeError("x must have contiguous rows")
+    if R == 1:
+        stride = K
     if out is None:
         dev = x.device
         codes, scales = torch.empty(R, K // 2, dtype=torch.uint8, device=dev), torch.empty(-(-K // 128), R, 4, dtype=torch.uint8, device=dev)
@@ -497,7 +501,7 @@ def moe_mx4_quantize_rows(x, out=None):
         codes, scales = out
         if _mx4_like(codes, scales, "out")[1:] != (R, K):
             raise MoeError("out does not fit x")
-    rc = load().moe_mx4_quantize_rows(x.data_ptr(), _DT[x.dtype], R, K, stride, _ptr(codes, torch.uint8, "codes"),
+    rc = load().moe_mx4_quantize_rows(x.data_ptr(), dtype, R, K, stride, _ptr(codes, torch.uint8, "codes"),
                                       _ptr(scales, torch.uint8, "scales"), _stream())
     _check(rc, "moe_mx4_quantize_rows")
     return codes, scales
@@ -592,7 +596,8 @@ def moe_grouped_ffn_mx4(x, expert_offsets, w1_codes, w1_scales, w2_codes, w2_sca
 # ---- the router's balance loss -------------------------------------------------------------------------------------------------------
 
 def _check_balance(logits, expert_idx):
-    if logits.dim() != 2 or expert_idx.dim() != 2 or expert_idx.shape[0] != logits.shape[0]:
+    z, i = logits.shape, expert_idx.shape
+    if len(z) != 2 or len(i) != 2 or z[0] != i[0]:
         raise MoeError("logits must be [T, E] and expert_idx [T, k]")
 
 
@@ -604,15 +609,19 @@ def moe_balance_loss(logits, expert_idx, coef: float = 0.01, renormalize: bool =
     """(loss [], counts int32 [E], prob_mean [E], expert_scale [T, k], weight [E]); weight is what moe_balance_loss_backward takes."""
     _check_balance(logits, expert_idx)
     (T, E), k, dev = logits.shape, expert_idx.shape[1], logits.device
-    lib, f32 = load(), torch.float32
-    loss, prob_mean, weight = (torch.empty((), dtype=f32, device=dev), torch.empty(E, dtype=f32, device=dev), torch.empty(E, dtype=f32, device=dev))
+    lib = load()
+    # (small tensors in one: an allocation costs the host as much as two views, and a decoder batch's call is all host)
+    sums = torch.empty(2 * E + 1, dtype=torch.float32, device=dev)
+    prob_mean, weight, loss = sums.as_strided((E,), (1,), 0), sums.as_strided((E,), (1,), E), sums.as_strided((), (), 2 * E)
     counts = torch.empty(E, dtype=torch.int32, device=dev)
-    scale = torch.empty(T, k, dtype=f32, device=dev)
+    scale = torch.empty(T, k, dtype=torch.float32, device=dev)
     if workspace is None:
-        workspace = torch.empty(lib.moe_balance_loss_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
+        need = lib.moe_balance_loss_workspace_bytes(T, E)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    at = sums.data_ptr()
     rc = lib.moe_balance_loss(_ptr(logits, _FLOATS, "logits"), _DT[logits.dtype], _ptr(expert_idx, torch.int32, "expert_idx"), T, E, k, int(renormalize),
-                              coef, loss.data_ptr(), counts.data_ptr(), prob_mean.data_ptr(), scale.data_ptr(), weight.data_ptr(),
-                              _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+                              coef, at + 8 * E, counts.data_ptr(), at, scale.data_ptr(), at + 4 * E, _ptr(workspace, torch.uint8, "workspace"),
+                              0 if workspace is None else workspace.numel(), _stream())
     _check(rc, "moe_balance_loss")
     return loss, counts, prob_mean, scale, weight
 

@@ -472,7 +472,7 @@ extern "C" size_t moe_balance_loss_workspace_bytes(int T, int E)
     using namespace moe;
     if (T < 0 || E < 1 || E > kBalanceMostExperts) return 0;
     const size_t blocks = balance_blocks(T, E), pitch = round_up(E, 4);
-    return blocks * (2 * pitch * 4 + 4) + 16;
+    return blocks == 1 ? 0 : blocks * (2 * pitch * 4 + 4);
 }
 
 extern "C" int moe_balance_loss(const void *logits, int dtype, const int32_t *expert_idx, int T, int E, int k, int renormalize, float coef, float *loss,
@@ -483,7 +483,8 @@ extern "C" int moe_balance_loss(const void *logits, int dtype, const int32_t *ex
     if (int rc = check_balance(what, logits, dtype, expert_idx, T, E, k)) return rc;
     if (!loss || !counts || !prob_mean || !weight || (T && !expert_scale)) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     const size_t need = moe_balance_loss_workspace_bytes(T, E);
-    if (!workspace || workspace_bytes < need) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : (size_t)0, need);
+    if (need && (!workspace || workspace_bytes < need))
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned16(workspace)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     const BalanceShape b = balance_shape(E);
     const int blocks = balance_blocks(T, E);
