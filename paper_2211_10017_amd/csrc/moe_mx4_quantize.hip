@@ -64,75 +64,84 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const void *__re
     }
 }
 
-// Experts: w is [K, N] with N contiguous and a block runs along K: a lane owns a channel and walks down the 32 values of a block, the eight wavefronts of
+// Experts: w is [K, N] with N contiguous and a block runs along K: a lane owns two channels and walks down the 32 values of a block, the eight wavefronts of
 // a workgroup eight blocks, and the codes go through LDS so that they are stored as whole lines too, eight lanes a channel.  Memory-bound.
-// (A lane storing its channel's sixteen bytes at a time: 32 experts of 1024 x 4096 173 us, so 135 = 4.5 TB/s.)
+// (A lane storing its channel's sixteen bytes at a time: 32 experts of 1024 x 4096 173 us, so 130 = 4.7 TB/s, a channel per lane 135.)
 __global__ __launch_bounds__(512) void mx4_quantize_experts_kernel(const float *__restrict__ w, int K, int N, uint8_t *__restrict__ codes,
                                                                    uint8_t *__restrict__ scales)
 {
-    __shared__ u32x4_t tile[64][9];                                    // (nine: neighbouring channels' blocks start in other banks)
-    __shared__ __align__(8) uint8_t bytes[64][8];
+    __shared__ u32x4_t tile[128][9];                                   // (nine: neighbouring channels' blocks start in other banks)
+    __shared__ __align__(8) uint8_t bytes[128][8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int blocks = K / kMxBlock, slices = (blocks + 7) / 8, ncol = (N + 63) / 64;
+    const int blocks = K / kMxBlock, slices = (blocks + 7) / 8, ncol = (N + 127) / 128;
     const int col = (int)(blockIdx.x % ncol), slice = (int)(blockIdx.x / ncol % slices);
     const size_t e = blockIdx.x / ncol / slices;
-    const int n = col * 64 + lane, block = slice * 8 + wave;
-    uint32_t byte = 0;
+    const int n = col * 128 + 2 * lane, block = slice * 8 + wave;
+    uint32_t byte[2] = {0, 0};
     if (n < N && block < blocks) {
         const float *src = w + (e * K + (size_t)block * kMxBlock) * N + n;
-        float v[32];
-        uint32_t amax = 0;
+        float2 v[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = src[(size_t)i * N];
+        for (int i = 0; i < 32; ++i) v[i] = *reinterpret_cast<const float2 *>(src + (size_t)i * N);
+        uint32_t amax[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) amax = max(amax, abs_bits(v[i]));
-        byte = mx_scale_byte(amax);
-        u32x4_t c;
+        for (int i = 0; i < 32; ++i) amax[0] = max(amax[0], abs_bits(v[i].x)), amax[1] = max(amax[1], abs_bits(v[i].y));
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float t[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
-            c[q] = mx_codes(t, byte);
+        for (int s = 0; s < 2; ++s) {
+            byte[s] = mx_scale_byte(amax[s]);
+            u32x4_t c;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float t[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] = s ? v[8 * q + i].y : v[8 * q + i].x;
+                c[q] = mx_codes(t, byte[s]);
+            }
+            tile[2 * lane + s][wave] = c;
         }
-        tile[lane][wave] = c;
     }
-    bytes[lane][wave] = (uint8_t)byte;
+    bytes[2 * lane][wave] = (uint8_t)byte[0], bytes[2 * lane + 1][wave] = (uint8_t)byte[1];
     __syncthreads();
-    const int m = col * 64 + (tid >> 3), b = slice * 8 + (tid & 7);
-    if (m < N && b < blocks) *reinterpret_cast<u32x4_t *>(codes + (e * N + m) * (size_t)(K / 2) + (size_t)b * 16) = tile[tid >> 3][tid & 7];
-    const int g = slice * 2 + wave;
-    if (wave < 2 && n < N && g < mx_groups(K))
-        *reinterpret_cast<uint32_t *>(scales + ((e * mx_groups(K) + g) * (size_t)N + n) * 4) = *reinterpret_cast<const uint32_t *>(&bytes[lane][4 * wave]);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int i = half * 64 + (tid >> 3), m = col * 128 + i, b = slice * 8 + (tid & 7);
+        if (m < N && b < blocks) *reinterpret_cast<u32x4_t *>(codes + (e * N + m) * (size_t)(K / 2) + (size_t)b * 16) = tile[i][tid & 7];
+    }
+    const int i = tid & 127, m = col * 128 + i, g = slice * 2 + (tid >> 7);
+    if (tid < 256 && m < N && g < mx_groups(K))
+        *reinterpret_cast<uint32_t *>(scales + ((e * mx_groups(K) + g) * (size_t)N + m) * 4) = *reinterpret_cast<const uint32_t *>(&bytes[i][4 * (tid >> 7)]);
 }
 
 template <int DT>
-__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, long rows, int per_matrix,
+__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int matrices, int rows,
                                                              int K, void *__restrict__ out)
 {
     const int part = threadIdx.x & 15, G = mx_groups(K);
-    const long row = (long)(blockIdx.x / G) * 16 + (threadIdx.x >> 4);
-    const int g = (int)(blockIdx.x % G), k = g * kMxGroup + part * 8;
-    if (row >= rows || k >= K) return;
-    const long m = row / per_matrix, n = row % per_matrix;
-    const uint32_t c = *reinterpret_cast<const uint32_t *>(codes + (size_t)row * (K / 2) + k / 2);
-    const uint32_t byte = scales[(((size_t)m * G + g) * per_matrix + n) * 4 + (part >> 2)];
-    const float s = mx_scale_value(byte);
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1),
-                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3)};
-    const size_t at = (size_t)row * K + k;
-    if constexpr (DT == MOE_F32) {
-        f32x4_t *q = reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(out) + at);
-        q[0] = f32x4_t{p[0][0] * s, p[0][1] * s, p[1][0] * s, p[1][1] * s};
-        q[1] = f32x4_t{p[2][0] * s, p[2][1] * s, p[3][0] * s, p[3][1] * s};
-    } else {
-        u32x4_t w;
+    const int n = (int)(blockIdx.x / G) * 16 + (threadIdx.x >> 4), g = (int)(blockIdx.x % G), k = g * kMxGroup + part * 8;
+    if (n >= rows || k >= K) return;
+    for (int m = blockIdx.y; m < matrices; m += gridDim.y) {      // (the same for all: no row's matrix has to be found by division)
+        const size_t row = (size_t)m * rows + n;
+        const uint32_t c = *reinterpret_cast<const uint32_t *>(codes + row * (K / 2) + k / 2);
+        const uint32_t byte = scales[(((size_t)m * G + g) * rows + n) * 4 + (part >> 2)];
+        const float s = mx_scale_value(byte);
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1),
+                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3)};
+        const size_t at = row * K + k;
+        if constexpr (DT == MOE_F32) {
+            f32x4_t *q = reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(out) + at);
+            q[0] = f32x4_t{p[0][0] * s, p[0][1] * s, p[1][0] * s, p[1][1] * s};
+            q[1] = f32x4_t{p[2][0] * s, p[2][1] * s, p[3][0] * s, p[3][1] * s};
+        } else {
+            u32x4_t w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float lo = p[i][0] * s, hi = p[i][1] * s;
-            if (DT == MOE_BF16) w[i] = (uint32_t)to_bf16_rne(lo) | ((uint32_t)to_bf16_rne(hi) << 16);
-            else w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16);
+            for (int i = 0; i < 4; ++i) {
+                const float lo = p[i][0] * s, hi = p[i][1] * s;
+                if (DT == MOE_BF16) w[i] = (uint32_t)to_bf16_rne(lo) | ((uint32_t)to_bf16_rne(hi) << 16);
+                else w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16);
+            }
+            *reinterpret_cast<u32x4_t *>(reinterpret_cast<uint16_t *>(out) + at) = w;
         }
-        *reinterpret_cast<u32x4_t *>(reinterpret_cast<uint16_t *>(out) + at) = w;
     }
 }
 
@@ -173,7 +182,7 @@ extern "C" int moe_mx4_quantize_experts(const float *w, int E, int K, int N, voi
     if (E == 0) return MOE_OK;
     if (!w || !codes || !scales) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(w) || !aligned16(codes) || !aligned16(scales)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
-    const double blocks = (double)E * ((K + 255) / 256) * ((N + 63) / 64);
+    const double blocks = (double)E * ((K + 255) / 256) * ((N + 127) / 128);
     if (2 * blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "%s: %.0f workgroups exceed one launch", what, blocks);
     hipLaunchKernelGGL(mx4_quantize_experts_kernel, dim3((unsigned)blocks), dim3(512), 0, as_stream(stream), w, K, N, (uint8_t *)codes, (uint8_t *)scales);
     return check_launch(what);
@@ -188,11 +197,12 @@ extern "C" int moe_mx4_dequantize(const void *codes, const void *scales, int mat
     if (matrices == 0 || rows == 0) return MOE_OK;
     if (!codes || !scales || !out) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(codes) || !aligned16(scales) || !aligned16(out)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
-    const long all = (long)matrices * rows;
-    const double blocks = (double)((all + 15) / 16) * mx_groups(K);
+    const double blocks = (double)((rows + 15) / 16) * mx_groups(K);
+    const int most = matrices < 0x8000 ? matrices : 0x8000;
     if (blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "%s: %.0f workgroups exceed one launch", what, blocks);
     auto run = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, as_stream(stream), (const uint8_t *)codes, (const uint8_t *)scales, all, rows, K, out);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)most), dim3(256), 0, as_stream(stream), (const uint8_t *)codes, (const uint8_t *)scales, matrices,
+                           rows, K, out);
     };
     if (out_dtype == MOE_F16) run(&mx4_dequantize_kernel<MOE_F16>);
     else if (out_dtype == MOE_BF16) run(&mx4_dequantize_kernel<MOE_BF16>);

@@ -195,11 +195,13 @@ static int launch_stream(const MxArgs &p, hipStream_t s)
     return check_launch("moe_grouped_gemm_mx4");
 }
 
-// Wavefronts and slabs of a block (kernel times, 4 KB of LDS per wavefront and slab; what counts is how many bytes a compute unit has in flight, so small blocks,
-// and how often a block's chain of index and rows is paid for, so not too small ones):
-//  - K up to 1024: four wavefronts, one slab (64 tokens, two of 32 experts, 1024 x 4096: 16.7 us, two slabs 16.8, four 18.1; 40 tokens, one each, 12.4 / 13.2 / 13.7);
-//  - longer K: eight wavefronts, two slabs where that makes two blocks per compute unit (4096 x 16384, 64 experts, 64 tokens: 285 us = 6.9 TB/s, one slab 311, 64 KB
-//    per four wavefronts 433; 2048 x 8192, 32 experts: 57 and 64), else one (16 tokens, fc2 of 4096 x 1024: 10.1 and 12.0).
+// Wavefronts, slabs and lines per wavefront of a block (kernel times in us, 4 KB of LDS for each of the three; what counts is how many bytes a compute unit has in
+// flight, so small blocks, and how often a block's chain of index and rows is paid for, so not too small ones):
+//  - few blocks: one slab, and K in as few rounds as wavefronts allow (16 tokens, two of 32 experts, fc2 of 4096 x 1024: eight wavefronts 10.3, four with two slabs 11.7);
+//  - K up to 1024: four wavefronts, one slab (64 tokens, two of 32 experts, 1024 x 4096: 16.7, two slabs 16.8, four 18.1; 40 tokens, one each, 12.4 / 13.2 / 13.7);
+//  - K up to 4096 and many blocks: two wavefronts with two slabs and two lines (64 tokens, two of 32 experts, 2048 x 8192: 48.9 = 5.7 TB/s, eight wavefronts 59.5;
+//    of 64 experts of 4096 x 16384 281 and 285 to 329); fewer: four wavefronts, two slabs (64 tokens, 4096 x 1024: 13.4, eight wavefronts 14.2);
+//  - longer K: eight wavefronts, two slabs (8192 x 2048: 46.6 = 6.0 TB/s, two wavefronts 58.1; 16384 x 4096 286 and 291).
 // Row tiles from 25 rows per expert on (us, streaming / tiles: 384 tokens, two of 32 experts of 1024 x 4096, 24 rows, fc1 21.3 / 19.1, fc2 20.7 / 19.8, of 2048 x 8192 65 / 64
 // and 59 / 69; 32 rows 27.7 / 19.7 and 22.4 / 20.5; 16 rows 20.4 / 18.7 and 16.9 / 20.1).
 static bool streams(int R, int E) { return (R + E - 1) / E <= 24; }
@@ -207,8 +209,11 @@ static bool streams(int R, int E) { return (R + E - 1) / E <= 24; }
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
 {
     if (!streams(p.R, p.E)) return launch_mx4_tiled(p, s);
+    const double blocks = decode_active_experts(p.R, p.E) * (p.N / 64);
     if (p.K <= 1024) return launch_stream<4, 1, 1>(p, s);
-    return decode_active_experts(p.R, p.E) * (p.N / 64) >= 450 ? launch_stream<8, 2, 1>(p, s) : launch_stream<8, 1, 1>(p, s);
+    if (blocks < 450) return launch_stream<8, 1, 1>(p, s);
+    if (p.K > 4096) return launch_stream<8, 2, 1>(p, s);
+    return blocks >= 2048 ? launch_stream<2, 2, 2>(p, s) : launch_stream<4, 2, 1>(p, s);
 }
 
 // Whether fc1 quantises its rows for itself: every block does so for the rows of its item, so only where there are few blocks.
