@@ -8,9 +8,16 @@ static int check_product(const char *what, int R, int E, int a_rows, int K, int 
     if (R < 0 || E < 0 || a_rows < 0 || K <= 0 || N <= 0 || K % 64 || N % 32)
         return fail(MOE_ERR_INVALID_ARG, "%s: need R, E and rows >= 0, K %% 64 == 0, N %% 32 == 0 (R=%d E=%d rows=%d K=%d N=%d)", what, R, E, a_rows, K, N);
     if (perm_src ? k < 1 : a_rows < R) return fail(MOE_ERR_INVALID_ARG, "%s: without perm_src there are as many rows as R, with it k >= 1", what);
+    if (K > 1 << 24 || N > 1 << 24) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d or N = %d above 2^24", what, K, N);      // (what a lane's 32-bit offsets reach)
     if (a_rows > 0x3fffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are more than 2^30", what, a_rows);
     if (E > 4096) return fail(MOE_ERR_UNSUPPORTED, "%s: E = %d above 4096", what, E);
     return MOE_OK;
+}
+
+// Rows that there can be: R, or less where the caller bounds every expert's.
+static int most_rows(int R, int E, int max_rows_per_expert)
+{
+    return max_rows_per_expert && (long)E * max_rows_per_expert < R ? E * max_rows_per_expert : R;
 }
 
 }  // namespace moe
@@ -32,7 +39,7 @@ extern "C" int moe_grouped_gemm_mx4(const void *a_codes, const void *a_scales, i
     MxArgs p{};
     p.a = (const uint8_t *)a_codes, p.as = (const uint8_t *)a_scales, p.a_rows = a_rows, p.a_src = perm_src, p.a_div = k;
     p.offsets = expert_offsets, p.w = (const uint8_t *)w_codes, p.ws = (const uint8_t *)w_scales, p.bias = (const __half *)bias;
-    p.out = y, p.E = E, p.R = R, p.K = K, p.N = N, p.out_dtype = y_dtype, p.act = activation;
+    p.out = y, p.E = E, p.R = R, p.most = most_rows(R, E, max_rows_per_expert), p.K = K, p.N = N, p.out_dtype = y_dtype, p.act = activation;
     return launch_mx4_gemm(p, as_stream(stream));
 }
 
@@ -65,7 +72,8 @@ extern "C" int moe_grouped_ffn_mx4(const void *x, int act_dtype, int T, const in
     uint8_t *xq = (uint8_t *)workspace, *xs = xq + round_up(mx_code_bytes(T, d), 256);
     uint8_t *hq = xs + round_up(mx_scale_bytes(T, d), 256), *hs = hq + round_up(mx_code_bytes(R, F), 256);
     MxArgs p{};
-    if (mx4_fuses_rows(R, E, F, act_dtype)) p.x = x, p.x_dtype = act_dtype;
+    p.most = most_rows(R, E, max_rows_per_expert);
+    if (mx4_fuses_rows(p.most, E, F, act_dtype)) p.x = x, p.x_dtype = act_dtype;
     else if (int rc = launch_mx4_quantize_rows(x, act_dtype, T, d, d, xq, xs, s)) return rc;
     p.a = xq, p.as = xs, p.a_rows = T, p.a_src = perm_src, p.a_div = k, p.offsets = expert_offsets;
     p.w = (const uint8_t *)w1_codes, p.ws = (const uint8_t *)w1_scales, p.bias = (const __half *)b1;

@@ -68,11 +68,12 @@ struct MxArgs {
     void *out;                // [R, N] in out_dtype, or, with out_scales, codes [R, N/2]
     uint8_t *out_scales;      // [ceil(N/128), R, 4] or null
     int E, R, K, N;
+    int most;                 // rows to choose a kernel for: R, or fewer if the caller knows
     int out_dtype, act;
 };
 
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s);
-bool mx4_fuses_rows(int R, int E, int N, int x_dtype);
+bool mx4_fuses_rows(int most, int E, int N, int x_dtype);
 int launch_mx4_tiled(const MxArgs &p, hipStream_t s);
 int launch_mx4_quantize_rows(const void *x, int dtype, int R, int K, long stride, uint8_t *codes, uint8_t *scales, hipStream_t s);
 

@@ -186,9 +186,11 @@ static int launch_stream(const MxArgs &p, hipStream_t s)
     static_assert(S::kLds <= 64 * 1024, "what a launch may ask for without more");
     using std::integral_constant;
     constexpr integral_constant<int, -1> codes{};
-    if (p.x && p.x_dtype == MOE_F16) run(codes, integral_constant<int, MOE_F16>{});
-    else if (p.x) run(codes, integral_constant<int, MOE_BF16>{});
-    else if (p.out_scales) run(codes, codes);
+    if constexpr (NS == 1) {                             // (mx4_fuses_rows: of few blocks, which are those of one slab)
+        if (p.x && p.x_dtype == MOE_F16) return run(codes, integral_constant<int, MOE_F16>{}), check_launch("moe_grouped_ffn_mx4");
+        if (p.x) return run(codes, integral_constant<int, MOE_BF16>{}), check_launch("moe_grouped_ffn_mx4");
+    } else if (p.x) return fail(MOE_ERR_UNSUPPORTED, "moe_grouped_ffn_mx4: rows that are not quantised, for %d slabs", NS);
+    if (p.out_scales) run(codes, codes);
     else if (p.out_dtype == MOE_F16) run(integral_constant<int, MOE_F16>{}, codes);
     else if (p.out_dtype == MOE_BF16) run(integral_constant<int, MOE_BF16>{}, codes);
     else run(integral_constant<int, MOE_F32>{}, codes);
@@ -204,12 +206,12 @@ static int launch_stream(const MxArgs &p, hipStream_t s)
 //  - longer K: eight wavefronts, two slabs (8192 x 2048: 46.6 = 6.0 TB/s, two wavefronts 58.1; 16384 x 4096 286 and 291).
 // Row tiles from 25 rows per expert on (us, streaming / tiles: 384 tokens, two of 32 experts of 1024 x 4096, 24 rows, fc1 21.3 / 19.1, fc2 20.7 / 19.8, of 2048 x 8192 65 / 64
 // and 59 / 69; 32 rows 27.7 / 19.7 and 22.4 / 20.5; 16 rows 20.4 / 18.7 and 16.9 / 20.1).
-static bool streams(int R, int E) { return (R + E - 1) / E <= 24; }
+static bool streams(int most, int E) { return ((long)most + E - 1) / E <= 24; }
 
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
 {
-    if (!streams(p.R, p.E)) return launch_mx4_tiled(p, s);
-    const double blocks = decode_active_experts(p.R, p.E) * (p.N / 64);
+    if (!streams(p.most, p.E)) return launch_mx4_tiled(p, s);
+    const double blocks = decode_active_experts(p.most, p.E) * (p.N / 64);
     if (p.K <= 1024) return launch_stream<4, 1, 1>(p, s);
     if (blocks < 450) return launch_stream<8, 1, 1>(p, s);
     if (p.K > 4096) return launch_stream<8, 2, 1>(p, s);
@@ -217,9 +219,9 @@ int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
 }
 
 // Whether fc1 quantises its rows for itself: every block does so for the rows of its item, so only where there are few blocks.
-bool mx4_fuses_rows(int R, int E, int N, int x_dtype)
+bool mx4_fuses_rows(int most, int E, int N, int x_dtype)
 {
-    return x_dtype != MOE_F32 && streams(R, E) && decode_active_experts(R, E) * (N / 32) <= 512;
+    return x_dtype != MOE_F32 && streams(most, E) && decode_active_experts(most, E) * (N / 32) <= 512;
 }
 
 }  // namespace moe

@@ -205,7 +205,7 @@ static int launch_tile(const MxArgs &p, hipStream_t s)
 // left to large ones 1600, two of 32, 1024 x 4096: 25.5, small 32.4).
 int launch_mx4_tiled(const MxArgs &p, hipStream_t s)
 {
-    return expected_row_tiles(p.R, p.E, 128) * ((p.N + 255) / 256) <= 384 ? launch_tile<2, 2, 1, 2, 3>(p, s) : launch_tile<1, 4, 4, 2, 3>(p, s);
+    return expected_row_tiles(p.most, p.E, 128) * ((p.N + 255) / 256) <= 384 ? launch_tile<2, 2, 1, 2, 3>(p, s) : launch_tile<1, 4, 4, 2, 3>(p, s);
 }
 
 }  // namespace moe

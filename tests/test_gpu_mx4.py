@@ -104,7 +104,7 @@ def experts_of(rng, E, K, N):
 # rows per expert: one, none, odd numbers, the edges of 16, 32, 64, 128 and 256 rows, everything in one expert
 LOADS = {"one": [0, 1], "few": [3, 0, 0, 7, 1, 0], "edges": [15, 16, 17, 31, 32, 33], "tiles": [63, 65, 0, 64, 127, 129], "tall": [0, 255, 257], "lone": [700],
          "many": [1] * 70 + [0] * 7 + [2, 5]}
-
+FFN_LOADS = dict(LOADS, large=[700, 1, 645, 830])
 
 @pytest.mark.parametrize("load", LOADS)
 @pytest.mark.parametrize("K,N,out,bias,act", [(64, 32, "f32", False, None), (192, 96, "f16", True, "relu"), (1024, 256, "f32", True, None), (2880, 320, "bf16", False, "gelu"),
@@ -133,6 +133,52 @@ def check_rows(got, want, size, K, out, act):
     # error on at most 1.13 times and GELU adds 4e-7 |v| of its own; the result is rounded once
     tol = 1.13 * (K / 64 + 9) * 2.0 ** -23 * size + (4e-7 * (np.abs(want) + size) if act == "gelu" else 0)
     assert (np.abs(got - want) <= tol + ROUND[out] * (np.abs(want) + tol) + TINY[out]).all(), np.abs(got - want).max()
+
+
+def repeated_experts(rng, E, K, N, different=2):
+    """E experts of `different` kinds (codes at random, so cheap to make in 64 bits): codes, scales, and the values of each kind."""
+    codes = rng.integers(0, 256, (different, N, K // 2)).astype(np.uint8)
+    scales = rng.integers(118, 123, (different, -(-K // 128), N, 4)).astype(np.uint8)
+    kind = np.arange(E) % different
+    return codes[kind], scales[kind], [mx4.dequantize(codes[i], scales[i]) for i in kind[:different]]
+
+
+# every shape of block, by what leads to it
+SHAPES = {"large tiles": (320, 5536, [700, 1, 645, 830]), "large tiles, one odd half group": (192, 5472, [609, 33, 97, 1000, 545]),      # (rows of the last tile: one to four times 32)
+          "small tiles": (1088, 416, [130, 255, 64, 1]), "streamed, one slab, short K": (960, 1056, [1, 3, 0, 2] * 9),
+          "streamed, one slab": (1216, 288, [2, 1, 0, 9]), "streamed, two slabs": (2112, 1056, [1, 2, 1, 1] * 10), "streamed, two lines each": (1088, 2080, [3, 1] * 40),
+          "streamed, long K": (4160, 1056, [1, 2, 1, 1, 33] * 8)}
+
+
+@pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_shapes_of_blocks(shape, out):
+    K, N, rows = SHAPES[shape]
+    print(f"mx4 product {shape} K={K} N={N} {out}", flush=True)
+    rng = np.random.default_rng(K)
+    E, off = len(rows), np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    a, w = held(rng, int(off[-1]), K), repeated_experts(rng, E, K, N)
+    src = rng.permutation(int(off[-1])).astype(np.int32)
+    y = B.moe_grouped_gemm_mx4(*[to_dev(t, torch.uint8) for t in a[:2]], to_dev(off, torch.int32), *[to_dev(t, torch.uint8) for t in w[:2]], perm_src=to_dev(src, torch.int32),
+                               y_dtype=DT[out])
+    got, v = host(y.double()), a[2][src]
+    for e in range(E):
+        r = slice(off[e], off[e + 1])
+        check_rows(got[r], v[r] @ w[2][e % 2].T, np.abs(v[r]) @ np.abs(w[2][e % 2]).T, K, out, None)
+
+
+def test_a_bound_on_the_rows_of_an_expert_only_chooses():
+    """A buffer of many rows of which few are in use: with and without the caller's bound on them, and with one that does not hold, the same product."""
+    rng = np.random.default_rng(8)
+    off = np.array([0, 3, 5, 41], dtype=np.int32)
+    a, w = held(rng, 200, 576), experts_of(rng, 3, 576, 96)
+    args = [to_dev(t, torch.uint8) for t in a[:2]] + [to_dev(off, torch.int32)] + [to_dev(t, torch.uint8) for t in w[:2]]
+    want, size = mx4.product(a[2], off, w[2])
+    for most in (0, 1, 36, 200, 2 ** 31 - 1):
+        y = torch.full((200, 96), -77.0, device="cuda:0")
+        got = host(B.moe_grouped_gemm_mx4(*args, y=y, max_rows_per_expert=most).double())
+        assert (got[41:] == -77.0).all()
+        check_rows(got[:41], want[:41], size[:41], 576, "f32", None)
 
 
 def test_product_without_an_index_and_its_repeats():
@@ -216,14 +262,14 @@ def ffn_with_bounds(x, off, src, w1, w2, b1, b2, act):
 
 
 FFN = [("few", 64, 64, "f16", False, "relu"), ("edges", 192, 320, "bf16", True, "relu"), ("tiles", 704, 576, "f16", True, "gelu"), ("tall", 256, 1024, "f32", False, "relu"),
-       ("lone", 128, 192, "bf16", True, "gelu"), ("one", 1024, 4096, "f16", False, "relu"), ("many", 512, 256, "f16", True, "relu")]
+       ("lone", 128, 192, "bf16", True, "gelu"), ("one", 1024, 4096, "f16", False, "relu"), ("many", 512, 256, "f16", True, "relu"), ("large", 192, 5568, "bf16", True, "relu")]
 
 
 @pytest.mark.parametrize("load,d,F,dtype,bias,act", FFN)
 def test_ffn(load, d, F, dtype, bias, act):
     print(f"mx4 ffn {load} d={d} F={F} {dtype} bias={bias} {act}", flush=True)
     rng = np.random.default_rng(d + F)
-    rows, k = LOADS[load], 2
+    rows, k = FFN_LOADS[load], 2
     E = len(rows)
     off = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
     R = int(off[-1]) + 1                                                            # the last row belongs to a pruned token

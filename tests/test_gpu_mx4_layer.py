@@ -82,15 +82,16 @@ def test_counted_waits_against_waits_for_everything():
     other.moe_grouped_gemm_mx4.argtypes = B.load().moe_grouped_gemm_mx4.argtypes
     gen = torch.Generator(device="cuda")
     gen.manual_seed(1)
-    for rows, K, N in (([3, 0, 17, 32], 704, 96), ([40, 100, 0, 65], 192, 320), ([130, 255, 64, 1], 1088, 352), ([300] * 4, 512, 8192), ([513, 20, 260, 999], 2880, 1056)):
+    for rows, K, N in (([3, 0, 17, 32], 704, 96), ([40, 100, 0, 65], 192, 320), ([130, 255, 64, 1], 1088, 352), ([300] * 4, 512, 8192), ([513, 20, 260, 999], 2880, 1056),
+                       ([700, 1, 645, 830], 320, 5536), ([2, 1, 9, 0], 1216, 288), ([3, 1, 2, 1] * 10, 2112, 1056), ([3, 1] * 40, 1088, 2080), ([1, 2, 1, 40] * 10, 4160, 1056)):
         print(f"waits {rows} K={K} N={N}", flush=True)
         off = torch.tensor([0] + list(np.cumsum(rows)), dtype=torch.int32, device="cuda")
         R = int(off[-1])
         a = B.moe_mx4_quantize_rows(torch.randn((R, K), generator=gen, device="cuda"))
-        w = B.moe_mx4_quantize_experts(torch.randn((4, K, N), generator=gen, device="cuda"))
+        w = B.moe_mx4_quantize_experts(torch.randn((len(rows), K, N), generator=gen, device="cuda"))
         y = B.moe_grouped_gemm_mx4(*a, off, *w, y_dtype=torch.float32)
         z = torch.empty_like(y)
         p = lambda t: t.data_ptr()  # noqa: E731
-        rc = other.moe_grouped_gemm_mx4(p(a[0]), p(a[1]), R, None, 1, p(off), R, 4, 0, K, N, p(w[0]), p(w[1]), None, -1, p(z), B.MOE_F32, B.current_stream_handle())
+        rc = other.moe_grouped_gemm_mx4(p(a[0]), p(a[1]), R, None, 1, p(off), R, len(rows), 0, K, N, p(w[0]), p(w[1]), None, -1, p(z), B.MOE_F32, B.current_stream_handle())
         torch.cuda.synchronize()
         assert rc == 0 and torch.equal(y, z)

@@ -32,7 +32,7 @@ def test_products_refuse(lib):
     for bad in (dict(K=32), dict(K=96), dict(N=16), dict(N=48), dict(R=-1), dict(k=0), dict(src=None, rows=7), dict(a=None), dict(y=None), dict(off=None), dict(w=ODD), dict(bias=ODD),
                 dict(most=-1)):
         assert gemm(**bad) == ARG, bad
-    for bad in (dict(dt=3), dict(act=2), dict(act=-2), dict(E=4097)):
+    for bad in (dict(dt=3), dict(act=2), dict(act=-2), dict(E=4097), dict(K=(1 << 24) + 64), dict(N=(1 << 24) + 32)):
         assert gemm(**bad) == UNSUPPORTED, bad
     assert gemm(R=0) == 0 and gemm(E=0) == 0
     ffn = lambda x=P, dt=0, T=8, R=8, d=64, F=64, act=0, y=P, ydt=0, ws=P, size=1 << 30, b1=None: lib.moe_grouped_ffn_mx4(  # noqa: E731
