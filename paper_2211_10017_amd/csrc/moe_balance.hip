@@ -7,7 +7,8 @@
 // Both directions are bound by reading the logits (and the backward by writing their gradient), small batches by their launches.  A token's logits are
 // spread over L lanes of a wavefront, V neighbouring ones per lane and step, so that a lane keeps the sums of its own experts in registers over all
 // of its tokens; a block's sums meet in LDS and the blocks' in a second launch, in the order of the blocks: no floating-point atomics, the same bits
-// every time.  (A launch of one block does without.)
+// every time.  (A launch of one block does without.)  131072 tokens by 256 experts, two each, fp32: forward 40 us = 3.4 TB/s (its exponentials and
+// reductions are as long as its loads), the blocks' sums 10 us, backward 51 us = 5.3 TB/s.
 #include <math.h>
 
 #include <type_traits>
@@ -43,7 +44,7 @@ __device__ inline float to_f32(uint32_t bits)
 }
 
 // FULL: the lanes and steps of a token hold its E logits and nothing besides, as they do for powers of two from eight on.  KM: the most experts of a token (with eight
-// for all, a token's scalar work is most of it: 131072 tokens by 256 experts, two each, forward 43 us).
+// for all, a token's scalar work is most of it: 131072 tokens by 256 experts, two each, forward 43 us instead of 40).
 // What a lane holds of a token: V neighbouring logits in each of S steps, as they lie in memory, the token's experts, their logits and the gradients of their
 // scales.  Requested one token ahead, the experts, which the others' addresses depend on, two.
 template <int DT, int V, int S, bool FULL, int KM>

@@ -41,7 +41,7 @@ __device__ inline uint32_t sixteen_lane_scales(uint32_t amax, uint32_t &byte)
 }
 
 // Rows: a wavefront takes four rows by 128 values at a time, sixteen lanes a row, so that loads are whole lines and the scales of a block's
-// sixteen rows one 64-byte piece.  Memory-bound: reads K values of a row once, writes 17/32 byte each.
+// sixteen rows one 64-byte piece.  Memory-bound: reads K values of a row once, writes 17/32 byte each (16384 rows of 4096, bf16: 34 us = 5.0 TB/s, what a copy reaches).
 template <int DT>
 __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const void *__restrict__ x, int R, int K, long stride, int per,
                                                                 uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
@@ -112,6 +112,7 @@ __global__ __launch_bounds__(512) void mx4_quantize_experts_kernel(const float *
         *reinterpret_cast<uint32_t *>(scales + ((e * mx_groups(K) + g) * (size_t)N + m) * 4) = *reinterpret_cast<const uint32_t *>(&bytes[i][4 * (tid >> 7)]);
 }
 
+// Codes times scales: eight values a lane, a row's 128 values in sixteen neighbouring lanes.  Memory-bound by what it writes (16384 rows of 4096 to bf16: 30 us = 5.7 TB/s).
 template <int DT>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int matrices, int rows,
                                                              int K, void *__restrict__ out)
