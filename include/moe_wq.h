@@ -408,6 +408,7 @@ int moe_grouped_ffn_mx4(const void *x, int act_dtype, int T, const int32_t *perm
  * an assignment and P_e the mean of p_te over those tokens:
  *   loss = coef * E * sum_e (c_e / A) P_e
  *   expert_scale[t,j] = p[t, expert_idx[t,j]], divided by the sum over the token's k when renormalize != 0 and k > 1
+ *     (then taken from the logits of the token's k alone: right also where every p[t, expert_idx[t,j]] is 0 in fp32)
  * An entry of expert_idx outside [0, E) (the gate's E marks a pruned row) is no assignment: counted nowhere, scale 0, no gradient; a token without one
  * takes no part.  No assignments at all: loss 0.
  *   logits [T,E] dtype; expert_idx [T,k]; loss [1] fp32, counts [E] int32, prob_mean [E] fp32 (P), expert_scale [T,k] fp32,

@@ -7,8 +7,8 @@
 // Both directions are bound by reading the logits (and the backward by writing their gradient), small batches by their launches.  A token's logits are
 // spread over L lanes of a wavefront, V neighbouring ones per lane and step, so that a lane keeps the sums of its own experts in registers over all
 // of its tokens; a block's sums meet in LDS and the blocks' in a second launch, in the order of the blocks: no floating-point atomics, the same bits
-// every time.  (A launch of one block does without.)  131072 tokens by 256 experts, two each, fp32: forward 40 us = 3.4 TB/s (its exponentials and
-// reductions are as long as its loads), the blocks' sums 10 us, backward 51 us = 5.3 TB/s.
+// every time.  (A launch of one block does without.)  131072 tokens by 256 experts, two each, fp32: forward 42 us = 3.2 TB/s (its exponentials and
+// reductions are as long as its loads), the blocks' sums 9.5 us, backward 53 us = 5.1 TB/s.
 #include <math.h>
 
 #include <type_traits>
@@ -44,7 +44,7 @@ __device__ inline float to_f32(uint32_t bits)
 }
 
 // FULL: the lanes and steps of a token hold its E logits and nothing besides, as they do for powers of two from eight on.  KM: the most experts of a token (with eight
-// for all, a token's scalar work is most of it: 131072 tokens by 256 experts, two each, forward 43 us instead of 40).
+// for all, a token's scalar work is most of it: 131072 tokens by 256 experts, two each, 4 us more of the forward pass).
 // What a lane holds of a token: V neighbouring logits in each of S steps, as they lie in memory, the token's experts, their logits and the gradients of their
 // scales.  Requested one token ahead, the experts, which the others' addresses depend on, two.
 template <int DT, int V, int S, bool FULL, int KM>
@@ -151,6 +151,36 @@ __device__ inline void token_softmax(const BalanceArgs &a, const TokenLoad<DT, V
     inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 }
 
+// Gate scales of a token's experts: their p, or, renormalised, a softmax over them alone.  That one starts from the largest logit among them, not among all: the p of experts far
+// below a token's best are 0 in 32 bits, their shares of each other are not.  Whether the token has an expert at all.
+template <int DT, int V, int S, bool FULL, int KM>
+__device__ inline bool gate_scales(const BalanceArgs &a, const TokenLoad<DT, V, S, FULL, KM> &x, bool renorm, float base, float inv, float (&scale)[KM])
+{
+    float from = base, total = 0.0f;
+    bool live = false;
+    if (renorm) {
+        from = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < KM; ++j)
+            if (j < a.k && x.used(a, j)) from = fmaxf(from, to_f32<DT>(x.chosen[j]));
+        if (from == -INFINITY) from = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < KM; ++j) {
+        if (j >= a.k) break;
+        const bool used = x.used(a, j);
+        scale[j] = used ? exp_of(to_f32<DT>(x.chosen[j]) - from) : 0.0f;
+        total += scale[j];
+        live |= used;
+    }
+    // (inv - inv: 0, or the NaN of a token that holds one)
+    const float factor = !renorm ? inv : (total == 0.0f ? 0.0f : 1.0f / total) + (inv - inv);
+#pragma unroll
+    for (int j = 0; j < KM; ++j)
+        if (j < a.k) scale[j] = x.used(a, j) ? scale[j] * factor : 0.0f;
+    return live;
+}
+
 // The tokens of a thread's L lanes, one after the other, the next one's loads ahead of the work on this one: f(token, whether it is there, loads).
 // (Two tokens a turn, so that what is loaded need not be moved, which would wait for it.)
 template <int DT, int V, int S, bool FULL, int KM, class F>
@@ -219,25 +249,19 @@ __global__ __launch_bounds__(kBalanceThreads) void balance_forward_kernel(Balanc
     for (int i = tid; i <= a.E; i += blockDim.x) cnt[i] = 0;
     __syncthreads();
     float acc[S][V] = {};
+    const bool renorm = a.renorm && a.k > 1;
     for_tokens<DT, V, S, FULL, KM>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL, KM> &x) {
-        float chosen[KM], total = 0.0f, base, inv, p[S][V];
+        float scale[KM], base, inv, p[S][V];
         token_softmax<DT, V, S, FULL, KM>(a, x, lane_in, p, base, inv);
-        bool live = false;
-#pragma unroll
-        for (int j = 0; j < KM; ++j) {
-            if (j >= a.k) break;
-            const bool used = x.used(a, j);
-            chosen[j] = used ? exp_of(to_f32<DT>(x.chosen[j]) - base) * inv : 0.0f;
-            total += chosen[j];
-            live |= used;
-            if (here && used && lane_in == 0) atomicAdd(&cnt[x.e[j]], 1);
-        }
-        if (here && live && lane_in == 0) atomicAdd(&cnt[a.E], 1);
-        const float norm = a.renorm && a.k > 1 && total != 0.0f ? 1.0f / total : 1.0f;
+        const bool live = gate_scales<DT, V, S, FULL, KM>(a, x, renorm, base, inv, scale);
         if (here && lane_in == 0) {
+            if (live) atomicAdd(&cnt[a.E], 1);
 #pragma unroll
-            for (int j = 0; j < KM; ++j)
-                if (j < a.k) a.scale[(size_t)t * a.k + j] = chosen[j] * norm;
+            for (int j = 0; j < KM; ++j) {
+                if (j >= a.k) break;
+                if (x.used(a, j)) atomicAdd(&cnt[x.e[j]], 1);
+                a.scale[(size_t)t * a.k + j] = scale[j];
+            }
         }
         if (__all(here && live)) {
 #pragma unroll
@@ -347,24 +371,14 @@ __global__ __launch_bounds__(kBalanceThreads) void balance_backward_kernel(Balan
         }
     const bool renorm = a.renorm && a.k > 1;
     for_tokens<DT, V, S, FULL, KM>(a, lane_in, [&](int t, bool here, const TokenLoad<DT, V, S, FULL, KM> &x) {
-        float sc[KM], ds[KM], total = 0.0f, base, inv, p[S][V];
+        float sc[KM], ds[KM], base, inv, p[S][V];
         token_softmax<DT, V, S, FULL, KM>(a, x, lane_in, p, base, inv);
-        bool live = false;
-#pragma unroll
-        for (int j = 0; j < KM; ++j) {
-            if (j >= a.k) break;
-            const bool used = x.used(a, j);
-            sc[j] = used ? exp_of(to_f32<DT>(x.chosen[j]) - base) * inv : 0.0f;
-            ds[j] = used && a.dscale ? x.ds[j] : 0.0f;
-            total += sc[j];
-            live |= used;
-        }
-        const float norm = renorm && total != 0.0f ? 1.0f / total : 1.0f;
+        const bool live = gate_scales<DT, V, S, FULL, KM>(a, x, renorm, base, inv, sc);
         float mean = 0.0f;                                    // sum_j s_j ds_j
 #pragma unroll
         for (int j = 0; j < KM; ++j) {
             if (j >= a.k) break;
-            sc[j] *= norm;
+            ds[j] = x.used(a, j) && a.dscale ? x.ds[j] : 0.0f;
             mean += sc[j] * ds[j];
         }
         // Renormalised scales are a softmax over the chosen experts: s_j (ds_j - sum_i s_i ds_i), which, as the s_i add up to one, is

@@ -97,6 +97,28 @@ def test_masked_logits(dtype):
     assert not host(scale)[5].any() and not grad[5].any() and not np.delete(grad, [6, 7], axis=0)[:, 15:].any()
 
 
+@pytest.mark.parametrize("k", [2, 3, 8])
+def test_experts_far_below_the_best(k):
+    """Tokens sent past their best expert, to some whose probability is nothing in 32 bits: the renormalised scales are shares of each other all the same."""
+    z, idx, ds = inputs(64, 40, k, 6, pruned=0.1)
+    z[::2, 39] = 300.0
+    z[1::2, 38] = 90.0
+    idx = np.where(idx == 39, 3, np.where(idx == 38, 4, idx)).astype(np.int32)
+    zt, it = to_dev(z, torch.float32), to_dev(idx, torch.int32)
+    for renorm in (True, False):
+        want = mx4.balance(z, idx, 0.01, renorm, 1.0, ds)
+        loss, _, _, scale, weight = B.moe_balance_loss(zt, it, 0.01, renorm)
+        grad = host(B.moe_balance_loss_backward(zt, it, weight, loss.new_ones(()), to_dev(ds, torch.float32), renorm).double())
+        np.testing.assert_allclose(host(scale), want["scale"], rtol=2 * REL, atol=1e-30)
+        # (the p of these experts do not carry what the shares' differences may cancel, so it is added: s_j sum_i s_i |ds_j - ds_i|)
+        size, s = want["size"].copy(), want["scale"]
+        used = idx < 40
+        for j in range(k if renorm else 0):
+            terms = np.where(used, s * np.abs(ds[:, j:j + 1] - ds), 0.0).sum(axis=1) * s[:, j]
+            np.add.at(size, (np.arange(64)[used[:, j]], idx[used[:, j], j]), terms[used[:, j]])
+        assert (np.abs(grad - want["dlogits"]) <= 4 * REL * size + ROUND["f32"] * np.abs(want["dlogits"]) + 1e-30).all()
+
+
 def test_numbers_that_are_none_stay_in_their_token():
     z, idx, ds = inputs(200, 32, 2, 4, pruned=0.0)
     z[17, 3] = np.nan
