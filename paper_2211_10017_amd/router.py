@@ -11,7 +11,8 @@ class _BalanceLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, expert_idx, coef, renormalize):
         loss, counts, prob_mean, scale, weight = B.moe_balance_loss(logits, expert_idx, coef, renormalize)
-        ctx.save_for_backward(logits, expert_idx, weight)
+        # (a copy of the index: a layer routes the next batch into the same buffer, through a pointer that torch's version counter does not see)
+        ctx.save_for_backward(logits, expert_idx.clone(), weight)
         ctx.renormalize = renormalize
         ctx.mark_non_differentiable(counts, prob_mean)
         ctx.set_materialize_grads(False)
@@ -29,5 +30,6 @@ class _BalanceLoss(torch.autograd.Function):
 
 def balance_loss(logits, expert_idx, coef: float = 0.01, renormalize: bool = True):
     """logits [T, E] (fp16, bf16 or fp32, contiguous), expert_idx int32 [T, k] as moe_gate_topk gives it (E: a pruned row)
-    -> (expert_scale [T, k], loss [], counts int32 [E], prob_mean [E]); expert_scale and loss carry gradients."""
+    -> (expert_scale [T, k], loss [], counts int32 [E], prob_mean [E]); expert_scale and loss carry gradients.
+    expert_idx may be written again before the backward pass; logits may not (torch raises)."""
     return _BalanceLoss.apply(logits, expert_idx, coef, renormalize)
