@@ -24,8 +24,21 @@ class _BalanceLoss(torch.autograd.Function):
         if dscale is None and dloss is None:
             return None, None, None, None
         dscale = None if dscale is None else dscale.contiguous()
-        dlogits = B.moe_balance_loss_backward(logits, expert_idx, weight, dloss, dscale, ctx.renormalize)
-        return dlogits, None, None, None
+        gradient = _Gradient.apply if torch.is_grad_enabled() else B.moe_balance_loss_backward
+        return gradient(logits, expert_idx, weight, dloss, dscale, ctx.renormalize), None, None, None
+
+
+class _Gradient(torch.autograd.Function):
+    """The gradient where a graph of it is asked for: a second derivative is refused, not left out.  (torch's once_differentiable refuses only where the
+    gradients that come in have a graph of their own; that of logits alone it drops.)"""
+
+    @staticmethod
+    def forward(ctx, logits, expert_idx, weight, dloss, dscale, renormalize):
+        return B.moe_balance_loss_backward(logits, expert_idx, weight, dloss, dscale, renormalize)
+
+    @staticmethod
+    def backward(ctx, _ddlogits):
+        raise B.MoeError("balance_loss has no second derivative")
 
 
 def balance_loss(logits, expert_idx, coef: float = 0.01, renormalize: bool = True):

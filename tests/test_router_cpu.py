@@ -55,3 +55,25 @@ def test_gradient_of_a_batch_whose_index_buffer_is_written_again(library, renorm
     balance_loss(torch.from_numpy(z1).requires_grad_(), buffer, 0.3, renorm)
     (2.0 * loss + (scale * torch.from_numpy(up0)).sum()).backward()
     close(logits.grad, mx4.balance(z0, i0, 0.3, renorm, 2.0, up0)["dlogits"])
+
+
+@pytest.mark.parametrize("of", ["loss", "scale"])
+def test_a_second_derivative_is_refused(library, of):
+    """The library has no second derivative: asking for one says so, and does not leave the term out."""
+    z, idx, up = batch(3)
+    logits = torch.from_numpy(z).requires_grad_()
+    scale, loss, _, _ = balance_loss(logits, torch.from_numpy(idx), 0.3, True)
+    value = loss if of == "loss" else (scale * torch.from_numpy(up)).sum()
+    grad, = torch.autograd.grad(value, logits, create_graph=True)
+    with pytest.raises(RuntimeError, match="no second derivative"):
+        (grad.square().sum() + logits.square().sum()).backward()
+
+
+def test_a_graph_of_the_gradient_that_nothing_goes_through(library):
+    z, idx, _ = batch(4)
+    logits = torch.from_numpy(z).requires_grad_()
+    loss = balance_loss(logits, torch.from_numpy(idx), 0.3, True)[1]
+    grad, = torch.autograd.grad(loss, logits, create_graph=True)
+    close(grad.detach(), mx4.balance(z, idx, 0.3, True, 1.0)["dlogits"])
+    (logits.square().sum()).backward()
+    close(logits.grad, 2.0 * z)
