@@ -610,17 +610,15 @@ def moe_balance_loss(logits, expert_idx, coef: float = 0.01, renormalize: bool =
     _check_balance(logits, expert_idx)
     (T, E), k, dev = logits.shape, expert_idx.shape[1], logits.device
     lib = load()
-    # (small tensors in one: an allocation costs the host as much as two views, and a decoder batch's call is all host)
-    sums = torch.empty(2 * E + 1, dtype=torch.float32, device=dev)
-    prob_mean, weight, loss = sums.as_strided((E,), (1,), 0), sums.as_strided((E,), (1,), E), sums.as_strided((), (), 2 * E)
+    # (tensors of their own, three allocations: views of one share a version counter, so that changing one in place would spoil the others for autograd)
+    loss, prob_mean, weight = (torch.empty(shape, dtype=torch.float32, device=dev) for shape in ((), (E,), (E,)))
     counts = torch.empty(E, dtype=torch.int32, device=dev)
     scale = torch.empty(T, k, dtype=torch.float32, device=dev)
     if workspace is None:
         need = lib.moe_balance_loss_workspace_bytes(T, E)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    at = sums.data_ptr()
     rc = lib.moe_balance_loss(_ptr(logits, _FLOATS, "logits"), _DT[logits.dtype], _ptr(expert_idx, torch.int32, "expert_idx"), T, E, k, int(renormalize),
-                              coef, at + 8 * E, counts.data_ptr(), at, scale.data_ptr(), at + 4 * E, _ptr(workspace, torch.uint8, "workspace"),
+                              coef, loss.data_ptr(), counts.data_ptr(), prob_mean.data_ptr(), scale.data_ptr(), weight.data_ptr(), _ptr(workspace, torch.uint8, "workspace"),
                               0 if workspace is None else workspace.numel(), _stream())
     _check(rc, "moe_balance_loss")
     return loss, counts, prob_mean, scale, weight

@@ -30,3 +30,17 @@ def test_two_batches_routed_before_their_backward(renorm):
     for logits, idx, up in kept:
         want = mx4.balance(logits.detach().cpu().numpy(), idx, 0.3, renorm, 2.0, up)["dlogits"]
         assert np.abs(logits.grad.cpu().numpy() - want).max() <= 2e-5 * np.abs(want).max()
+
+
+def test_a_loss_and_a_statistic_changed_in_place():
+    rng = np.random.default_rng(22)
+    z = rng.standard_normal((37, 12)).astype(np.float32)
+    idx = np.argsort(-z, axis=1)[:, :2].astype(np.int32)
+    logits = to_dev(z, torch.float32).requires_grad_()
+    _, loss, _, mean = balance_loss(logits, to_dev(idx, torch.int32), 0.3, True)
+    mean.mul_(0.9)                                                                 # a moving average
+    loss += 7.0
+    loss.backward()
+    want = mx4.balance(z, idx, 0.3, True, 1.0)
+    assert abs(float(loss.detach()) - 7.0 - want["loss"]) <= 1e-5
+    assert np.abs(logits.grad.cpu().numpy() - want["dlogits"]).max() <= 2e-5 * np.abs(want["dlogits"]).max()

@@ -77,3 +77,46 @@ def test_a_graph_of_the_gradient_that_nothing_goes_through(library):
     close(grad.detach(), mx4.balance(z, idx, 0.3, True, 1.0)["dlogits"])
     (logits.square().sum()).backward()
     close(logits.grad, 2.0 * z)
+
+
+def small_tensors(monkeypatch):
+    """The binding itself with a library that only fills its outputs: everything but the pointers is as with the real one."""
+    import ctypes
+
+    class Library:
+        @staticmethod
+        def moe_balance_loss_workspace_bytes(T, E):
+            return 0
+
+        @staticmethod
+        def moe_balance_loss(logits, dtype, idx, T, E, k, renorm, coef, loss, counts, mean, scale, weight, ws, size, stream):
+            for at, n, value in ((loss, 1, 1.0), (mean, E, 2.0), (scale, T * k, 3.0), (weight, E, 4.0)):
+                (ctypes.c_float * n).from_address(at)[:] = [value] * n
+            (ctypes.c_int32 * E).from_address(counts)[:] = [5] * E
+            return 0
+
+        @staticmethod
+        def moe_balance_loss_backward(logits, dtype, idx, T, E, k, renorm, weight, dloss, dscale, out, stream):
+            w = (ctypes.c_float * E).from_address(weight)[:]
+            (ctypes.c_float * (T * E)).from_address(out)[:] = w * T
+            return 0
+
+    monkeypatch.setattr(B, "load", lambda: Library)
+    monkeypatch.setattr(B, "_ptr", lambda t, *a: None if t is None else t.data_ptr())
+    monkeypatch.setattr(B, "_stream", lambda: 0)
+
+
+def test_outputs_are_tensors_of_their_own(monkeypatch):
+    """What a training loop does to a loss and to a statistic in place: neither is refused, and neither reaches the other outputs or the gradient."""
+    small_tensors(monkeypatch)
+    z, idx, _ = batch(5)
+    outputs = B.moe_balance_loss(torch.from_numpy(z), torch.from_numpy(idx))
+    assert not any(t._is_view() for t in outputs) and len({t.untyped_storage().data_ptr() for t in outputs}) == 5
+    logits = torch.from_numpy(z).requires_grad_()
+    scale, loss, counts, mean = balance_loss(logits, torch.from_numpy(idx), 0.3, True)
+    mean.mul_(0.9)
+    counts.zero_()
+    loss += 2.0 * (scale * 0.0).sum() + 7.0
+    assert float(loss.detach()) == 8.0 and (mean == 2.0 * 0.9).all()
+    loss.backward()
+    assert (logits.grad == 4.0).all()
