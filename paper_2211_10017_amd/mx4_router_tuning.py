@@ -17,8 +17,10 @@ from .router import balance_loss
 
 
 def layer_output(layer, scale):
-    """The combine of the last experts() call as a function of the gate scales, for their gradient."""
-    y = layer.y_perm.float()[layer.inv_perm.long()].view(layer.T, layer.k, layer.d)
+    """The combine of the last experts() call as a function of the gate scales, for their gradient.  Rows behind the last expert's, those of finished
+    sentences, are not written by a call: they count as 0, whatever is in them."""
+    row = layer.inv_perm.long()
+    y = torch.where((row < layer.expert_offsets[layer.E])[:, None], layer.y_perm.float()[row], 0.0).view(layer.T, layer.k, layer.d)
     return (scale.unsqueeze(-1) * y).sum(1)
 
 

@@ -120,3 +120,30 @@ def test_outputs_are_tensors_of_their_own(monkeypatch):
     assert float(loss.detach()) == 8.0 and (mean == 2.0 * 0.9).all()
     loss.backward()
     assert (logits.grad == 4.0).all()
+
+
+class _Layer:
+    """What layer_output reads of a layer: the buffers of one call with a pruned token, whose rows no kernel has written."""
+    T, k, d = 3, 2, 4
+
+    def __init__(self, junk, dtype):
+        self.y_perm = torch.arange(24, dtype=torch.float32).reshape(6, 4).to(dtype)
+        self.y_perm[4:] = junk
+        self.inv_perm = torch.tensor([1, 0, 4, 5, 3, 2], dtype=torch.int32)       # token 1 is pruned: its assignments are behind the others
+        self.expert_offsets = torch.tensor([0, 2, 4], dtype=torch.int32)
+        self.E = 2
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), 3.0])
+def test_layer_output_of_pruned_tokens(junk, dtype):
+    """0 for them whatever their rows of y hold, and no gradient for their scales."""
+    from paper_2211_10017_amd.mx4_router_tuning import layer_output
+    layer = _Layer(junk, dtype)
+    scale = torch.tensor([[0.5, 0.25], [0.0, 0.0], [1.0, 2.0]], requires_grad=True)
+    out = layer_output(layer, scale)
+    y = torch.arange(24.0).reshape(6, 4)
+    want = torch.stack([0.5 * y[1] + 0.25 * y[0], torch.zeros(4), y[3] + 2.0 * y[2]])
+    assert torch.equal(out.detach(), want)
+    out.sum().backward()
+    assert torch.equal(scale.grad, torch.stack([y[[1, 0]].sum(1), torch.zeros(2), y[[3, 2]].sum(1)]))
