@@ -244,8 +244,10 @@ def moe_permute(expert_idx, x, E: int, out=None, workspace=None):
 def moe_permute_index(expert_idx, E: int, d: int, act_dtype, perm_src, inv_perm, expert_offsets, workspace):
     """moe_permute without the copy of the rows, into buffers of the caller's."""
     T, k = expert_idx.shape
+    if perm_src.numel() < T * k or inv_perm.numel() < T * k or expert_offsets.numel() < E + 1:
+        raise MoeError("perm_src and inv_perm must hold %d numbers and expert_offsets %d" % (T * k, E + 1))
     rc = load().moe_permute(_ptr(expert_idx, torch.int32, "expert_idx"), None, _DT[act_dtype], T, k, E, d, None, _ptr(perm_src, torch.int32, "perm_src"),
-                            _ptr(inv_perm, torch.int32, "inv_perm"), _ptr(expert_offsets, torch.int32, "expert_offsets"), _ptr(workspace), workspace.numel(), _stream())
+                            _ptr(inv_perm, torch.int32, "inv_perm"), _ptr(expert_offsets, torch.int32, "expert_offsets"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
     _check(rc, "moe_permute")
 
 
