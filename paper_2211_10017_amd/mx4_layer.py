@@ -45,6 +45,8 @@ class MoEMx4Layer:
         """Gate and the index of the permutation; finished as for MoEExpertLayer.forward."""
         if x.dtype != self.act_dtype or tuple(x.shape) != (self.T, self.d):
             raise B.MoeError("x must be [T, d] in the layer's activation dtype")
+        if finished is not None and finished.numel() != self.T:
+            raise B.MoeError("finished must be a contiguous uint8 [T] CUDA tensor")
         B.moe_gate_topk(x, self.wg, self.gate_bias, self.k, self.renormalize, out=(self.expert_idx, self.expert_scale), finished=finished)
         B.moe_permute_index(self.expert_idx, self.E, self.d, x.dtype, self.perm_src, self.inv_perm, self.expert_offsets, self.ws_permute)
 

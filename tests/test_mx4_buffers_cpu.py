@@ -25,3 +25,27 @@ def test_permute_index_refuses_buffers_that_do_not_fit(monkeypatch, bad):
     with pytest.raises(B.MoeError):
         call(dict(size, **bad))
     assert len(called) == 2
+
+
+@pytest.mark.parametrize("finished", [torch.zeros(15, dtype=torch.uint8), torch.zeros(17, dtype=torch.uint8), torch.zeros(16, dtype=torch.bool), torch.zeros((16, 2), dtype=torch.uint8)[:, 0],
+                                      torch.zeros(16, dtype=torch.int32)])
+def test_layer_refuses_a_mask_that_does_not_fit(monkeypatch, finished):
+    """The gate reads a byte of it per token."""
+    from paper_2211_10017_amd import MoEMx4Layer
+    layer = MoEMx4Layer(16, 64, 64, 8, 2, device="cpu")
+    called = []
+
+    class Library:
+        moe_gate_topk = staticmethod(lambda *args: called.append(args) or 0)
+        moe_permute = staticmethod(lambda *args: 0)
+
+    monkeypatch.setattr(B, "load", lambda: Library)
+    monkeypatch.setattr(B, "_stream", lambda: 0)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
+    x = torch.zeros((16, 64), dtype=torch.float16)
+    layer.route(x, torch.zeros(16, dtype=torch.uint8))
+    layer.route(x)
+    assert len(called) == 2
+    with pytest.raises(B.MoeError, match="finished"):
+        layer.route(x, finished)
+    assert len(called) == 2
