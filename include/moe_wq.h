@@ -414,7 +414,7 @@ int moe_grouped_ffn_mx4(const void *x, int act_dtype, int T, const int32_t *perm
  *   logits [T,E] dtype; expert_idx [T,k]; loss [1] fp32, counts [E] int32, prob_mean [E] fp32 (P), expert_scale [T,k] fp32,
  *   weight [E] fp32: d loss / d p_te, the same for every token, which is all that the backward pass needs of the forward one
  *   backward: dloss [1] fp32 and dscale [T,k] fp32, gradients of loss and of expert_scale, each may be NULL (zero); dlogits [T,E] in dtype.
- * Counts take no gradient.  Limits: 1 <= k <= 8, k <= E <= 1024.  Sums are added in a fixed order.  (Small batches need no workspace: the query says 0.)
+ * Counts take no gradient.  Limits: 1 <= k <= 8, k <= E <= 1024, T * k < 2^31.  Sums are added in a fixed order.  (Small batches need no workspace: the query says 0.)
  */
 size_t moe_balance_loss_workspace_bytes(int T, int E);
 int moe_balance_loss(const void *logits, int dtype, const int32_t *expert_idx, int T, int E, int k, int renormalize, float coef, float *loss,

@@ -474,6 +474,7 @@ static int check_balance(const char *what, const void *logits, int dtype, const 
 {
     if (T < 0 || E < 1 || k < 1 || k > E) return fail(MOE_ERR_INVALID_ARG, "%s: need T >= 0 and 1 <= k <= E (T=%d E=%d k=%d)", what, T, E, k);
     if (E > kBalanceMostExperts || k > kBalanceMostK) return fail(MOE_ERR_UNSUPPORTED, "%s: E = %d above %d or k = %d above %d", what, E, kBalanceMostExperts, k, kBalanceMostK);
+    if ((long)T * k > 0x7fffffffL) return fail(MOE_ERR_INVALID_ARG, "%s: T*k overflows int32", what);
     if (dtype < 0 || dtype > 2) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
     if (T && (!logits || !idx)) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(logits)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
