@@ -391,7 +391,7 @@ int moe_mx4_dequantize(const void *codes, const void *scales, int matrices, int 
  *     x [T, d] act_dtype (any of the three); both roundings to the 4-bit format are moe_mx4_quantize_rows' (h from its fp32 value); y_perm [R, d] y_dtype
  *     workspace: the 4-bit forms of x and h (moe_grouped_ffn_mx4_workspace_bytes, 16-byte aligned)
  * max_rows_per_expert: an upper bound on the rows of one expert or 0; it only takes part in the choice of kernels.
- * Requires K, d, F % 64 == 0, N % 32 == 0, E <= 4096, K and N at most 2^24.
+ * Requires K, d, F % 64 == 0, N % 32 == 0, E <= 4096, K and N at most 2^24, a_rows, and T and R of the FFN, below 2^30.
  */
 int moe_grouped_gemm_mx4(const void *a_codes, const void *a_scales, int a_rows, const int32_t *perm_src, int k, const int32_t *expert_offsets,
                          int R, int E, int max_rows_per_expert, int K, int N, const void *w_codes, const void *w_scales, const void *bias,

@@ -9,7 +9,7 @@ static int check_product(const char *what, int R, int E, int a_rows, int K, int 
         return fail(MOE_ERR_INVALID_ARG, "%s: need R, E and rows >= 0, K %% 64 == 0, N %% 32 == 0 (R=%d E=%d rows=%d K=%d N=%d)", what, R, E, a_rows, K, N);
     if (perm_src ? k < 1 : a_rows < R) return fail(MOE_ERR_INVALID_ARG, "%s: without perm_src there are as many rows as R, with it k >= 1", what);
     if (K > 1 << 24 || N > 1 << 24) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d or N = %d above 2^24", what, K, N);      // (what a lane's 32-bit offsets reach)
-    if (a_rows > 0x3fffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are more than 2^30", what, a_rows);
+    if (a_rows > 0x3fffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are 2^30 or more", what, a_rows);
     if (E > 4096) return fail(MOE_ERR_UNSUPPORTED, "%s: E = %d above 4096", what, E);
     return MOE_OK;
 }
@@ -59,6 +59,7 @@ extern "C" int moe_grouped_ffn_mx4(const void *x, int act_dtype, int T, const in
     const char *what = "moe_grouped_ffn_mx4";
     if (int rc = check_product(what, R, E, T, d, F, perm_src, k)) return rc;
     if (F % 64) return fail(MOE_ERR_INVALID_ARG, "%s: F must be a multiple of 64", what);
+    if (R > 0x3fffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are 2^30 or more", what, R);       // (fc2's rows are h's)
     if (act_dtype < 0 || act_dtype > 2 || y_dtype < 0 || y_dtype > 2) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
     if (activation < MOE_ACT_RELU || activation > MOE_ACT_GELU) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown activation %d", what, activation);
     if (max_rows_per_expert < 0) return fail(MOE_ERR_INVALID_ARG, "%s: max_rows_per_expert < 0", what);

@@ -25,3 +25,12 @@ def test_assignments_are_counted_in_32_bits(lib):
     for T, k in ((2 ** 28 - 1, 8), (2 ** 30 - 1, 2), (MOST, 1)):
         assert fwd(T, k) == WORKSPACE                                              # (what a call is refused for that goes past the counts)
         assert back(T, k, None) == ARG and b"NULL" in lib.moe_last_error()
+
+
+def test_rows_that_a_lanes_offsets_reach(lib):
+    """A lane finds its row's scales by four bytes times the row's number in 32 bits: fewer than 2^30 rows, those of h as well, which are R."""
+    ffn = lambda T, R: lib.moe_grouped_ffn_mx4(P, 0, T, P, 1, P, R, 2, 0, 64, 64, 0, P, P, None, P, P, None, P, 0, P, 0, None)  # noqa: E731
+    gemm = lambda rows, R, y=P: lib.moe_grouped_gemm_mx4(P, P, rows, P, 1, P, R, 2, 0, 64, 32, P, P, None, -1, y, 0, None)  # noqa: E731
+    assert ffn(2 ** 30, 8) == UNSUPPORTED and ffn(8, 2 ** 30) == UNSUPPORTED and b"2^30" in lib.moe_last_error() and ffn(8, MOST) == UNSUPPORTED
+    assert ffn(2 ** 30 - 1, 2 ** 30 - 1) == WORKSPACE
+    assert gemm(2 ** 30, 8) == UNSUPPORTED and gemm(8, MOST, None) == ARG          # (a product's R is only how many rows it writes)
