@@ -15,7 +15,7 @@ namespace moe {
 
 constexpr int kMxBlock = 32;
 constexpr int kMxGroup = 128;                       // values whose four scales share a dword
-__host__ __device__ inline int mx_groups(int K) { return (K + kMxGroup - 1) / kMxGroup; }
+__host__ __device__ inline int mx_groups(int K) { return K / kMxGroup + (K % kMxGroup != 0); }
 __host__ __device__ inline size_t mx_code_bytes(size_t rows, int K) { return rows * (size_t)(K / 2); }
 __host__ __device__ inline size_t mx_scale_bytes(size_t rows, int K) { return rows * 4 * (size_t)mx_groups(K); }
 

@@ -151,7 +151,7 @@ constexpr double kMostBlocks = 0xffffff;          // of 256 threads: a launch ta
 int launch_mx4_quantize_rows(const void *x, int dtype, int R, int K, long stride, uint8_t *codes, uint8_t *scales, hipStream_t s)
 {
     const int G = mx_groups(K), per = (long)R * G >= 16384 ? 4 : 1;
-    const long blocks = (long)((R + 15) / 16) * ((G + per - 1) / per);
+    const long blocks = ((long)R + 15) / 16 * ((G + per - 1) / per);
     if (blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "moe_mx4_quantize_rows: %ld workgroups exceed one launch", blocks);
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, R, K, stride, per, codes, scales); };
     if (dtype == MOE_F16) run(&mx4_quantize_rows_kernel<MOE_F16>);
@@ -183,7 +183,7 @@ extern "C" int moe_mx4_quantize_experts(const float *w, int E, int K, int N, voi
     if (E == 0) return MOE_OK;
     if (!w || !codes || !scales) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(w) || !aligned16(codes) || !aligned16(scales)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
-    const double blocks = (double)E * ((K + 255) / 256) * ((N + 127) / 128);
+    const double blocks = (double)E * (((long)K + 255) / 256) * (((long)N + 127) / 128);
     if (2 * blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "%s: %.0f workgroups exceed one launch", what, blocks);
     hipLaunchKernelGGL(mx4_quantize_experts_kernel, dim3((unsigned)blocks), dim3(512), 0, as_stream(stream), w, K, N, (uint8_t *)codes, (uint8_t *)scales);
     return check_launch(what);
@@ -198,7 +198,7 @@ extern "C" int moe_mx4_dequantize(const void *codes, const void *scales, int mat
     if (matrices == 0 || rows == 0) return MOE_OK;
     if (!codes || !scales || !out) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(codes) || !aligned16(scales) || !aligned16(out)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
-    const double blocks = (double)((rows + 15) / 16) * mx_groups(K);
+    const double blocks = (double)(((long)rows + 15) / 16) * mx_groups(K);
     const int most = matrices < 0x8000 ? matrices : 0x8000;
     if (blocks > kMostBlocks) return fail(MOE_ERR_UNSUPPORTED, "%s: %.0f workgroups exceed one launch", what, blocks);
     auto run = [&](auto kernel) {

@@ -3,6 +3,7 @@ import ctypes
 
 import pytest
 
+from launches import P as PTR, record
 from paper_2211_10017_amd import binding as B
 
 P = ctypes.c_void_p(0x1000)          # never dereferenced: validation fails first
@@ -34,3 +35,18 @@ def test_rows_that_a_lanes_offsets_reach(lib):
     assert ffn(2 ** 30, 8) == UNSUPPORTED and ffn(8, 2 ** 30) == UNSUPPORTED and b"2^30" in lib.moe_last_error() and ffn(8, MOST) == UNSUPPORTED
     assert ffn(2 ** 30 - 1, 2 ** 30 - 1) == WORKSPACE
     assert gemm(2 ** 30, 8) == UNSUPPORTED and gemm(8, MOST, None) == ARG          # (a product's R is only how many rows it writes)
+
+
+def test_more_rows_than_a_launch_takes(lib):
+    for R in (2 ** 28 + 16, MOST - 15, MOST - 14, MOST):
+        for dtype in (0, 1, 2):
+            assert lib.moe_mx4_quantize_rows(P, dtype, R, 64, 64, P, P, None) == UNSUPPORTED and b"exceed one launch" in lib.moe_last_error()
+            assert lib.moe_mx4_dequantize(P, P, 1, R, 64, P, dtype, None) == UNSUPPORTED and b"exceed one launch" in lib.moe_last_error()
+    assert lib.moe_mx4_quantize_rows(P, 0, 40000, MOST - 63, MOST - 63, P, P, None) == UNSUPPORTED
+    assert lib.moe_mx4_quantize_experts(P, 1, MOST - 63, 64, P, P, None) == UNSUPPORTED
+    assert lib.moe_mx4_quantize_experts(P, 1, 64, MOST - 31, P, P, None) == UNSUPPORTED and lib.moe_mx4_dequantize(P, P, 1, 64, MOST - 63, P, 0, None) == UNSUPPORTED
+
+
+def test_the_longest_row_takes_a_launch():
+    one = record([("moe_mx4_quantize_rows", [PTR, 0, 1, MOST - 63, [MOST - 63], PTR, PTR, None])])[0]
+    assert one.rc == 0 and one.launches[0].grid[0] == 2 ** 24 // 4
