@@ -22,6 +22,8 @@ __device__ inline u32x4_t mx_quantize_block(const u32x4_t (&raw)[4], uint32_t &b
 {
     typedef unsigned short us2_t __attribute__((ext_vector_type(2)));
     typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+    // (by value: the compiler's bit_cast of a vector's element is that of its first one)
+    auto pair = [](uint32_t v) { return __builtin_bit_cast(bf2_t, v); };
     us2_t m = {0, 0};
 #pragma unroll
     for (int i = 0; i < 16; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2_t, raw[i >> 2][i & 3] & 0x7fff7fffu));
@@ -33,10 +35,10 @@ __device__ inline u32x4_t mx_quantize_block(const u32x4_t (&raw)[4], uint32_t &b
     for (int q = 0; q < 4; ++q) {
         uint32_t d = 0;
         if constexpr (XDT == MOE_BF16) {
-            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][0]), s, 0);
-            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][1]), s, 1);
-            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][2]), s, 2);
-            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, __builtin_bit_cast(bf2_t, raw[q][3]), s, 3);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(raw[q][0]), s, 0);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(raw[q][1]), s, 1);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(raw[q][2]), s, 2);
+            d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(raw[q][3]), s, 3);
         } else {
             d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(d, bits_h2(raw[q][0]), s, 0);
             d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(d, bits_h2(raw[q][1]), s, 1);
