@@ -4,11 +4,11 @@
 //   loss = coef E sum_e (c_e / A) P_e,     weight_e = d loss / d p_te = coef E c_e / (A N)
 //   dlogits_te = dloss p_te (weight_e - sum_j p_tj weight_j) + the gate scales' part
 //
-// Both directions are bound by reading the logits (and the backward by writing their gradient), small batches by their launches.  A token's logits are
-// spread over L lanes of a wavefront, V neighbouring ones per lane and step, so that a lane keeps the sums of its own experts in registers over all
+// A token's logits are spread over L lanes of a wavefront, V neighbouring ones per lane and step, so that a lane keeps the sums of its own experts in registers over all
 // of its tokens; a block's sums meet in LDS and the blocks' in a second launch, in the order of the blocks: no floating-point atomics, the same bits
-// every time.  (A launch of one block does without.)  131072 tokens by 256 experts, two each, fp32: forward 42 us = 3.2 TB/s (its exponentials and
-// reductions are as long as its loads), the blocks' sums 9.5 us, backward 53 us = 5.1 TB/s.
+// every time.  (A launch of one block does without.)  131072 tokens by 256 experts, two each, fp32: forward 42 us = 3.2 TB/s, the blocks' sums 9.4 us,
+// backward 53 us = 5.1 TB/s.  Large batches are bound by both the instructions and the loads of too few wavefronts: of the cycles of a SIMD, which has two of them, instructions
+// take 53 % forward and 60 % backward.  Small ones are bound by their launches.
 #include <math.h>
 
 #include <type_traits>
@@ -17,6 +17,8 @@
 
 namespace moe {
 
+// Blocks, one per compute unit (us, forward with the blocks' sums + backward: 131072 tokens by 256 experts 128 blocks 71 + 94, 256 48 + 54, 512 44 + 51, 1024 59 + 53;
+// by 64 49 + 52, 30 + 29, 25 + 21, 28 + 21; 16384 by 64 13.3 + 8.0, 11.3 + 5.6, 12.3 + 5.5, 12.2 + 5.5: the largest batches would gain by two per unit).
 constexpr int kBalanceThreads = 512, kBalanceMostBlocks = 256, kBalanceMostExperts = 1024, kBalanceMostK = 8;
 
 struct BalanceArgs {
@@ -437,7 +439,8 @@ static BalanceShape balance_shape(int E)
     return b;
 }
 
-// Blocks of the forward launch.  Up to four rounds of tokens stay in one block, which then needs no second launch to join the blocks' sums (4 us).
+// Blocks of the forward launch.  Up to four rounds of tokens stay in one block, which then needs no second launch to join the blocks' sums (us, one block / several and that launch:
+// two rounds, 128 tokens by 32 experts 7.2 / 9.4, 64 by 256 9.5 / 10.9; four, 256 by 32 9.3 / 9.3, 128 by 61 9.2 / 9.1, 128 by 256 12.2 / 11.2; eight, 512 by 32 13.5 / 9.4, 256 by 256 17.5 / 11.3).
 static int balance_blocks(int T, int E)
 {
     const long per = kBalanceThreads / balance_shape(E).L, want = T <= 4 * per ? 1 : ((long)T + per - 1) / per;

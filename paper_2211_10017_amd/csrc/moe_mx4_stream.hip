@@ -206,8 +206,10 @@ static int launch_stream(const MxArgs &p, hipStream_t s)
 //  - K up to 4096 and many blocks: two wavefronts with two slabs and two lines (64 tokens, two of 32 experts, 2048 x 8192: 48.9 = 5.7 TB/s, eight wavefronts 59.5;
 //    of 64 experts of 4096 x 16384 281 and 285 to 329); fewer: four wavefronts, two slabs (64 tokens, 4096 x 1024: 13.4, eight wavefronts 14.2);
 //  - longer K: eight wavefronts, two slabs (8192 x 2048: 46.6 = 6.0 TB/s, two wavefronts 58.1; 16384 x 4096 286 and 291).
-// Row tiles from 25 rows per expert on (us, streaming / tiles: 384 tokens, two of 32 experts of 1024 x 4096, 24 rows, fc1 21.3 / 19.1, fc2 20.7 / 19.8, of 2048 x 8192 65 / 64
-// and 59 / 69; 32 rows 27.7 / 19.7 and 22.4 / 20.5; 16 rows 20.4 / 18.7 and 16.9 / 20.1).
+// Row tiles from 25 rows per expert on.  One bound on the mean for all products, which is where an FFN's two together are about as fast either way (us, fc1 + fc2, streaming / tiles,
+// two of 32 experts): of 1024 x 4096 16 rows 20.4 + 16.9 / 18.7 + 20.1, 24 rows 21.3 + 20.7 / 19.1 + 19.8, 32 rows 27.7 + 22.4 / 19.7 + 20.5; of 2048 x 8192 24 rows 65 + 59 / 64 + 69.
+// What it gives away: 1 to 2 us of a product with short K at 16 to 24 rows, which tiles would win, and an expert with much of an uneven batch, which is streamed in items of
+// 32 rows that each read its weights.
 static bool streams(int most, int E) { return ((long)most + E - 1) / E <= 24; }
 
 int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
@@ -220,7 +222,9 @@ int launch_mx4_gemm(const MxArgs &p, hipStream_t s)
     return blocks >= 2048 ? launch_stream<2, 2, 2>(p, s) : launch_stream<4, 2, 1>(p, s);
 }
 
-// Whether fc1 quantises its rows for itself: every block does so for the rows of its item, so only where there are few blocks.
+// Whether fc1 quantises its rows for itself: every block does so for the rows of its item, so only where there are few blocks.  An FFN of two experts a token, us, by itself / after the
+// quantiser: 32 experts of 1024 x 4096, fp16, 252 blocks 10.8 / 12.0, 488 12.0 / 12.7, 919 15.5 / 14.9; bf16 10.5 / 11.8, 12.5 / 13.1, 16.0 / 15.4; 16 of 704 x 2880, 581 blocks 12.6 / 12.9, 927
+// 13.9 / 13.7; 32 of 512 x 2048, 816 blocks 11.9 / 11.7.  Longer rows want fewer blocks, which the bound leaves aside: 4096 x 1024, 230 blocks 14.5 / 14.9, 408 20.9 / 18.9; 2048 x 8192, 448 17.0 / 16.4.
 bool mx4_fuses_rows(int most, int E, int N, int x_dtype)
 {
     return x_dtype != MOE_F32 && streams(most, E) && decode_active_experts(most, E) * (N / 32) <= 512;

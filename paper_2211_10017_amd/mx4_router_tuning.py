@@ -3,8 +3,8 @@
     python -m paper_2211_10017_amd.mx4_router_tuning [--steps 60]
 
 The experts stay as they are; the router learns, from the layer's error against what the unquantised layer gave, which experts to use, and
-its balance loss keeps their loads even.  Everything of a step but the optimiser and the small products with the router's
-weight is the library's: gate, permutation, expert FFN, the balance loss with the gate scales, and the gradient of both."""
+its balance loss keeps their loads even.  The library's part of a step is the gate, the permutation, the expert FFN, the balance loss with the gate scales, and the
+gradient of both; the products with the router's weight, the combine as a function of the scales, the error and the optimiser are torch's."""
 from __future__ import annotations
 
 import argparse
