@@ -422,6 +422,70 @@ int moe_balance_loss(const void *logits, int dtype, const int32_t *expert_idx, i
 int moe_balance_loss_backward(const void *logits, int dtype, const int32_t *expert_idx, int T, int E, int k, int renormalize, const float *weight,
                               const float *dloss, const float *dscale, void *dlogits, void *stream);
 
+/*
+ * Gradient of sorting tokens by expert and back (moe_permute, moe_combine):
+ *   moe_combine_backward: dy_perm[inv_perm[a]] = expert_scale[a] * dout[a / k], dscale[a] = <dout[a / k], y_perm[inv_perm[a]]>, a = t*k + j < T*k
+ *     dout [T,d] out_dtype; y_perm, dy_perm [R,d] y_dtype; inv_perm, expert_scale [T*k] as for moe_combine; dscale [T,k] fp32
+ *   moe_permute_backward: dx[t] = sum_j dx_perm[inv_perm[t*k+j]]  (fp32, j ascending; one rounding)
+ *     dx_perm [R,d] perm_dtype; dx [T,d] dx_dtype
+ * Types MOE_F16 | MOE_BF16 | MOE_F32.  active_rows: as for moe_combine, or NULL.  An assignment whose row is at or past it (or outside [0, R)) belongs to a pruned token: its
+ * dscale is 0, its row of dy_perm (if it is inside) is written as 0, its rows of y_perm and dx_perm are not read.  inv_perm has no row twice; rows of dy_perm that it does not
+ * name are not written.  dout and the buffers written must not overlap.  d % 8 == 0, T*k < 2^31.
+ */
+int moe_combine_backward(const void *dout, int out_dtype, const void *y_perm, int y_dtype, const int32_t *inv_perm, const float *expert_scale,
+                         const int32_t *active_rows, int T, int k, int d, int R, void *dy_perm, float *dscale, void *stream);
+int moe_permute_backward(const void *dx_perm, int perm_dtype, const int32_t *inv_perm, const int32_t *active_rows, int T, int k, int d, int R,
+                         void *dx, int dx_dtype, void *stream);
+
+/*
+ * Low-rank adapters of many requests, or of experts, beside a projection that they share.  With e the adapter of row r and t = perm_src[r] / k its token:
+ *   v[r] = A[e] x[t],  out[r] = y[r] + scale[e] * v[r] B[e]
+ *   x [T,K] dtype (MOE_F16 | MOE_BF16), x_stride values from row to row; A [E,rank,K], B [E,rank,N] in dtype; scale [E] fp32 or NULL (1)
+ *   perm_src [R], expert_offsets [E+1]: the sorted index of moe_permute (R = T*k), whose "experts" are the adapters.  Requests: moe_permute on the request's adapter with
+ *     k = 1, E for a request without one.  perm_src NULL: x's first R rows are sorted already (k = 1).
+ *   y, out [R,N] y_dtype (any of the three), y_stride and out_stride values from row to row: in sorted order or, by_assignment != 0, in the order of the assignments
+ *     perm_src[r] (with k = 1 the tokens').  y == out: in place; y NULL: 0.  Otherwise they must not overlap.
+ *   Rows of no adapter (at or past expert_offsets[E]) are y's; in place they are neither read nor written.
+ *   v [R,rank] fp32: what the backward pass needs of this one, in sorted order (rows of no adapter are not written), or NULL.
+ * Backward, of dy [R,N] dy_dtype (ordered as y):  u[r] = scale[e] * B[e] dy[r],
+ *   dx[r] = u[r] A[e] in dtype, ordered as y, 0 for rows of no adapter (with more than one row per token moe_permute_backward adds them up)
+ *   da[e] = sum_r u[r] x[t]^T,  db[e] = scale[e] * sum_r v[r] dy[r]^T  in grad_dtype, 0 for adapters without rows; sums over rows in a fixed order
+ *   dx, da, db may each be NULL (x is read for da only, v for db only).
+ * Products are summed in fp32, v and u kept in it.  Strides and K, N are multiples of 8, K and N at most 2^24, 1 <= rank <= 128, E <= 4096, R < 2^24.  expert_offsets and
+ * perm_src are forced into range: wrong contents give wrong results but no stray access.
+ */
+size_t moe_adapters_workspace_bytes(int R, int E, int K, int N, int rank);
+int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k, const int32_t *expert_offsets, int R, int E, int K, int N, int rank,
+                 const void *a, const void *b, const float *scale, int by_assignment, const void *y, int64_t y_stride, void *out, int64_t out_stride, int y_dtype, float *v,
+                 void *workspace, size_t workspace_bytes, void *stream);
+int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_stride, const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k,
+                          const int32_t *expert_offsets, int R, int E, int K, int N, int rank, const void *a, const void *b, const float *scale, int by_assignment,
+                          const float *v, void *dx, int64_t dx_stride, void *da, void *db, int grad_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * An AdamW step over `count` tensors, with g = grad * grad_scale and t the step's number, from 1 on:
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, p rounded once to its type, and once to copy_dtype (MOE_F16 | MOE_BF16, for fp32 p; -1: no copies) into copy.
+ *   state_bits 32: m and v are fp32 [n].  state_bits 8: m holds codes of m, v codes of sqrt(v), n bytes each, e4m3 numbers in units of 2^(scale - 127), a byte of
+ *   m_scales / v_scales for each 32 neighbouring values ([ceil(n/32)]): with amax the largest magnitude of the 32, scale = floor(log2(amax)) - 7 + 127, at least 0; nearest code,
+ *   ties to the even one, but for sqrt(v) > 0 at least the smallest number; 255 for a block with an infinity or a NaN, which then reads as NaN.  All zero bytes: zeros.
+ *   tensors: HOST array (read before the call returns); its pointers are device pointers, aligned for their types (16-byte alignment is the fast way).  No two tensors overlap.
+ *   step_ptr: t on the device instead of `step` (a captured step then counts on; numbers below 1 count as 1), or NULL.
+ * moe_adamw_state: the values of n codes, [n] in out_dtype.
+ */
+typedef struct {
+    void *p;
+    const void *g;
+    void *m, *v;
+    uint8_t *m_scales, *v_scales;
+    void *copy;
+    int64_t n;
+} moe_adamw_tensor;
+int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2,
+              double eps, double weight_decay, double grad_scale, int step, const int32_t *step_ptr, void *stream);
+int moe_adamw_state(const void *codes, const void *scales, int64_t n, void *out, int out_dtype, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

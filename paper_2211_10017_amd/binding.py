@@ -28,7 +28,9 @@ EXPORTS = ["moe_last_error", "moe_last_ffn_kernels", "moe_device_info", "moe_abi
            "moe_grouped_ffn_wq_noalloc_max_bytes", "moe_grouped_ffn_wq_noalloc",
            "moe_mx4_quantize_rows", "moe_mx4_quantize_experts", "moe_mx4_dequantize", "moe_grouped_gemm_mx4",
            "moe_grouped_ffn_mx4_workspace_bytes", "moe_grouped_ffn_mx4",
-           "moe_balance_loss_workspace_bytes", "moe_balance_loss", "moe_balance_loss_backward"]
+           "moe_balance_loss_workspace_bytes", "moe_balance_loss", "moe_balance_loss_backward",
+           "moe_combine_backward", "moe_permute_backward", "moe_adapters_workspace_bytes", "moe_adapters", "moe_adapters_backward",
+           "moe_adamw", "moe_adamw_state"]
 
 LAYER_MAX_EXPERTS = 256   # experts of a whole layer call: moe_gate_topk's limit (moe_permute: 1024, the FFN: 4096)
 
@@ -129,6 +131,21 @@ def load():
     lib.moe_balance_loss.argtypes = [vp, i, vp, i, i, i, i, f, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.moe_balance_loss_backward.restype = i
     lib.moe_balance_loss_backward.argtypes = [vp, i, vp, i, i, i, i, vp, vp, vp, vp, vp]
+    lib.moe_combine_backward.restype = i
+    lib.moe_combine_backward.argtypes = [vp, i, vp, i, vp, vp, vp, i, i, i, i, vp, vp, vp]
+    lib.moe_permute_backward.restype = i
+    lib.moe_permute_backward.argtypes = [vp, i, vp, vp, i, i, i, i, vp, i, vp]
+    lib.moe_adapters_workspace_bytes.restype = sz
+    lib.moe_adapters_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.moe_adapters.restype = i
+    lib.moe_adapters.argtypes = [vp, i, i64, i, vp, i, vp, i, i, i, i, i, vp, vp, vp, i, vp, i64, vp, i64, i, vp, vp, sz, vp]
+    lib.moe_adapters_backward.restype = i
+    lib.moe_adapters_backward.argtypes = [vp, i, i64, vp, i, i64, i, vp, i, vp, i, i, i, i, i, vp, vp, vp, i, vp, vp, i64, vp, vp, i, vp, sz, vp]
+    d = ctypes.c_double
+    lib.moe_adamw.restype = i
+    lib.moe_adamw.argtypes = [vp, i, i, i, i, i, d, d, d, d, d, d, i, vp, vp]
+    lib.moe_adamw_state.restype = i
+    lib.moe_adamw_state.argtypes = [vp, vp, i64, vp, i, vp]
     _lib = lib
     return lib
 
@@ -640,4 +657,223 @@ def moe_balance_loss_backward(logits, expert_idx, weight, dloss=None, dscale=Non
                                           int(renormalize), _ptr(weight, torch.float32, "weight"), _ptr(dloss, torch.float32, "dloss"),
                                           _ptr(dscale, torch.float32, "dscale"), _ptr(out, logits.dtype, "out"), _stream())
     _check(rc, "moe_balance_loss_backward")
+    return out
+
+
+# ---- gradient of sorting tokens by expert and back -------------------------------------------------------------------------------------
+
+def _check_device(*tensors):
+    """A call runs on the current device's stream: its tensors have to be there."""
+    here = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise MoeError("a tensor is on device %d, the current device is %d" % (t.get_device(), here))
+
+
+def moe_combine_backward(dout, y_perm, inv_perm, expert_scale, active_rows=None, out=None):
+    """Gradient of moe_combine: (dy_perm like y_perm, dscale fp32 [T, k]) of dout [T, d]; rows of pruned assignments are 0."""
+    if dout.dim() != 2 or expert_scale.dim() != 2 or y_perm.dim() != 2:
+        raise MoeError("dout must be [T, d], y_perm [R, d] and expert_scale [T, k]")
+    (T, d), (R, width), k = dout.shape, y_perm.shape, expert_scale.shape[1]
+    if width != d or expert_scale.shape[0] != T or inv_perm.numel() != T * k or (active_rows is not None and active_rows.numel() < 1):
+        raise MoeError("y_perm must be [R, %d], expert_scale [%d, k] and inv_perm [T * k]" % (d, T))
+    if out is None:
+        if R == T * k:
+            dy = torch.empty_like(y_perm)
+        else:
+            dy = torch.zeros_like(y_perm)                               # (rows that belong to none of these tokens)
+        dscale = torch.empty(T, k, dtype=torch.float32, device=dout.device)
+    else:
+        dy, dscale = out
+        if dy.shape != y_perm.shape or dscale.shape != (T, k):
+            raise MoeError("out must be [R, d] and [T, k]")
+    _check_device(dout, y_perm, inv_perm, expert_scale, active_rows, dy, dscale)
+    rc = load().moe_combine_backward(_ptr(dout, _FLOATS, "dout"), _DT[dout.dtype], _ptr(y_perm, _FLOATS, "y_perm"), _DT[y_perm.dtype], _ptr(inv_perm, torch.int32, "inv_perm"),
+                                     _ptr(expert_scale, torch.float32, "expert_scale"), _ptr(active_rows, torch.int32, "active_rows"), T, k, d, R,
+                                     _ptr(dy, y_perm.dtype, "dy_perm"), _ptr(dscale, torch.float32, "dscale"), _stream())
+    _check(rc, "moe_combine_backward")
+    return dy, dscale
+
+
+def moe_permute_backward(dx_perm, inv_perm, T: int, k: int, active_rows=None, out_dtype=None, out=None):
+    """Gradient of moe_permute's copy of the rows: dx[t] = sum over the token's rows of dx_perm [R, d]; rows of pruned assignments count as 0."""
+    if dx_perm.dim() != 2 or inv_perm.numel() != T * k or (active_rows is not None and active_rows.numel() < 1):
+        raise MoeError("dx_perm must be [R, d] and inv_perm [T * k]")
+    R, d = dx_perm.shape
+    if out is None:
+        out = torch.empty(T, d, dtype=out_dtype or dx_perm.dtype, device=dx_perm.device)
+    elif out.shape != (T, d):
+        raise MoeError("out must be %s" % ((T, d),))
+    _check_device(dx_perm, inv_perm, active_rows, out)
+    rc = load().moe_permute_backward(_ptr(dx_perm, _FLOATS, "dx_perm"), _DT[dx_perm.dtype], _ptr(inv_perm, torch.int32, "inv_perm"), _ptr(active_rows, torch.int32, "active_rows"),
+                                     T, k, d, R, _ptr(out, _FLOATS, "out"), _DT[out.dtype], _stream())
+    _check(rc, "moe_permute_backward")
+    return out
+
+
+# ---- low-rank adapters -----------------------------------------------------------------------------------------------------------------
+
+def _rows(t, name, columns, dtypes):
+    """(pointer, values from row to row) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.shape[1] != columns or not t.is_cuda or (t.stride(1) != 1 and columns > 1):
+        raise MoeError("%s must be a [.., %d] CUDA tensor with contiguous rows" % (name, columns))
+    if t.dtype not in dtypes:
+        raise MoeError("%s has dtype %s, expected %s" % (name, t.dtype, dtypes))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else columns
+
+
+def _adapter_sizes(a, b, expert_offsets, perm_src, k, scale, by_assignment, x_rows):
+    if a.dim() != 3 or b.dim() != 3 or a.shape[:2] != b.shape[:2] or a.dtype not in (torch.float16, torch.bfloat16):
+        raise MoeError("a must be [E, rank, K] and b [E, rank, N], fp16 or bf16")
+    (E, rank, K), N = a.shape, b.shape[2]
+    if expert_offsets.numel() != E + 1 or (scale is not None and scale.numel() != E):
+        raise MoeError("E = %d adapters take E + 1 offsets and E scales" % E)
+    if perm_src is None and (k != 1 or by_assignment):
+        raise MoeError("without perm_src there is one row per row of x, in their order")
+    return E, rank, K, N, x_rows if perm_src is None else perm_src.numel()
+
+
+def moe_adapters_workspace_bytes(R: int, E: int, K: int, N: int, rank: int) -> int:
+    return int(load().moe_adapters_workspace_bytes(R, E, K, N, rank))
+
+
+def moe_adapters(x, a, b, expert_offsets, perm_src=None, k: int = 1, scale=None, by_assignment: bool = False, y=None, out=None, y_dtype=None, v=None, workspace=None):
+    """out[r] = y[r] + scale[e] * (A[e] x[perm_src[r] / k]) B[e] for the rows r of every adapter e; rows of no adapter are y's.
+
+    x [T, K] and y, out [R, N] may be slices of wider rows; out is y: in place.  by_assignment: y and out in the order of the assignments (with k = 1 the
+    tokens'), not the sorted one.  v: fp32 [R, rank], filled for moe_adapters_backward."""
+    E, rank, K, N, R = _adapter_sizes(a, b, expert_offsets, perm_src, k, scale, by_assignment, x.shape[0])
+    if out is None:
+        out = torch.empty(R, N, dtype=y_dtype or (x.dtype if y is None else y.dtype), device=x.device)
+    xp, xs = _rows(x, "x", K, (a.dtype,))
+    op, os_ = _rows(out, "out", N, _FLOATS)
+    yp, ys = (None, N) if y is None else _rows(y, "y", N, (out.dtype,))
+    if out.shape[0] != R or (y is not None and y.shape[0] != R) or (v is not None and v.shape != (R, rank)):
+        raise MoeError("y and out must have %d rows, v [%d, %d]" % (R, R, rank))
+    lib = load()
+    if workspace is None:
+        workspace = torch.empty(lib.moe_adapters_workspace_bytes(R, E, K, N, rank), dtype=torch.uint8, device=x.device)
+    _check_device(x, a, b, expert_offsets, perm_src, scale, y, out, v, workspace)
+    rc = lib.moe_adapters(xp, _DT[x.dtype], xs, x.shape[0], _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E, K, N, rank,
+                          _ptr(a, x.dtype, "a"), _ptr(b, x.dtype, "b"), _ptr(scale, torch.float32, "scale"), int(by_assignment), yp, ys, op, os_, _DT[out.dtype],
+                          _ptr(v, torch.float32, "v"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    _check(rc, "moe_adapters")
+    return out
+
+
+def moe_adapters_backward(dy, x, a, b, v, expert_offsets, perm_src=None, k: int = 1, scale=None, by_assignment: bool = False, need=(True, True, True), grad_dtype=None,
+                          out=(None, None, None), workspace=None):
+    """(dx, da, db) of dy [R, N], ordered as y in moe_adapters; `need` says which of them (None in the place of the others).
+
+    dx [R, K] in x's type and dy's order, 0 for rows of no adapter; da, db like a, b in grad_dtype (theirs).  v is the forward call's (needed for db), x is needed for da."""
+    E, rank, K, N, R = _adapter_sizes(a, b, expert_offsets, perm_src, k, scale, by_assignment, dy.shape[0])
+    dyp, dys = _rows(dy, "dy", N, _FLOATS)
+    xp, xs = (None, K) if x is None else _rows(x, "x", K, (a.dtype,))
+    if dy.shape[0] != R or (v is not None and v.shape != (R, rank)):
+        raise MoeError("dy must have %d rows, v be [%d, %d]" % (R, R, rank))
+    if (need[1] and x is None) or (need[2] and v is None):
+        raise MoeError("da needs x and db needs v")
+    dev, kind = dy.device, grad_dtype or a.dtype
+    dx, da, db = out
+    if need[0] and dx is None:
+        dx = torch.empty(R, K, dtype=a.dtype, device=dev)
+    if need[1] and da is None:
+        da = torch.empty(E, rank, K, dtype=kind, device=dev)
+    if need[2] and db is None:
+        db = torch.empty(E, rank, N, dtype=kind, device=dev)
+    if not (need[0] and need[1] and need[2]):
+        dx, da, db = (t if n else None for t, n in zip((dx, da, db), need))
+    dxp, dxs = (None, K) if dx is None else _rows(dx, "dx", K, (a.dtype,))
+    if (dx is not None and dx.shape[0] != R) or (da is not None and da.shape != a.shape) or (db is not None and db.shape != b.shape):
+        raise MoeError("dx must be [%d, %d], da like a and db like b" % (R, K))
+    if da is not None and db is not None and da.dtype != db.dtype:
+        raise MoeError("da and db must have one dtype")
+    grads = da if da is not None else db
+    T = R // k if x is None else x.shape[0]
+    lib = load()
+    if workspace is None:
+        workspace = torch.empty(lib.moe_adapters_workspace_bytes(R, E, K, N, rank), dtype=torch.uint8, device=dev)
+    _check_device(dy, x, a, b, v, expert_offsets, perm_src, scale, dx, da, db, workspace)
+    rc = lib.moe_adapters_backward(dyp, _DT[dy.dtype], dys, xp, _DT[a.dtype], xs, T, _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"),
+                                   R, E, K, N, rank, _ptr(a, a.dtype, "a"), _ptr(b, a.dtype, "b"), _ptr(scale, torch.float32, "scale"), int(by_assignment),
+                                   _ptr(v, torch.float32, "v"), dxp, dxs, _ptr(da, _FLOATS, "da"), _ptr(db, _FLOATS, "db"), _DT[a.dtype if grads is None else grads.dtype],
+                                   _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    _check(rc, "moe_adapters_backward")
+    return dx, da, db
+
+
+# ---- AdamW -----------------------------------------------------------------------------------------------------------------------------
+
+def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, copies=None):
+    """An AdamW step over lists of tensors, in place (include/moe_wq.h).
+
+    params of one type, grads of one type.  exp_avg and exp_avg_sq: fp32 tensors, or pairs (codes uint8 [n], scales uint8 [ceil(n/32)]) for states in 8 bits, of the moment and
+    of the second one's root.  step: the step's number from 1 on, or an int32 CUDA tensor that holds it.  copies: 16-bit copies of fp32 params to be written as well."""
+    count = len(params)
+    if not count == len(grads) == len(exp_avg) == len(exp_avg_sq) or (copies is not None and len(copies) != count):
+        raise MoeError("params, grads, exp_avg, exp_avg_sq and copies must be lists of one length")
+    if not count:
+        return
+    bits = 8 if isinstance(exp_avg[0], (tuple, list)) else 32
+    pd, gd, cd = params[0].dtype, grads[0].dtype, copies[0].dtype if copies is not None else None
+    here = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    flat, seen = [], set()
+    for i in range(count):
+        p, g = params[i], grads[i]
+        n = p.numel()
+        buffers = [p, g]
+        if bits == 8:
+            (mc, ms), (vc, vs) = exp_avg[i], exp_avg_sq[i]
+            blocks = (n + 31) // 32
+            if mc.numel() != n or vc.numel() != n or ms.numel() != blocks or vs.numel() != blocks:
+                raise MoeError("states of tensor %d must be %d codes and %d scales" % (i, n, blocks))
+            if not (mc.dtype is vc.dtype is ms.dtype is vs.dtype is torch.uint8):
+                raise MoeError("states of tensor %d must be uint8" % i)
+            buffers += (mc, vc, ms, vs)
+        else:
+            m, v = exp_avg[i], exp_avg_sq[i]
+            if m.numel() != n or v.numel() != n or m.dtype is not torch.float32 or v.dtype is not torch.float32:
+                raise MoeError("states of tensor %d must be fp32 and have its %d values" % (i, n))
+            buffers += (m, v)
+        if g.numel() != n or p.dtype is not pd or g.dtype is not gd:
+            raise MoeError("tensor %d: parameters must be of one type, and gradients, of the same sizes" % i)
+        if copies is not None:
+            if copies[i].numel() != n or copies[i].dtype is not cd:
+                raise MoeError("copy %d must have %d values, and the type of the others" % (i, n))
+            buffers.append(copies[i])
+        at = [t.data_ptr() for t in buffers]
+        for t in buffers:
+            if t.get_device() != here or not t.is_contiguous():
+                raise MoeError("tensor %d: buffers must be contiguous and on the current CUDA device" % i)
+        flat += at[:4]
+        flat += (at[4], at[5]) if bits == 8 else (0, 0)
+        flat += (at[-1] if copies is not None else 0, n)
+        if n and at[0] in seen:
+            raise MoeError("tensor %d is in the list twice" % i)
+        seen.add(at[0])
+    on_device = isinstance(step, torch.Tensor)
+    if on_device:
+        if step.numel() != 1:
+            raise MoeError("step must be one number")
+        _check_device(step)
+    if pd not in _DT or gd not in _DT or (cd is not None and cd not in (torch.float16, torch.bfloat16)):
+        raise MoeError("parameters and gradients must be fp16, bf16 or fp32, copies fp16 or bf16")
+    table = (ctypes.c_int64 * len(flat))(*flat)
+    rc = load().moe_adamw(ctypes.addressof(table), count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits, lr, betas[0], betas[1], eps, weight_decay, grad_scale,
+                          1 if on_device else step, _ptr(step, torch.int32, "step") if on_device else None, _stream())
+    _check(rc, "moe_adamw")
+
+
+def moe_adamw_state(codes, scales, dtype=torch.float32, out=None):
+    """The values of a state in 8 bits: codes uint8 [n], scales uint8 [ceil(n/32)] -> [n]."""
+    n = codes.numel()
+    if scales.numel() != (n + 31) // 32:
+        raise MoeError("%d codes take %d scales" % (n, (n + 31) // 32))
+    if out is None:
+        out = torch.empty(n, dtype=dtype, device=codes.device)
+    elif out.numel() != n:
+        raise MoeError("out must have %d values" % n)
+    _check_device(codes, scales, out)
+    rc = load().moe_adamw_state(_ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), n, _ptr(out, _FLOATS, "out"), _DT[out.dtype], _stream())
+    _check(rc, "moe_adamw_state")
     return out

@@ -1,0 +1,195 @@
+"""What the calls that layers are tuned with refuse on the host, before anything is launched: the exchange's gradient, adapters, AdamW."""
+import ctypes
+
+import pytest
+import torch
+
+from launches import P as PTR, record
+from paper_2211_10017_amd import binding as B
+
+P, ODD = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1008)          # never dereferenced: validation fails first
+OK, ARG, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
+F16, BF16, F32 = 0, 1, 2
+MOST = 2 ** 31 - 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return B.load()
+
+
+def test_exchange_refusals(lib):
+    def combine(dout=P, odt=F32, y=P, ydt=F16, inv=P, scale=P, T=4, k=2, d=64, R=8, dy=P, ds=P):
+        return lib.moe_combine_backward(dout, odt, y, ydt, inv, scale, None, T, k, d, R, dy, ds, None)
+
+    def permute(g=P, gdt=F16, inv=P, T=4, k=2, d=64, R=8, dx=P, dt=F32):
+        return lib.moe_permute_backward(g, gdt, inv, None, T, k, d, R, dx, dt, None)
+
+    for name in ("dout", "y", "inv", "scale", "dy", "ds"):
+        assert combine(**{name: None}) == ARG and b"NULL" in lib.moe_last_error(), name
+    for name in ("dout", "y", "dy"):
+        assert combine(**{name: ODD}) == ARG and b"aligned" in lib.moe_last_error(), name
+    for name in ("g", "inv", "dx"):
+        assert permute(**{name: None}) == ARG and b"NULL" in lib.moe_last_error(), name
+    for name in ("g", "dx"):
+        assert permute(**{name: ODD}) == ARG, name
+    for call in (combine, permute):
+        for bad in (dict(T=-1), dict(k=0), dict(d=0), dict(d=60), dict(R=-1), dict(T=2 ** 30, k=2)):
+            assert call(**bad) == ARG, bad
+        assert call(T=0, inv=None) == OK                            # empty buffers may be NULL
+    assert combine(odt=3) == UNSUPPORTED and combine(ydt=-1) == UNSUPPORTED and permute(gdt=3) == UNSUPPORTED and permute(dt=7) == UNSUPPORTED
+
+
+def _adapters(lib, x=P, dt=F16, xs=64, T=4, perm=P, k=2, off=P, R=8, E=3, K=64, N=72, rank=8, a=P, b=P, by=0, y=P, ys=72, out=P, os=72, ydt=F16, v=P, ws=P, size=1 << 40):
+    return lib.moe_adapters(x, dt, xs, T, perm, k, off, R, E, K, N, rank, a, b, P, by, y, ys, out, os, ydt, v, ws, size, None)
+
+
+def _backward(lib, dy=P, ydt=F16, dys=72, x=P, dt=F16, xs=64, T=4, perm=P, k=2, off=P, R=8, E=3, K=64, N=72, rank=8, a=P, b=P, by=0, v=P, dx=P, dxs=64, da=P, db=P, gdt=F32, ws=P,
+              size=1 << 40):
+    return lib.moe_adapters_backward(dy, ydt, dys, x, dt, xs, T, perm, k, off, R, E, K, N, rank, a, b, P, by, v, dx, dxs, da, db, gdt, ws, size, None)
+
+
+def test_adapter_refusals(lib):
+    for call in (_adapters, _backward):
+        for bad in (dict(T=-1), dict(R=-1), dict(k=0), dict(E=0), dict(K=0), dict(N=-8), dict(K=60, xs=60), dict(N=68), dict(rank=0), dict(R=7), dict(T=5), dict(perm=None), dict(off=None),
+                    dict(a=None), dict(b=None), dict(a=ODD), dict(b=ODD), dict(x=None), dict(x=ODD), dict(xs=56), dict(xs=68), dict(v=ODD), dict(ws=ODD), dict(perm=None, k=1, by=1, R=4)):
+            assert call(lib, **bad) == ARG, (call.__name__, bad, lib.moe_last_error())
+        for bad in (dict(rank=129), dict(E=4097), dict(dt=F32), dict(ydt=4), dict(K=2 ** 24 + 8, xs=2 ** 24 + 8), dict(R=2 ** 30, T=2 ** 29)):
+            assert call(lib, **bad) == UNSUPPORTED, (call.__name__, bad)
+        assert call(lib, ws=None) == WORKSPACE and call(lib, size=15) == WORKSPACE and b"workspace" in lib.moe_last_error()
+    for bad in (dict(y=ODD), dict(out=ODD), dict(out=None), dict(ys=64), dict(os=64), dict(ys=76), dict(ys=80)):      # (the last: in place with two strides)
+        assert _adapters(lib, **bad) == ARG, bad
+    for bad in (dict(dy=None), dict(dy=ODD), dict(dys=64), dict(v=None), dict(dx=ODD), dict(dxs=56), dict(da=ODD), dict(db=ODD)):
+        assert _backward(lib, **bad) == ARG, bad
+    assert _backward(lib, gdt=3) == UNSUPPORTED
+    assert _adapters(lib, T=0, R=0, x=None, y=None, out=None, ws=None, size=0, perm=P) == OK
+
+
+def test_adapter_workspaces(lib):
+    q = lib.moe_adapters_workspace_bytes
+    assert q(0, 4, 64, 64, 8) == 0 and q(8, 0, 64, 64, 8) == 0
+    assert q(100, 4, 64, 64, 8) >= 100 * 8 * 4
+    need = q(8, 3, 64, 72, 8)
+    assert _adapters(lib, size=need - 1) == WORKSPACE and _backward(lib, size=need - 1) == WORKSPACE
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "ms", "vs", "copy")] + [("n", ctypes.c_int64)]
+
+
+def test_adamw_refusals(lib):
+    def call(count=1, pd=F32, gd=F32, cd=-1, bits=32, lr=1e-3, b1=0.9, b2=0.99, eps=1e-8, wd=0.0, gs=1.0, step=1, table=None, **fields):
+        t = Tensor(*[0x1000] * 7, 64)
+        for name, value in fields.items():
+            setattr(t, name, value)
+        return lib.moe_adamw(ctypes.byref(t) if table is None else table, count, pd, gd, cd, bits, lr, b1, b2, eps, wd, gs, step, None, None)
+
+    nan, inf = float("nan"), float("inf")
+    for bad in (dict(count=-1), dict(step=0), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=nan), dict(lr=-1.0), dict(lr=nan), dict(lr=inf), dict(eps=-1e-8), dict(eps=inf), dict(wd=-1.0),
+                dict(gs=inf), dict(gs=nan), dict(n=-1), dict(p=0), dict(g=0), dict(m=0), dict(v=0), dict(bits=8, ms=0), dict(bits=8, vs=0), dict(cd=F16, copy=0), dict(p=0x1002),
+                dict(g=0x1001, gd=F16), dict(m=0x1002), dict(cd=BF16, copy=0x1001)):
+        assert call(**bad) == ARG, bad
+    for bad in (dict(pd=3), dict(gd=-1), dict(cd=F32), dict(cd=F16, pd=BF16), dict(bits=16), dict(n=2 ** 40)):
+        assert call(**bad) == UNSUPPORTED, bad
+    assert lib.moe_adamw(None, 1, F32, F32, -1, 32, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1.0, 1, None, None) == ARG
+    assert lib.moe_adamw(None, 0, F32, F32, -1, 32, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1.0, 1, None, None) == OK and call(n=0, p=0) == OK
+    state = lambda codes=P, scales=P, n=64, out=P, dt=F32: lib.moe_adamw_state(codes, scales, n, out, dt, None)  # noqa: E731
+    assert state(n=-1) == ARG and state(codes=None) == ARG and state(scales=None) == ARG and state(out=None) == ARG and state(out=ctypes.c_void_p(0x1002)) == ARG
+    assert state(dt=5) == UNSUPPORTED and state(n=0, codes=None) == OK
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """The binding with a library that takes every call, on tensors of the CPU."""
+    called = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: called.append(name) or 0
+
+    monkeypatch.setattr(B, "load", lambda: Library())
+    monkeypatch.setattr(B, "_stream", lambda: 0)
+    monkeypatch.setattr(B, "_raw_device", lambda: -1)                # (where a tensor of the CPU says it is)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
+    return called
+
+
+def test_binding_refuses_shapes_that_do_not_fit(on_host):
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt)  # noqa: E731
+    h, i32 = torch.float16, torch.int32
+    T, k, d, R = 4, 2, 64, 8
+    combine = dict(dout=z(T, d), y_perm=z(R, d, dt=h), inv_perm=z(R, dt=i32), expert_scale=z(T, k))
+    B.moe_combine_backward(**combine)
+    for bad in (dict(dout=z(T, d + 8)), dict(dout=z(T + 1, d)), dict(dout=z(T, 2 * d)[:, ::2]), dict(inv_perm=z(R - 1, dt=i32)), dict(inv_perm=z(R)), dict(expert_scale=z(T, k, dt=h)),
+                dict(expert_scale=z(R)), dict(y_perm=z(R, d, dt=i32)), dict(out=(z(R, d), z(T, k))), dict(out=(z(R - 1, d, dt=h), z(T, k))), dict(active_rows=z(0, dt=i32))):
+        with pytest.raises(B.MoeError):
+            B.moe_combine_backward(**dict(combine, **bad))
+    B.moe_permute_backward(z(R, d), z(R, dt=i32), T, k)
+    for bad in ((z(R * d), z(R, dt=i32), T, k), (z(R, d), z(R, dt=i32), T + 1, k), (z(R, d), z(R), T, k)):
+        with pytest.raises(B.MoeError):
+            B.moe_permute_backward(*bad)
+    with pytest.raises(B.MoeError):
+        B.moe_permute_backward(z(R, d), z(R, dt=i32), T, k, out=z(T, d + 8))
+    E, rank, K, N = 3, 8, 64, 72
+    make = lambda: dict(x=z(T, K, dt=h), a=z(E, rank, K, dt=h), b=z(E, rank, N, dt=h), expert_offsets=z(E + 1, dt=i32), perm_src=z(R, dt=i32), k=k, scale=z(E), y=z(R, N), out=z(R, N),  # noqa: E731
+                        v=z(R, rank), workspace=z(4096, dt=torch.uint8))
+    B.moe_adapters(**make())
+    B.moe_adapters(**dict(make(), x=z(T, 2 * K, dt=h)[:, K:]))         # a slice of wider rows
+    for bad in (dict(x=z(T, K)), dict(x=z(T, K + 8, dt=h)), dict(x=z(T, 2 * K, dt=h)[:, ::2]), dict(a=z(E, rank, K)), dict(b=z(E, rank + 1, N, dt=h)), dict(b=z(E, rank, N, dt=torch.bfloat16)),
+                dict(expert_offsets=z(E, dt=i32)), dict(scale=z(E + 1)), dict(scale=z(E, dt=h)), dict(perm_src=z(R)), dict(perm_src=None), dict(y=z(R - 1, N)), dict(y=z(R, N, dt=h)),
+                dict(out=z(R + 1, N)), dict(out=z(R, N, dt=i32)), dict(v=z(R, rank + 1)), dict(v=z(R, rank, dt=h)), dict(a=z(E * rank, K, dt=h)), dict(workspace=z(4096))):
+        with pytest.raises(B.MoeError):
+            B.moe_adapters(**dict(make(), **bad))
+    back = lambda: dict(dy=z(R, N), x=z(T, K, dt=h), a=z(E, rank, K, dt=h), b=z(E, rank, N, dt=h), v=z(R, rank), expert_offsets=z(E + 1, dt=i32), perm_src=z(R, dt=i32), k=k,  # noqa: E731
+                        workspace=z(4096, dt=torch.uint8))
+    B.moe_adapters_backward(**back())
+    for bad in (dict(dy=z(R + 1, N)), dict(dy=z(R, N, dt=i32)), dict(x=None), dict(v=None), dict(v=z(R, rank, dt=h)), dict(x=z(T, K)), dict(out=(z(R, K), None, None)),
+                dict(out=(None, z(E, rank, K), z(E, rank, N, dt=h))), dict(out=(None, z(E, rank, K + 8), None))):
+        with pytest.raises(B.MoeError):
+            B.moe_adapters_backward(**dict(back(), **bad))
+
+
+def test_binding_refuses_lists_that_do_not_fit(on_host):
+    z = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt)  # noqa: E731
+    u8 = torch.uint8
+    make = lambda: [[z(40), z(3)], [z(40), z(3)], [z(40), z(3)], [z(40), z(3)], 1]  # noqa: E731
+    B.moe_adamw(*make())
+    B.moe_adamw([], [], [], [], 1)
+    with pytest.raises(B.MoeError, match="twice"):
+        p = z(40)
+        B.moe_adamw([p, p], [z(40), z(40)], [z(40), z(40)], [z(40), z(40)], 1)
+    for at, value in ((0, [z(40)]), (1, [z(40), z(4)]), (1, [z(40), z(3, torch.float16)]), (2, [z(40), z(3, torch.float16)]), (3, [z(41), z(3)]), (0, [z(40), z(3, torch.float64)]),
+                      (1, [z(80)[::2], z(3)]), (4, z(2, torch.int32)), (4, z(1)), (2, [(z(40, u8), z(2, u8))] * 2)):
+        args = make()
+        args[at] = value
+        with pytest.raises((B.MoeError, ValueError, TypeError)):
+            B.moe_adamw(*args)
+    eight = lambda: [(z(40, u8), z(2, u8)), (z(3, u8), z(1, u8))]  # noqa: E731
+    B.moe_adamw([z(40), z(3)], [z(40), z(3)], eight(), eight(), 1, copies=[z(40, torch.float16), z(3, torch.float16)])
+    for m in ([(z(40, u8), z(1, u8)), (z(3, u8), z(1, u8))], [(z(39, u8), z(2, u8)), (z(3, u8), z(1, u8))], [(z(40), z(2, u8)), (z(3, u8), z(1, u8))]):
+        with pytest.raises(B.MoeError):
+            B.moe_adamw([z(40), z(3)], [z(40), z(3)], m, eight(), 1)
+    for copies in ([z(40, torch.float16)], [z(40, torch.float16), z(4, torch.float16)], [z(40), z(3)], [z(40, torch.float16), z(3, torch.bfloat16)]):
+        with pytest.raises(B.MoeError):
+            B.moe_adamw([z(40), z(3)], [z(40), z(3)], eight(), eight(), 1, copies=copies)
+    with pytest.raises(B.MoeError):
+        B.moe_adamw_state(z(40, u8), z(1, u8))
+
+
+def test_binding_refuses_another_device(on_host, monkeypatch):
+    monkeypatch.setattr(B, "_raw_device", lambda: 1)
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt)  # noqa: E731
+    i32 = torch.int32
+    for call in (lambda: B.moe_combine_backward(z(2, 8), z(2, 8), z(2, dt=i32), z(2, 1)), lambda: B.moe_permute_backward(z(2, 8), z(2, dt=i32), 2, 1),
+                 lambda: B.moe_adapters(z(2, 8, dt=torch.float16), z(1, 4, 8, dt=torch.float16), z(1, 4, 8, dt=torch.float16), z(2, dt=i32), workspace=z(64, dt=torch.uint8)),
+                 lambda: B.moe_adamw([z(4)], [z(4)], [z(4)], [z(4)], 1), lambda: B.moe_adamw_state(z(4, dt=torch.uint8), z(1, dt=torch.uint8))):
+        with pytest.raises(B.MoeError, match="device"):
+            call()
+    assert not [name for name in on_host if not name.endswith("bytes")]
+
+
+def test_the_largest_batches_take_a_launch():
+    for T, d in ((1, 8), (2 ** 30, 8192)):
+        for call in (("moe_combine_backward", [PTR, F32, PTR, F16, PTR, PTR, None, T, 1, d, T, PTR, PTR, None]), ("moe_permute_backward", [PTR, F16, PTR, None, T, 1, d, T, PTR, F16, None])):
+            got = record([call])[0]
+            assert got.rc == OK and len(got.launches) == 1 and 0 < got.launches[0].grid[0] * got.launches[0].block < 2 ** 32
