@@ -451,13 +451,13 @@ int moe_permute_backward(const void *dx_perm, int perm_dtype, const int32_t *inv
  *   dx[r] = u[r] A[e] in dtype, ordered as y, 0 for rows of no adapter (with more than one row per token moe_permute_backward adds them up)
  *   da[e] = sum_r u[r] x[t]^T,  db[e] = scale[e] * sum_r v[r] dy[r]^T  in grad_dtype, 0 for adapters without rows; sums over rows in a fixed order
  *   dx, da, db may each be NULL (x is read for da only, v for db only).
- * Products are summed in fp32, v and u kept in it.  Strides and K, N are multiples of 8, K and N at most 2^24, 1 <= rank <= 128, E <= 4096, R < 2^24.  expert_offsets and
+ * Products are summed in fp32, v and u kept in it.  Strides and K, N are multiples of 8, K and N at most 2^20, 1 <= rank <= 128, E <= 4096.  expert_offsets and
  * perm_src are forced into range: wrong contents give wrong results but no stray access.
  */
-size_t moe_adapters_workspace_bytes(int R, int E, int K, int N, int rank);
 int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k, const int32_t *expert_offsets, int R, int E, int K, int N, int rank,
                  const void *a, const void *b, const float *scale, int by_assignment, const void *y, int64_t y_stride, void *out, int64_t out_stride, int y_dtype, float *v,
-                 void *workspace, size_t workspace_bytes, void *stream);
+                 void *stream);
+size_t moe_adapters_backward_workspace_bytes(int R, int E, int K, int N, int rank);
 int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_stride, const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k,
                           const int32_t *expert_offsets, int R, int E, int K, int N, int rank, const void *a, const void *b, const float *scale, int by_assignment,
                           const float *v, void *dx, int64_t dx_stride, void *da, void *db, int grad_dtype, void *workspace, size_t workspace_bytes, void *stream);

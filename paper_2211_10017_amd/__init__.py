@@ -15,5 +15,5 @@ from .binding import (MoeError, moe_combine, moe_gate_topk, moe_grouped_ffn_wq, 
 from .binding import (moe_balance_loss, moe_balance_loss_backward, moe_grouped_ffn_mx4,  # noqa: E402,F401
                       moe_grouped_ffn_mx4_workspace_bytes, moe_grouped_gemm_mx4, moe_mx4_dequantize, moe_mx4_quantize_experts,
                       moe_mx4_quantize_rows)
-from .binding import (moe_adamw, moe_adamw_state, moe_adapters, moe_adapters_backward, moe_adapters_workspace_bytes,  # noqa: E402,F401
+from .binding import (moe_adamw, moe_adamw_state, moe_adapters, moe_adapters_backward, moe_adapters_backward_workspace_bytes,  # noqa: E402,F401
                       moe_combine_backward, moe_permute_backward)

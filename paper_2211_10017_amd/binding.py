@@ -29,7 +29,7 @@ EXPORTS = ["moe_last_error", "moe_last_ffn_kernels", "moe_device_info", "moe_abi
            "moe_mx4_quantize_rows", "moe_mx4_quantize_experts", "moe_mx4_dequantize", "moe_grouped_gemm_mx4",
            "moe_grouped_ffn_mx4_workspace_bytes", "moe_grouped_ffn_mx4",
            "moe_balance_loss_workspace_bytes", "moe_balance_loss", "moe_balance_loss_backward",
-           "moe_combine_backward", "moe_permute_backward", "moe_adapters_workspace_bytes", "moe_adapters", "moe_adapters_backward",
+           "moe_combine_backward", "moe_permute_backward", "moe_adapters", "moe_adapters_backward_workspace_bytes", "moe_adapters_backward",
            "moe_adamw", "moe_adamw_state"]
 
 LAYER_MAX_EXPERTS = 256   # experts of a whole layer call: moe_gate_topk's limit (moe_permute: 1024, the FFN: 4096)
@@ -135,10 +135,10 @@ def load():
     lib.moe_combine_backward.argtypes = [vp, i, vp, i, vp, vp, vp, i, i, i, i, vp, vp, vp]
     lib.moe_permute_backward.restype = i
     lib.moe_permute_backward.argtypes = [vp, i, vp, vp, i, i, i, i, vp, i, vp]
-    lib.moe_adapters_workspace_bytes.restype = sz
-    lib.moe_adapters_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.moe_adapters_backward_workspace_bytes.restype = sz
+    lib.moe_adapters_backward_workspace_bytes.argtypes = [i, i, i, i, i]
     lib.moe_adapters.restype = i
-    lib.moe_adapters.argtypes = [vp, i, i64, i, vp, i, vp, i, i, i, i, i, vp, vp, vp, i, vp, i64, vp, i64, i, vp, vp, sz, vp]
+    lib.moe_adapters.argtypes = [vp, i, i64, i, vp, i, vp, i, i, i, i, i, vp, vp, vp, i, vp, i64, vp, i64, i, vp, vp]
     lib.moe_adapters_backward.restype = i
     lib.moe_adapters_backward.argtypes = [vp, i, i64, vp, i, i64, i, vp, i, vp, i, i, i, i, i, vp, vp, vp, i, vp, vp, i64, vp, vp, i, vp, sz, vp]
     d = ctypes.c_double
@@ -733,11 +733,11 @@ def _adapter_sizes(a, b, expert_offsets, perm_src, k, scale, by_assignment, x_ro
     return E, rank, K, N, x_rows if perm_src is None else perm_src.numel()
 
 
-def moe_adapters_workspace_bytes(R: int, E: int, K: int, N: int, rank: int) -> int:
-    return int(load().moe_adapters_workspace_bytes(R, E, K, N, rank))
+def moe_adapters_backward_workspace_bytes(R: int, E: int, K: int, N: int, rank: int) -> int:
+    return int(load().moe_adapters_backward_workspace_bytes(R, E, K, N, rank))
 
 
-def moe_adapters(x, a, b, expert_offsets, perm_src=None, k: int = 1, scale=None, by_assignment: bool = False, y=None, out=None, y_dtype=None, v=None, workspace=None):
+def moe_adapters(x, a, b, expert_offsets, perm_src=None, k: int = 1, scale=None, by_assignment: bool = False, y=None, out=None, y_dtype=None, v=None):
     """out[r] = y[r] + scale[e] * (A[e] x[perm_src[r] / k]) B[e] for the rows r of every adapter e; rows of no adapter are y's.
 
     x [T, K] and y, out [R, N] may be slices of wider rows; out is y: in place.  by_assignment: y and out in the order of the assignments (with k = 1 the
@@ -750,13 +750,10 @@ def moe_adapters(x, a, b, expert_offsets, perm_src=None, k: int = 1, scale=None,
     yp, ys = (None, N) if y is None else _rows(y, "y", N, (out.dtype,))
     if out.shape[0] != R or (y is not None and y.shape[0] != R) or (v is not None and v.shape != (R, rank)):
         raise MoeError("y and out must have %d rows, v [%d, %d]" % (R, R, rank))
-    lib = load()
-    if workspace is None:
-        workspace = torch.empty(lib.moe_adapters_workspace_bytes(R, E, K, N, rank), dtype=torch.uint8, device=x.device)
-    _check_device(x, a, b, expert_offsets, perm_src, scale, y, out, v, workspace)
-    rc = lib.moe_adapters(xp, _DT[x.dtype], xs, x.shape[0], _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E, K, N, rank,
+    _check_device(x, a, b, expert_offsets, perm_src, scale, y, out, v)
+    rc = load().moe_adapters(xp, _DT[x.dtype], xs, x.shape[0], _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E, K, N, rank,
                           _ptr(a, x.dtype, "a"), _ptr(b, x.dtype, "b"), _ptr(scale, torch.float32, "scale"), int(by_assignment), yp, ys, op, os_, _DT[out.dtype],
-                          _ptr(v, torch.float32, "v"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+                          _ptr(v, torch.float32, "v"), _stream())
     _check(rc, "moe_adapters")
     return out
 
@@ -792,7 +789,7 @@ def moe_adapters_backward(dy, x, a, b, v, expert_offsets, perm_src=None, k: int 
     T = R // k if x is None else x.shape[0]
     lib = load()
     if workspace is None:
-        workspace = torch.empty(lib.moe_adapters_workspace_bytes(R, E, K, N, rank), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(lib.moe_adapters_backward_workspace_bytes(R, E, K, N, rank), dtype=torch.uint8, device=dev)
     _check_device(dy, x, a, b, v, expert_offsets, perm_src, scale, dx, da, db, workspace)
     rc = lib.moe_adapters_backward(dyp, _DT[dy.dtype], dys, xp, _DT[a.dtype], xs, T, _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"),
                                    R, E, K, N, rank, _ptr(a, a.dtype, "a"), _ptr(b, a.dtype, "b"), _ptr(scale, torch.float32, "scale"), int(by_assignment),

@@ -1,0 +1,111 @@
+// What the adapters' kernels share: arguments, and how coefficients go into 16-bit products.
+#pragma once
+
+#include "moe_rows.h"
+
+namespace moe {
+
+constexpr int kAdapterMostRank = 128, kAdapterMostAdapters = 4096;
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+
+// Where row r of the sorted order is found: in rows of tokens (source / div), of assignments (source), or in place.
+struct RowMap {
+    const int32_t *source;      // perm_src or null
+    int div;                    // k for tokens, 1 for assignments
+    int rows;                   // of the buffer
+    int64_t stride;
+
+    __device__ inline int row(int r) const { return source ? min(max(source[r] / div, 0), rows - 1) : r; }
+};
+
+// coef[r] = A[e] x[r] (for phase two times scale[e]), out[r] = y[r] + coef[r] B[e]
+struct AdapterArgs {
+    const int32_t *offsets;     // [E + 1]
+    const float *scale;         // [E] or null
+    int R, E, K, N, rank;
+    const void *x, *a, *b;
+    RowMap x_map;
+    const void *y;              // or null; may be out
+    int64_t y_stride;
+    void *out;
+    RowMap out_map;             // of y as well, but for the stride
+    float *coef;                // [R, rank] or null
+    int coef_scaled;            // coef holds scale * (A x)
+    int ncol;                   // slices of N, each a block's
+    int width;                  // channels of a slice, a multiple of 64
+    int items;                  // blocks for rows of adapters; those behind them copy the others
+};
+
+// out[e][j] = scale sum_r coef[r][j] rows[r]
+struct OuterJob {
+    const void *rows;
+    RowMap map;
+    const float *coef;          // [R, rank]
+    const float *scale;         // [E] or null
+    void *out;                  // [E, rank, C] or null: no such job
+    int C, ncol;                // ncol: slices of 64 channels
+    int chunk;                  // rows of a block, a multiple of 32
+    float *part;                // [slots, rank, C]: sums of adapters with more than one chunk
+    int slots;                  // enough for every partition of the R rows
+};
+struct OuterArgs {
+    const int32_t *offsets;
+    int R, E, rank, out_dtype;
+    OuterJob job[2];
+    int first;                  // blocks of job 0
+    int join;                   // adapters that can have more than one chunk
+};
+
+int launch_adapter_f16(const AdapterArgs &p, int x_dtype, int out_dtype, hipStream_t s, const char *what);
+int launch_adapter_bf16(const AdapterArgs &p, int x_dtype, int out_dtype, hipStream_t s, const char *what);
+int launch_adapter_outer(const OuterArgs &p, int dtype0, int dtype1, hipStream_t s, const char *what);
+
+template <int DT>
+__device__ inline float4_t product16(u32x4_t a, u32x4_t b, float4_t c)          // 16 x 16 x 32
+{
+    if constexpr (DT == MOE_BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+}
+
+// A coefficient as two 16-bit numbers, hi the nearest and lo the nearest to what is left: off by at most 2^-16 (bf16) or 2^-22 (fp16) of it, where one alone would be off by 2^-8
+// and 2^-11, as much as the whole result may be.  (fp16: of numbers that a power of two has brought into range.)
+template <int DT>
+struct Split {
+    uint16_t hi, lo;
+    __device__ inline explicit Split(float c)
+    {
+        if constexpr (DT == MOE_BF16) {
+            const __bf16 h = (__bf16)c;
+            const float left = c - (float)h;
+            hi = __builtin_bit_cast(uint16_t, h), lo = __builtin_bit_cast(uint16_t, (__bf16)(left == left ? left : 0.0f));      // (an infinity leaves none)
+        } else {
+            const _Float16 h = (_Float16)c;
+            const float left = c - (float)h;
+            hi = __builtin_bit_cast(uint16_t, h), lo = __builtin_bit_cast(uint16_t, (_Float16)(left == left ? left : 0.0f));
+        }
+    }
+};
+
+// The power of two that numbers of up to `most` are divided by before they are split in fp16: the largest then lies in [2^14, 2^15) (infinities stay infinities).
+__device__ inline int split_exponent(float most)
+{
+    const int e = (int)(__float_as_uint(most) >> 23) - 127 - 14;
+    return min(max(e, -100), 100);
+}
+__device__ inline float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }       // -126 <= e <= 127
+
+// Four columns of eight rows, a row's four as two words, become the columns: column t's eight values as four words.
+__device__ inline void transpose_8x4(const uint2 (&row)[8], u32x4_t (&col)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        col[0][i] = __builtin_amdgcn_perm(row[2 * i + 1].x, row[2 * i].x, 0x05040100u);
+        col[1][i] = __builtin_amdgcn_perm(row[2 * i + 1].x, row[2 * i].x, 0x07060302u);
+        col[2][i] = __builtin_amdgcn_perm(row[2 * i + 1].y, row[2 * i].y, 0x05040100u);
+        col[3][i] = __builtin_amdgcn_perm(row[2 * i + 1].y, row[2 * i].y, 0x07060302u);
+    }
+}
+
+}  // namespace moe

@@ -3,166 +3,11 @@
 //   v_r = A_e x_t,  y_r += s_e B_e^T v_r                                        (row r of adapter e, of token t = perm_src[r] / k)
 //   u_r = s_e B_e dy_r,  dx_r = A_e^T u_r,  dA_e = sum_r u_r x_t^T,  dB_e = s_e sum_r v_r dy_r^T
 //
-// Both matrices lie by rank, [rank, K] and [rank, N], so that three products make up all of it: rows times a matrix along their channels ("shrink": v, u), coefficients times a matrix
-// along the rank ("expand": y, dx), and coefficients times rows along an adapter's rows ("outer": dA, dB).  Coefficients are kept in fp32.
-#include "moe_rows.h"
+// Both matrices lie by rank, [rank, K] and [rank, N], so that the way from dy to dx is the way from x to y with the matrices exchanged: one kernel (moe_adapters_kernel.h), which keeps
+// the coefficients v or u on chip between its two products and leaves them in fp32 for the backward pass and the gradients of the matrices (moe_adapters_outer.hip).
+#include "moe_adapters.h"
 
 namespace moe {
-
-constexpr int kAdapterMostRank = 128, kAdapterMostAdapters = 4096;
-
-// Where row r of the sorted order is found: in rows of tokens (source / k), of assignments (source), or in place.
-struct RowMap {
-    const int32_t *source;      // perm_src or null
-    int div;                    // k for tokens, 1 for assignments
-    int rows;                   // of the buffer
-    int64_t stride;
-
-    __device__ inline size_t at(int r) const { return (size_t)(source ? min(max(source[r] / div, 0), rows - 1) : r) * stride; }
-};
-
-struct AdapterArgs {
-    const int32_t *offsets;     // [E + 1]
-    const float *scale;         // [E] or null
-    int R, E, C, rank;          // C: channels
-    const void *rows;           // shrink, outer: what is multiplied; expand: what the product is added to, or null
-    RowMap map;
-    const void *w;              // [E, rank, C]
-    float *coef;                // [R, rank]: shrink writes it, expand and outer read it
-    void *out;                  // expand: rows, by out_map; outer: [E, rank, C]
-    RowMap out_map;
-};
-
-// Adapter of row r: the last one that begins at or before it; false for rows behind the last adapter's.
-__device__ inline bool adapter_of(const AdapterArgs &p, int r, int *e)
-{
-    int lo = 0, hi = p.E;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (p.offsets[mid] <= r) lo = mid;
-        else hi = mid;
-    }
-    *e = lo;
-    return p.offsets[lo] <= r && r < p.offsets[lo + 1];
-}
-
-// coef[r][j] = scale <rows[r], w[e][j]>
-template <int DT, int WDT>
-__global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs p)
-{
-    const int r = blockIdx.x, lane = threadIdx.x & 63;
-    int e;
-    if (!adapter_of(p, r, &e)) return;
-    const size_t at = p.map.at(r);
-    const float s = p.scale ? p.scale[e] : 1.0f;
-    for (int j = threadIdx.x >> 6; j < p.rank; j += 4) {
-        const size_t row = ((size_t)e * p.rank + j) * p.C;
-        float sum = 0.0f;
-        for (int c = lane * 8; c < p.C; c += 512) {
-            Raw<DT, 8> x;
-            Raw<WDT, 8> w;
-            x.load(p.rows, at + c), w.load(p.w, row + c);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(x.get(i), w.get(i), sum);
-        }
-        sum = wave_sum(sum);
-        if (lane == 0) p.coef[(size_t)r * p.rank + j] = s * sum;
-    }
-}
-
-// out[r] = rows[r] + scale sum_j coef[r][j] w[e][j]; rows of no adapter are copied where out is another buffer
-template <int DT, int WDT>
-__global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs p)
-{
-    const int r = blockIdx.x;
-    int e;
-    const bool live = adapter_of(p, r, &e);
-    if (!live && p.rows == p.out) return;
-    const size_t from = p.map.at(r), to = p.out_map.at(r);
-    const float s = p.scale ? p.scale[e] : 1.0f;
-    for (int c = threadIdx.x * 8; c < p.C; c += 2048) {
-        Raw<DT, 8> y;
-        if (p.rows) y.load(p.rows, from + c);
-        else y.clear();
-        if (live) {
-            float v[8] = {};
-            for (int j = 0; j < p.rank; ++j) {
-                const float f = p.coef[(size_t)r * p.rank + j] * s;
-                Raw<WDT, 8> w;
-                w.load(p.w, ((size_t)e * p.rank + j) * p.C + c);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = fmaf(f, w.get(i), v[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += y.get(i);
-            y.set(v);
-        }
-        y.store(p.out, to + c);
-    }
-}
-
-// out[e][j] = scale sum_r coef[r][j] rows[r]
-template <int DT, int ODT>
-__global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterArgs p)
-{
-    const int e = blockIdx.x, j = blockIdx.y;
-    int lo, hi;
-    expert_range(p.offsets, e, p.R, &lo, &hi);
-    const float s = p.scale ? p.scale[e] : 1.0f;
-    for (int c = threadIdx.x * 8; c < p.C; c += 2048) {
-        float v[8] = {};
-        for (int r = lo; r < hi; ++r) {
-            const float f = p.coef[(size_t)r * p.rank + j];
-            Raw<DT, 8> x;
-            x.load(p.rows, p.map.at(r) + c);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = fmaf(f, x.get(i), v[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= s;
-        Raw<ODT, 8> o;
-        o.set(v);
-        o.store(p.out, ((size_t)e * p.rank + j) * p.C + c);
-    }
-}
-
-static size_t coefficient_bytes(int R, int rank) { return round_up((size_t)R * rank * sizeof(float), 256); }
-
-template <class F>
-static int with_half(int dtype, F &&f)
-{
-    return dtype == MOE_F16 ? f(std::integral_constant<int, MOE_F16>{}) : f(std::integral_constant<int, MOE_BF16>{});
-}
-
-static int launch_shrink(const AdapterArgs &p, int dtype, int w_dtype, hipStream_t s, const char *what)
-{
-    return with_dtype(dtype, [&](auto d) {
-        return with_half(w_dtype, [&](auto w) {
-            hipLaunchKernelGGL((adapter_shrink_kernel<decltype(d)::value, decltype(w)::value>), dim3(p.R), dim3(256), 0, s, p);
-            return check_launch(what);
-        });
-    });
-}
-
-static int launch_expand(const AdapterArgs &p, int dtype, int w_dtype, hipStream_t s, const char *what)
-{
-    return with_dtype(dtype, [&](auto d) {
-        return with_half(w_dtype, [&](auto w) {
-            hipLaunchKernelGGL((adapter_expand_kernel<decltype(d)::value, decltype(w)::value>), dim3(p.R), dim3(256), 0, s, p);
-            return check_launch(what);
-        });
-    });
-}
-
-static int launch_outer(const AdapterArgs &p, int dtype, int out_dtype, hipStream_t s, const char *what)
-{
-    return with_dtype(dtype, [&](auto d) {
-        return with_dtype(out_dtype, [&](auto o) {
-            hipLaunchKernelGGL((adapter_outer_kernel<decltype(d)::value, decltype(o)::value>), dim3(p.E, p.rank), dim3(256), 0, s, p);
-            return check_launch(what);
-        });
-    });
-}
 
 struct AdapterCall {
     const char *what;
@@ -179,8 +24,7 @@ static int check_adapters(const AdapterCall &c)
     if (c.rank <= 0) return fail(MOE_ERR_INVALID_ARG, "%s: rank > 0 required", what);
     if (c.rank > kAdapterMostRank) return fail(MOE_ERR_UNSUPPORTED, "%s: rank %d above %d", what, c.rank, kAdapterMostRank);
     if (c.E > kAdapterMostAdapters) return fail(MOE_ERR_UNSUPPORTED, "%s: %d adapters, above %d", what, c.E, kAdapterMostAdapters);
-    if (c.K > 1 << 24 || c.N > 1 << 24) return fail(MOE_ERR_UNSUPPORTED, "%s: K and N of at most 2^24", what);
-    if (c.R >= 1 << 24) return fail(MOE_ERR_UNSUPPORTED, "%s: fewer than 2^24 rows", what);
+    if (c.K > 1 << 20 || c.N > 1 << 20) return fail(MOE_ERR_UNSUPPORTED, "%s: K and N of at most 2^20", what);
     if (c.dtype != MOE_F16 && c.dtype != MOE_BF16) return fail(MOE_ERR_UNSUPPORTED, "%s: x and the adapters must be fp16 or bf16", what);
     if (!known_dtype(c.other_dtype)) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
     if (!c.perm_src && c.by_assignment) return fail(MOE_ERR_INVALID_ARG, "%s: rows by assignment need perm_src", what);
@@ -198,17 +42,28 @@ static int check_rows(const char *what, const char *name, const void *p, int64_t
     return MOE_OK;
 }
 
-}  // namespace moe
-
-extern "C" size_t moe_adapters_workspace_bytes(int R, int E, int K, int N, int rank)
+// Rows of a wavefront's part of a matrix's gradient.  Enough parts to fill the chip (a part is 64 channels of `chunk` rows; two thousand wavefronts), as the sums of parts have to be
+// written and added up; at most 1024 rows, or an adapter that has much of the batch is one long chain, unless that would make more than 256 parts of it.
+static int outer_chunk(int R, int C)
 {
-    if (R <= 0 || E <= 0 || K <= 0 || N <= 0 || rank <= 0) return 0;
-    return moe::coefficient_bytes(R, rank);
+    const long even = (long)R * ((C + 63) / 64) / 2048, most = R / 256 > 1024 ? R / 256 : 1024;
+    const long rows = even < 64 ? 64 : even > most ? most : even;
+    return (int)((rows + 31) / 32 * 32);
 }
+
+static int part_slots(int R, int C) { return 2 * (R / outer_chunk(R, C)); }        // n rows in more than one chunk are at most 2 (n / chunk) of them
+static size_t part_bytes(int R, int C, int rank) { return (size_t)part_slots(R, C) * rank * C * sizeof(float); }
+
+static int launch_adapter(const AdapterArgs &p, int dtype, int x_dtype, int out_dtype, hipStream_t s, const char *what)
+{
+    return dtype == MOE_F16 ? launch_adapter_f16(p, x_dtype, out_dtype, s, what) : launch_adapter_bf16(p, x_dtype, out_dtype, s, what);
+}
+
+}  // namespace moe
 
 extern "C" int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k, const int32_t *expert_offsets, int R, int E, int K, int N, int rank,
                             const void *a, const void *b, const float *scale, int by_assignment, const void *y, int64_t y_stride, void *out, int64_t out_stride, int y_dtype, float *v,
-                            void *workspace, size_t workspace_bytes, void *stream)
+                            void *stream)
 {
     using namespace moe;
     const char *what = "moe_adapters";
@@ -221,16 +76,19 @@ extern "C" int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, c
     if (y)
         if (const int rc = check_rows(what, "y", y, y_stride, N)) return rc;
     if (y == out && y_stride != out_stride) return fail(MOE_ERR_INVALID_ARG, "%s: in place the strides of y and out are one", what);
-    const size_t need = moe_adapters_workspace_bytes(R, E, K, N, rank);
-    if (!workspace || workspace_bytes < need) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", what, need, workspace_bytes);
-    if (!aligned16(workspace) || !aligned16(v)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
-    const hipStream_t s = as_stream(stream);
-    const RowMap tokens{perm_src, k, T, x_stride}, y_map{by_assignment ? perm_src : nullptr, 1, R, y_stride}, out_map{by_assignment ? perm_src : nullptr, 1, R, out_stride};
-    float *coef = v ? v : (float *)workspace;
-    AdapterArgs p{expert_offsets, nullptr, R, E, K, rank, x, tokens, a, coef, nullptr, RowMap{}};
-    if (const int rc = launch_shrink(p, dtype, dtype, s, what)) return rc;
-    p = AdapterArgs{expert_offsets, scale, R, E, N, rank, y, y_map, b, coef, out, out_map};
-    return launch_expand(p, y_dtype, dtype, s, what);
+    AdapterArgs p{};
+    p.offsets = expert_offsets, p.scale = scale, p.R = R, p.E = E, p.K = K, p.N = N, p.rank = rank;
+    p.x = x, p.a = a, p.b = b, p.x_map = RowMap{perm_src, k, T, x_stride};
+    p.y = y, p.y_stride = y_stride, p.out = out, p.out_map = RowMap{by_assignment ? perm_src : nullptr, 1, R, out_stride};
+    p.coef = v, p.coef_scaled = 0;
+    return launch_adapter(p, dtype, dtype, y_dtype, as_stream(stream), what);
+}
+
+extern "C" size_t moe_adapters_backward_workspace_bytes(int R, int E, int K, int N, int rank)
+{
+    using namespace moe;
+    if (R <= 0 || E <= 0 || K <= 0 || N <= 0 || rank <= 0) return 0;
+    return round_up((size_t)R * rank * sizeof(float), 256) + round_up(part_bytes(R, K, rank), 256) + part_bytes(R, N, rank);
 }
 
 extern "C" int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_stride, const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k,
@@ -250,29 +108,25 @@ extern "C" int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_st
             if (const int rc = check_rows(what, "x", x, x_stride, K)) return rc;
         if (dx)
             if (const int rc = check_rows(what, "dx", dx, dx_stride, K)) return rc;
-        const size_t need = moe_adapters_workspace_bytes(R, E, K, N, rank);
+        const size_t need = moe_adapters_backward_workspace_bytes(R, E, K, N, rank);
         if (!workspace || workspace_bytes < need) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", what, need, workspace_bytes);
         if (!aligned16(workspace) || !aligned16(v)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     }
     const hipStream_t s = as_stream(stream);
-    const int32_t *assignments = by_assignment ? perm_src : nullptr;
-    const RowMap tokens{perm_src, k, T, x_stride}, dy_map{assignments, 1, R, dy_stride}, dx_map{assignments, 1, R, dx_stride};
-    float *u = (float *)workspace;
+    const RowMap tokens{perm_src, k, T, x_stride}, rows{by_assignment ? perm_src : nullptr, 1, R, dy_stride};
+    float *u = (float *)workspace, *part0 = R > 0 ? (float *)((char *)workspace + round_up((size_t)R * rank * sizeof(float), 256)) : nullptr;
+    float *part1 = R > 0 ? (float *)((char *)part0 + round_up(part_bytes(R, K, rank), 256)) : nullptr;
     if (R > 0 && (dx || da)) {
-        const AdapterArgs p{expert_offsets, scale, R, E, N, rank, dy, dy_map, b, u, nullptr, RowMap{}};
-        if (const int rc = launch_shrink(p, dy_dtype, dtype, s, what)) return rc;
+        AdapterArgs p{};
+        p.offsets = expert_offsets, p.scale = scale, p.R = R, p.E = E, p.K = N, p.N = K, p.rank = rank;
+        p.x = dy, p.a = b, p.b = a, p.x_map = rows;
+        p.out = dx, p.out_map = RowMap{rows.source, 1, R, dx_stride};
+        p.coef = u, p.coef_scaled = 1;
+        if (const int rc = launch_adapter(p, dtype, dy_dtype, dtype, s, what)) return rc;
     }
-    if (R > 0 && dx) {
-        const AdapterArgs p{expert_offsets, nullptr, R, E, K, rank, nullptr, RowMap{}, a, u, dx, dx_map};
-        if (const int rc = launch_expand(p, dtype, dtype, s, what)) return rc;
-    }
-    if (da) {
-        const AdapterArgs p{expert_offsets, nullptr, R, E, K, rank, x, tokens, nullptr, u, da, RowMap{}};
-        if (const int rc = launch_outer(p, dtype, grad_dtype, s, what)) return rc;
-    }
-    if (db) {
-        const AdapterArgs p{expert_offsets, scale, R, E, N, rank, dy, dy_map, nullptr, const_cast<float *>(v), db, RowMap{}};
-        if (const int rc = launch_outer(p, dy_dtype, grad_dtype, s, what)) return rc;
-    }
-    return MOE_OK;
+    OuterArgs p{};
+    p.offsets = expert_offsets, p.R = R, p.E = E, p.rank = rank, p.out_dtype = grad_dtype;
+    p.job[0] = OuterJob{x, tokens, u, nullptr, da, K, 0, outer_chunk(R, K), part0, part_slots(R, K)};
+    p.job[1] = OuterJob{dy, rows, v, scale, db, N, 0, outer_chunk(R, N), part1, part_slots(R, N)};
+    return launch_adapter_outer(p, dtype, dy_dtype, s, what);
 }

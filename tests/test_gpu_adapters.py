@@ -98,6 +98,32 @@ def test_slices_of_wider_rows(T, E, K, N, rank):
         assert bool((t[:, :8] == 3).all()) and bool((t[:, t.shape[1] - 16:] == 3).all())
 
 
+def test_offsets_that_are_no_partition_stay_inside():
+    """Wrong results, but nothing behind the buffers: the canaries around them stay."""
+    T, E, K, N, rank = 3000, 9, 64, 128, 16
+    d = inputs(T, 1, E, K, N, rank, "even", BF16, BF16)
+    need = B.moe_adapters_backward_workspace_bytes(T, E, K, N, rank)
+    for offsets in ([0, T] * 5, [T, 0] * 5, [-5, 10 ** 9] * 5, [2 ** 31 - 1] * 10, [0, 2500, 100, 2900, 0, 3000, 0, 3000, 10, 3000]):
+        off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+        guarded = {}
+
+        def guard(name, n, dtype):
+            t = torch.full((n + 1024,), 7.0, dtype=dtype, device="cuda")
+            guarded[name] = t
+            return t[512:512 + n]
+
+        out, v = guard("out", T * N, BF16).view(T, N), guard("v", T * rank, F32).view(T, rank)
+        grads = guard("dx", T * K, BF16).view(T, K), guard("da", E * rank * K, F32).view(E, rank, K), guard("db", E * rank * N, F32).view(E, rank, N)
+        B.moe_adapters(d["x"], d["a"], d["b"], off, y=d["y"], out=out, v=v, perm_src=d["perm"], by_assignment=True)
+        v.nan_to_num_(0.0)
+        B.moe_adapters_backward(d["dy"], d["x"], d["a"], d["b"], v, off, perm_src=d["perm"], out=grads, workspace=ws[:need])
+        torch.cuda.synchronize()
+        assert bool((ws[need:] == 77).all())
+        for name, t in guarded.items():
+            assert bool((t[:512] == 7).all()) and bool((t[-512:] == 7).all()), name
+
+
 def test_needs_one_by_one_and_repeats():
     """Each gradient alone has the bits of all together; the same call has the same bits."""
     d = inputs(300, 2, 8, 264, 136, 16, "pruned", F16, F16)
@@ -186,11 +212,11 @@ def test_replays_from_a_graph_and_on_a_side_stream():
     gen = generator(4)
     index = dict(perm_src=d["perm"], k=k, scale=d["scale"])
     v, out = torch.empty((d["R"], rank), device="cuda"), torch.empty_like(d["y"])
-    ws = torch.empty(B.moe_adapters_workspace_bytes(d["R"], E, K, N, rank), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(B.moe_adapters_backward_workspace_bytes(d["R"], E, K, N, rank), dtype=torch.uint8, device="cuda")
     grads = torch.empty((d["R"], K), dtype=F16, device="cuda"), torch.empty_like(d["a"]), torch.empty_like(d["b"])
 
     def step():
-        B.moe_adapters(d["x"], d["a"], d["b"], d["offsets"], y=d["y"], out=out, v=v, workspace=ws, **index)
+        B.moe_adapters(d["x"], d["a"], d["b"], d["offsets"], y=d["y"], out=out, v=v, **index)
         B.moe_adapters_backward(d["dy"], d["x"], d["a"], d["b"], v, d["offsets"], out=grads, workspace=ws, **index)
 
     step()
