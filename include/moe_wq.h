@@ -446,7 +446,7 @@ int moe_permute_backward(const void *dx_perm, int perm_dtype, const int32_t *inv
  *   y, out [R,N] y_dtype (any of the three), y_stride and out_stride values from row to row: in sorted order or, by_assignment != 0, in the order of the assignments
  *     perm_src[r] (with k = 1 the tokens').  y == out: in place; y NULL: 0.  Otherwise they must not overlap.
  *   Rows of no adapter (at or past expert_offsets[E]) are y's; in place they are neither read nor written.
- *   v [R,rank] fp32: what the backward pass needs of this one, in sorted order (rows of no adapter are not written), or NULL.
+ *   v [R,rank] fp32: what the backward pass needs of this one, in sorted order (rows of no adapter are not written); of at most 512 rows it may be NULL.
  * Backward, of dy [R,N] dy_dtype (ordered as y):  u[r] = scale[e] * B[e] dy[r],
  *   dx[r] = u[r] A[e] in dtype, ordered as y, 0 for rows of no adapter (with more than one row per token moe_permute_backward adds them up)
  *   da[e] = sum_r u[r] x[t]^T,  db[e] = scale[e] * sum_r v[r] dy[r]^T  in grad_dtype, 0 for adapters without rows; sums over rows in a fixed order

@@ -750,6 +750,8 @@ def moe_adapters(x, a, b, expert_offsets, perm_src=None, k: int = 1, scale=None,
     yp, ys = (None, N) if y is None else _rows(y, "y", N, (out.dtype,))
     if out.shape[0] != R or (y is not None and y.shape[0] != R) or (v is not None and v.shape != (R, rank)):
         raise MoeError("y and out must have %d rows, v [%d, %d]" % (R, R, rank))
+    if v is None and R > 512:                                           # (more rows than a call keeps on chip between its products)
+        v = torch.empty(R, rank, dtype=torch.float32, device=x.device)
     _check_device(x, a, b, expert_offsets, perm_src, scale, y, out, v)
     rc = load().moe_adapters(xp, _DT[x.dtype], xs, x.shape[0], _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E, K, N, rank,
                           _ptr(a, x.dtype, "a"), _ptr(b, x.dtype, "b"), _ptr(scale, torch.float32, "scale"), int(by_assignment), yp, ys, op, os_, _DT[out.dtype],

@@ -6,6 +6,7 @@
 namespace moe {
 
 constexpr int kAdapterMostRank = 128, kAdapterMostAdapters = 4096;
+constexpr int kAdapterRowsWithoutV = 512;           // more rows take two launches, between which the coefficients are in memory
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
@@ -17,8 +18,37 @@ struct RowMap {
     int rows;                   // of the buffer
     int64_t stride;
 
-    __device__ inline int row(int r) const { return source ? min(max(source[r] / div, 0), rows - 1) : r; }
+    // Several rows at once: their loads are requested together.
+    template <int N>
+    __device__ inline void find(int (&r)[N]) const
+    {
+        if (!source) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = source[r[i]];
+        if (div == 2) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) r[i] >>= 1;
+        } else if (div != 1) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) r[i] /= div;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = min(max(r[i], 0), rows - 1);
+    }
 };
+
+// f(integral_constant 0), ... f(integral_constant N - 1)
+template <int N, class F, int I = 0>
+__device__ inline void unrolled(F &&f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unrolled<N, F &, I + 1>(f);
+    }
+}
+
+// Requests stand ahead of what is done while they are under way: left to itself the compiler moves them behind it.
+__device__ inline void requested() { __builtin_amdgcn_sched_barrier(0); }
 
 // coef[r] = A[e] x[r] (for phase two times scale[e]), out[r] = y[r] + coef[r] B[e]
 struct AdapterArgs {
@@ -31,11 +61,12 @@ struct AdapterArgs {
     int64_t y_stride;
     void *out;
     RowMap out_map;             // of y as well, but for the stride
-    float *coef;                // [R, rank] or null
+    float *coef;                // [R, rank], or null (one launch does without)
     int coef_scaled;            // coef holds scale * (A x)
     int ncol;                   // slices of N, each a block's
-    int width;                  // channels of a slice, a multiple of 64
+    int width;                  // channels of a slice, a multiple of 64 (one launch)
     int items;                  // blocks for rows of adapters; those behind them copy the others
+    int share;                  // many rows: those of a block, about
 };
 
 // out[e][j] = scale sum_r coef[r][j] rows[r]
@@ -58,8 +89,11 @@ struct OuterArgs {
     int join;                   // adapters that can have more than one chunk
 };
 
-int launch_adapter_f16(const AdapterArgs &p, int x_dtype, int out_dtype, hipStream_t s, const char *what);
-int launch_adapter_bf16(const AdapterArgs &p, int x_dtype, int out_dtype, hipStream_t s, const char *what);
+// Forward: x in the adapters' type.  Backward: `x` is dy, of any type, and out is dx, in the adapters'.
+int launch_adapter_forward_f16(const AdapterArgs &p, int out_dtype, hipStream_t s, const char *what);
+int launch_adapter_forward_bf16(const AdapterArgs &p, int out_dtype, hipStream_t s, const char *what);
+int launch_adapter_backward_f16(const AdapterArgs &p, int x_dtype, hipStream_t s, const char *what);
+int launch_adapter_backward_bf16(const AdapterArgs &p, int x_dtype, hipStream_t s, const char *what);
 int launch_adapter_outer(const OuterArgs &p, int dtype0, int dtype1, hipStream_t s, const char *what);
 
 template <int DT>
@@ -69,22 +103,33 @@ __device__ inline float4_t product16(u32x4_t a, u32x4_t b, float4_t c)          
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
 }
 
-// A coefficient as two 16-bit numbers, hi the nearest and lo the nearest to what is left: off by at most 2^-16 (bf16) or 2^-22 (fp16) of it, where one alone would be off by 2^-8
-// and 2^-11, as much as the whole result may be.  (fp16: of numbers that a power of two has brought into range.)
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+
+template <int DT>
+__device__ inline float4_t product16(u32x2_t a, u32x2_t b, float4_t c)          // 16 x 16 x 16
+{
+    if constexpr (DT == MOE_BF16) return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(half4_t, a), __builtin_bit_cast(half4_t, b), c, 0, 0, 0);
+}
+
+// A coefficient as 16-bit terms, each the nearest to what those before it leave: two are off by at most 2^-16 of it in bf16 and 2^-22 in fp16, where one alone would be off by
+// 2^-8 and 2^-11, as much as a 16-bit result may be altogether; in bf16 a third (2^-24) where the result is fp32.  (fp16: of numbers that a power of two has brought into range.)
 template <int DT>
 struct Split {
-    uint16_t hi, lo;
+    uint16_t hi, lo, rest;
     __device__ inline explicit Split(float c)
     {
-        if constexpr (DT == MOE_BF16) {
-            const __bf16 h = (__bf16)c;
-            const float left = c - (float)h;
-            hi = __builtin_bit_cast(uint16_t, h), lo = __builtin_bit_cast(uint16_t, (__bf16)(left == left ? left : 0.0f));      // (an infinity leaves none)
-        } else {
-            const _Float16 h = (_Float16)c;
-            const float left = c - (float)h;
-            hi = __builtin_bit_cast(uint16_t, h), lo = __builtin_bit_cast(uint16_t, (_Float16)(left == left ? left : 0.0f));
-        }
+        hi = take(c), lo = take(c), rest = DT == MOE_BF16 ? take(c) : 0;
+    }
+    __device__ static inline uint16_t take(float &c)
+    {
+        using T = std::conditional_t<DT == MOE_BF16, __bf16, _Float16>;
+        const T h = (T)c;
+        c -= (float)h;
+        c = c == c ? c : 0.0f;                                  // (an infinity leaves none)
+        return __builtin_bit_cast(uint16_t, h);
     }
 };
 
@@ -96,11 +141,12 @@ __device__ inline int split_exponent(float most)
 }
 __device__ inline float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }       // -126 <= e <= 127
 
-// Four columns of eight rows, a row's four as two words, become the columns: column t's eight values as four words.
-__device__ inline void transpose_8x4(const uint2 (&row)[8], u32x4_t (&col)[4])
+// Four columns of four or eight rows, a row's four as two words, become the columns: column t's values as words.
+template <int ROWS, class Operand>
+__device__ inline void transpose_columns(const uint2 (&row)[ROWS], Operand (&col)[4])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < ROWS / 2; ++i) {
         col[0][i] = __builtin_amdgcn_perm(row[2 * i + 1].x, row[2 * i].x, 0x05040100u);
         col[1][i] = __builtin_amdgcn_perm(row[2 * i + 1].x, row[2 * i].x, 0x07060302u);
         col[2][i] = __builtin_amdgcn_perm(row[2 * i + 1].y, row[2 * i].y, 0x05040100u);

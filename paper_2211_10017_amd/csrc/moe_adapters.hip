@@ -43,21 +43,18 @@ static int check_rows(const char *what, const char *name, const void *p, int64_t
 }
 
 // Rows of a wavefront's part of a matrix's gradient.  Enough parts to fill the chip (a part is 64 channels of `chunk` rows; two thousand wavefronts), as the sums of parts have to be
-// written and added up; at most 1024 rows, or an adapter that has much of the batch is one long chain, unless that would make more than 256 parts of it.
+// written and added up by a launch of their own; at most 1024 rows, or an adapter that has much of the batch is one long chain, unless that would make more than 256 parts of it.  Up to
+// 1024 rows are one part, without that launch.
 static int outer_chunk(int R, int C)
 {
+    if (R <= 1024) return 1024;
     const long even = (long)R * ((C + 63) / 64) / 2048, most = R / 256 > 1024 ? R / 256 : 1024;
-    const long rows = even < 64 ? 64 : even > most ? most : even;
+    const long rows = even < 256 ? 256 : even > most ? most : even;
     return (int)((rows + 31) / 32 * 32);
 }
 
 static int part_slots(int R, int C) { return 2 * (R / outer_chunk(R, C)); }        // n rows in more than one chunk are at most 2 (n / chunk) of them
 static size_t part_bytes(int R, int C, int rank) { return (size_t)part_slots(R, C) * rank * C * sizeof(float); }
-
-static int launch_adapter(const AdapterArgs &p, int dtype, int x_dtype, int out_dtype, hipStream_t s, const char *what)
-{
-    return dtype == MOE_F16 ? launch_adapter_f16(p, x_dtype, out_dtype, s, what) : launch_adapter_bf16(p, x_dtype, out_dtype, s, what);
-}
 
 }  // namespace moe
 
@@ -70,7 +67,8 @@ extern "C" int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, c
     const AdapterCall call{what, dtype, y_dtype, T, k, R, E, K, N, rank, by_assignment, perm_src, expert_offsets, a, b};
     if (const int rc = check_adapters(call)) return rc;
     if (R == 0) return MOE_OK;                                      // empty buffers may be NULL
-    if (!x || !out) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!x || !out || (!v && R > kAdapterRowsWithoutV)) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned16(v)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     if (const int rc = check_rows(what, "x", x, x_stride, K)) return rc;
     if (const int rc = check_rows(what, "out", out, out_stride, N)) return rc;
     if (y)
@@ -81,7 +79,7 @@ extern "C" int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, c
     p.x = x, p.a = a, p.b = b, p.x_map = RowMap{perm_src, k, T, x_stride};
     p.y = y, p.y_stride = y_stride, p.out = out, p.out_map = RowMap{by_assignment ? perm_src : nullptr, 1, R, out_stride};
     p.coef = v, p.coef_scaled = 0;
-    return launch_adapter(p, dtype, dtype, y_dtype, as_stream(stream), what);
+    return dtype == MOE_F16 ? launch_adapter_forward_f16(p, y_dtype, as_stream(stream), what) : launch_adapter_forward_bf16(p, y_dtype, as_stream(stream), what);
 }
 
 extern "C" size_t moe_adapters_backward_workspace_bytes(int R, int E, int K, int N, int rank)
@@ -122,7 +120,8 @@ extern "C" int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_st
         p.x = dy, p.a = b, p.b = a, p.x_map = rows;
         p.out = dx, p.out_map = RowMap{rows.source, 1, R, dx_stride};
         p.coef = u, p.coef_scaled = 1;
-        if (const int rc = launch_adapter(p, dtype, dy_dtype, dtype, s, what)) return rc;
+        const int rc = dtype == MOE_F16 ? launch_adapter_backward_f16(p, dy_dtype, s, what) : launch_adapter_backward_bf16(p, dy_dtype, s, what);
+        if (rc != MOE_OK) return rc;
     }
     OuterArgs p{};
     p.offsets = expert_offsets, p.R = R, p.E = E, p.rank = rank, p.out_dtype = grad_dtype;

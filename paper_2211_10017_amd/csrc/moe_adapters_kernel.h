@@ -5,109 +5,127 @@
 
 namespace moe {
 
-// A block takes up to 16 MT rows of an adapter and a slice of N.  Phase one: its W wavefronts split K, each with all of the rows and all of the rank, operands straight from memory in
-// the matrix cores' order (both lie along K); their sums meet in LDS in a fixed order.  Phase two: the coefficients, as pairs of 16-bit numbers that stand beside each other along the
-// products' inner axis (so that a product of 32 holds 16 of the rank), times B, whose columns a lane puts together from four neighbouring channels of eight of its rows.
-template <int XDT, int WDT, int ODT, int W, int MT, int NT>
+// ---- phase one: rows times A ---------------------------------------------------------------------------------------------------------------------
+
+// acc[m][n] += rows 16 m.. of the item times the rows 16 n.. of A[e], over this wavefront's share of K: of every 4 W steps the four that are its own.  Operands come straight from memory
+// in the matrix cores' order (both lie along K) and stay D steps ahead of their products: a step's registers are requested anew as soon as it has been multiplied.
+template <int XDT, int WDT, int D, int W, int MT, int NT>
+__device__ inline void multiply_rows(const AdapterArgs &p, int e, int row0, int rows, int wave, float4_t (&acc)[MT][NT])
+{
+    constexpr bool kNarrow = XDT == WDT;                        // products in 16 bits; otherwise fp32 ones, 16 channels a step instead of 32
+    constexpr int KS = kNarrow ? 32 : 16, LV = KS / 4;          // channels of a step, and of a lane
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, K = p.K, rank = p.rank;
+    int x_row[MT], w_at[NT];
+    size_t x_at[MT];
+    const uint16_t *w = reinterpret_cast<const uint16_t *>(p.a) + (size_t)e * rank * K;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x_row[m] = row0 + min(16 * m + l, rows - 1);
+    p.x_map.find(x_row);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x_at[m] = (size_t)x_row[m] * p.x_map.stride + g * LV;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) w_at[n] = min(16 * n + l, rank - 1) * K + g * LV;      // (past the rank: the last row again, left out by the caller)
+    Raw<XDT, LV> x[D][MT];
+    Raw<WDT, LV> a[D][NT];
+    const int steps = K / KS, own = steps / (4 * W) * 4 + min(max(steps % (4 * W) - 4 * wave, 0), 4);
+    auto request = [&](auto u_c, int i) {
+        constexpr int B = decltype(u_c)::value;
+        const int k = ((i >> 2) * 4 * W + wave * 4 + (i & 3)) * KS;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) a[B][n].load(w, w_at[n] + k);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) x[B][m].load(p.x, x_at[m] + k);
+        requested();
+    };
+    auto use = [&](auto u_c) {
+        constexpr int B = decltype(u_c)::value;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (kNarrow) {
+                    acc[m][n] = product16<WDT>(u32x4_t{x[B][m].w[0], x[B][m].w[1], x[B][m].w[2], x[B][m].w[3]}, u32x4_t{a[B][n].w[0], a[B][n].w[1], a[B][n].w[2], a[B][n].w[3]}, acc[m][n]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < LV; ++i) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[B][m].get(i), a[B][n].get(i), acc[m][n], 0, 0, 0);
+                }
+            }
+        requested();
+    };
+    if (own > 0) {
+        unrolled<D>([&](auto u) { request(u, min((int)decltype(u)::value, own - 1)); });
+        int i = 0;
+        for (; i + D < own; i += D)
+            unrolled<D>([&](auto u) { use(u), request(u, min(i + D + (int)decltype(u)::value, own - 1)); });
+        unrolled<D>([&](auto u) {
+            if (i + (int)decltype(u)::value < own) use(u);
+        });
+    }
+    if (K % KS && (steps >> 2) % W == wave) {                   // channels behind the last whole step
+        const int k = steps * KS;
+        const bool in = k + g * LV < K;                         // (a lane's channels are all inside or all outside)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (in) a[0][n].load(w, w_at[n] + k);
+            else a[0][n].clear();
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if (in) x[0][m].load(p.x, x_at[m] + k);
+            else x[0][m].clear();
+        }
+        use(std::integral_constant<int, 0>{});
+    }
+}
+
+// ---- what both kernels below hold in LDS ---------------------------------------------------------------------------------------------------------
+
+template <int WDT, int ODT, int W, int MT, int NT>
 struct AdapterShape {
-    static constexpr bool kNarrow = XDT == WDT;                  // products in 16 bits; otherwise fp32 ones, 16 channels a step instead of 32
-    static constexpr int KS = kNarrow ? 32 : 16, LV = KS / 4;   // channels of a step, and of a lane
-    static constexpr int U = NT <= 2 ? 4 : NT == 4 ? 2 : 1;     // steps whose operands are requested together
-    static constexpr int BM = 16 * MT, J = 16 * NT, kRed = J + 4, kPairs = 2 * J + 8;      // padded against bank conflicts
-    static constexpr int kLds = W * BM * kRed * 4 + BM * kPairs * 2 + BM * 4;
+    static constexpr int BM = 16 * MT, J = 16 * NT;             // rows, and the rank in whole products
+    static constexpr int D = (W == 16 ? 40 : 96) / (4 * (MT + NT)) < 2 ? 2 : (W == 16 ? 40 : 96) / (4 * (MT + NT)) > 6 ? 6 : (W == 16 ? 40 : 96) / (4 * (MT + NT));
+    static constexpr int kParts = W == 8 && NT >= 4 ? W / 2 : W, kRed = J + 4;              // wavefronts' sums at a time; rows padded against bank conflicts
+    static constexpr int KI = NT == 1 ? 16 : 32, NC = J / KI, JL = KI / 4;                  // phase two: inner size of a product, products over the rank, rank of a lane in one
+    static constexpr int TERMS = WDT == MOE_BF16 && ODT == MOE_F32 ? 3 : 2, kTermRow = TERMS * J + 8;
+    static constexpr int kTerms = kParts * BM * kRed * 4, kUnit = kTerms + BM * kTermRow * 2, kPlace = kUnit + BM * 4, kLds = kPlace + BM * 16;
 };
 
-template <int XDT, int WDT, int ODT, int W, int MT, int NT>
-__global__ __launch_bounds__(64 * W) void adapter_kernel(AdapterArgs p)
+// The wavefronts' sums become coefficients: added in a fixed order, written to memory if they are wanted there, and left in LDS as 16-bit terms.
+template <class S, int WDT, int W, int MT, int NT>
+__device__ inline void make_terms(const AdapterArgs &p, uint8_t *lds, float4_t (&acc)[MT][NT], int e, int row0, int rows, int wave, bool keep)
 {
-    using S = AdapterShape<XDT, WDT, ODT, W, MT, NT>;
-    constexpr int BM = S::BM, J = S::J, KS = S::KS, LV = S::LV, U = S::U;
-    extern __shared__ __align__(16) uint8_t lds[];
-    float *red = reinterpret_cast<float *>(lds);
-    uint16_t *pairs = reinterpret_cast<uint16_t *>(lds + W * BM * S::kRed * 4);
-    float *unit = reinterpret_cast<float *>(lds + W * BM * S::kRed * 4 + BM * S::kPairs * 2);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15, g = lane >> 4;
-    const int K = p.K, N = p.N, rank = p.rank;
-
-    if ((int)blockIdx.x >= p.items) {                           // rows of no adapter: y's, or 0
-        const int active = min(max(p.offsets[p.E], 0), p.R);
-        for (int r = active + ((int)blockIdx.x - p.items) * W + wave; r < p.R; r += (gridDim.x - p.items) * W) {
-            const size_t row = p.out_map.row(r);
-            for (int c = lane * 8; c < N; c += 512) {
-                Raw<ODT, 8> y;
-                if (p.y) y.load(p.y, row * p.y_stride + c);
-                else y.clear();
-                y.store(p.out, row * p.out_map.stride + c);
-            }
-        }
-        return;
-    }
-    int e, col, row0, rows;
-    if (!find_item<16>(p.offsets, p.E, p.R, BM, p.ncol, blockIdx.x, &e, &col, &row0, &rows)) return;
-    e = __builtin_amdgcn_readfirstlane(e), col = __builtin_amdgcn_readfirstlane(col);
-    row0 = __builtin_amdgcn_readfirstlane(row0), rows = __builtin_amdgcn_readfirstlane(rows);
-    const float scale = p.scale ? p.scale[e] : 1.0f;
-
-    // Phase one.
-    float4_t acc[MT][NT] = {};
-    {
-        size_t x_at[MT];
-        int w_at[NT];
-        const uint16_t *w = reinterpret_cast<const uint16_t *>(p.a) + (size_t)e * rank * K;
+    constexpr int BM = S::BM, J = S::J, P = S::kParts, TPR = 64 * W / BM >= 64 ? 64 : 64 * W / BM >= 32 ? 32 : 64 * W / BM >= 16 ? 16 : 8, Q = (J + TPR - 1) / TPR;
+    static_assert(64 * W >= BM * TPR || TPR == 8, "a row's threads are lanes of one wavefront");
+    float *red = reinterpret_cast<float *>(lds), *unit = reinterpret_cast<float *>(lds + S::kUnit);
+    uint16_t *terms = reinterpret_cast<uint16_t *>(lds + S::kTerms);
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, rank = p.rank;
+    auto at = [&](int part, int m, int n, int i) -> float & { return red[(part * BM + 16 * m + 4 * g + i) * S::kRed + 16 * n + l]; };
+    auto put = [&](int part) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) x_at[m] = (size_t)p.x_map.row(row0 + min(16 * m + l, rows - 1)) * p.x_map.stride + g * LV;
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) w_at[n] = min(16 * n + l, rank - 1) * K + g * LV;      // (past the rank: the last row again, left out below)
-        auto steps = [&](int k0, auto whole_c) {
-            constexpr bool WHOLE = decltype(whole_c)::value;
-            Raw<XDT, LV> x[U][MT];
-            Raw<WDT, LV> a[U][NT];
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int k = k0 + u * KS;
-                const bool in = WHOLE || k + g * LV < K;        // (a lane's channels are all inside or all outside)
+                for (int i = 0; i < 4; ++i) at(part, m, n, i) = acc[m][n][i];
+    };
+    if constexpr (P == W) put(wave);
+    else {                                                      // (the second half's first where all would be too much)
+        if (wave >= P) put(wave - P);
+        __syncthreads();
+        if (wave < P) {
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    if (in) x[u][m].load(p.x, x_at[m] + k);
-                    else x[u][m].clear();
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (in) a[u][n].load(w, w_at[n] + k);
-                    else a[u][n].clear();
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        if constexpr (S::kNarrow) {
-                            acc[m][n] = product16<WDT>(u32x4_t{x[u][m].w[0], x[u][m].w[1], x[u][m].w[2], x[u][m].w[3]},
-                                                       u32x4_t{a[u][n].w[0], a[u][n].w[1], a[u][n].w[2], a[u][n].w[3]}, acc[m][n]);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < LV; ++i) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[u][m].get(i), a[u][n].get(i), acc[m][n], 0, 0, 0);
-                        }
-                    }
-        };
-        for (int k0 = wave * U * KS; k0 < K; k0 += W * U * KS) {
-            if (k0 + U * KS <= K) steps(k0, std::true_type{});
-            else steps(k0, std::false_type{});
+                    for (int i = 0; i < 4; ++i) acc[m][n][i] += at(wave, m, n, i);
+            put(wave);                                          // (each place is read and written by the same lane)
         }
     }
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) red[(wave * BM + 16 * m + 4 * g + i) * S::kRed + 16 * n + l] = acc[m][n][i];
     __syncthreads();
-    {
-        constexpr int TPR = 64 * W / BM, Q = (J + TPR - 1) / TPR;       // threads of a row, and what each has of the rank
-        static_assert(64 % TPR == 0 && TPR <= 64, "a row's threads are lanes of one wavefront");
-        const int row = threadIdx.x / TPR, j0 = threadIdx.x % TPR;
+    const float scale = p.scale ? p.scale[e] : 1.0f;
+    const int j0 = threadIdx.x % TPR;
+    for (int row = threadIdx.x / TPR; row < BM; row += 64 * W / TPR) {
         float c[Q], most = 0.0f;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
@@ -115,11 +133,11 @@ __global__ __launch_bounds__(64 * W) void adapter_kernel(AdapterArgs p)
             float sum = 0.0f;
             if (j < J) {
 #pragma unroll
-                for (int w = 0; w < W; ++w) sum += red[(w * BM + row) * S::kRed + j];
+                for (int w = 0; w < P; ++w) sum += red[(w * BM + row) * S::kRed + j];
             }
             const bool in = j < rank && row < rows;
             c[q] = in ? scale * sum : 0.0f;
-            if (in && p.coef && col == 0) p.coef[(size_t)(row0 + row) * rank + j] = p.coef_scaled ? c[q] : sum;
+            if (in && keep) p.coef[(size_t)(row0 + row) * rank + j] = p.coef_scaled ? c[q] : sum;
             most = fmaxf(most, fabsf(c[q]));
         }
         float back = 1.0f;
@@ -135,118 +153,258 @@ __global__ __launch_bounds__(64 * W) void adapter_kernel(AdapterArgs p)
             const int j = j0 + q * TPR;
             if (j >= J) continue;
             const Split<WDT> s(WDT == MOE_F16 ? c[q] * back : c[q]);
-            uint16_t *at = pairs + row * S::kPairs + (j >> 4) * 32 + (j & 15);          // sixteen of the rank: their hi, then their lo
-            at[0] = s.hi, at[16] = s.lo;
+            uint16_t *to = terms + row * S::kTermRow + j;
+            to[0] = s.hi, to[J] = s.lo;
+            if constexpr (S::TERMS == 3) to[2 * J] = s.rest;
         }
-    }
-    if (!p.out) return;                                         // (coefficients alone)
-    __syncthreads();
-
-    // Phase two.
-    u32x4_t coef[MT][NT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) coef[m][n] = *reinterpret_cast<const u32x4_t *>(pairs + (16 * m + l) * S::kPairs + 32 * n + 8 * g);
-    int out_row[MT][4];
-    float power[MT][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 16 * m + 4 * g + i;
-            out_row[m][i] = r < rows ? p.out_map.row(row0 + r) : -1;
-            if constexpr (WDT == MOE_F16) power[m][i] = unit[r];
-        }
-    const uint16_t *b = reinterpret_cast<const uint16_t *>(p.b) + (size_t)e * rank * N;
-    const int end = min(N, (col + 1) * p.width);
-    for (int c0 = col * p.width + wave * 64; c0 < end; c0 += 64 * W) {
-        const int c = c0 + 4 * l;
-        const bool in = c < end;
-        Raw<ODT, 4> y[MT][4];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (p.y && in && out_row[m][i] >= 0) y[m][i].load(p.y, (size_t)out_row[m][i] * p.y_stride + c);
-                else y[m][i].clear();
-            }
-        float4_t sum[MT][4] = {};                               // [..][t]: column c + t
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            uint2 row[8];
-            u32x4_t column[4];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int j = 16 * n + 8 * (g & 1) + i;
-                row[i] = j < rank && in ? *reinterpret_cast<const uint2 *>(b + (j * N + c)) : make_uint2(0, 0);
-            }
-            transpose_8x4(row, column);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) sum[m][t] = product16<WDT>(coef[m][n], column[t], sum[m][t]);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!in || out_row[m][i] < 0) continue;
-                float v[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) v[t] = y[m][i].get(t) + (WDT == MOE_F16 ? sum[m][t][i] * power[m][i] : sum[m][t][i]);
-                y[m][i].set(v);
-                y[m][i].store(p.out, (size_t)out_row[m][i] * p.out_map.stride + c);
-            }
     }
 }
 
-template <int XDT, int WDT, int ODT, int W, int MT, int NT>
-static int launch_adapter_shape(AdapterArgs p, int slices, hipStream_t s, const char *what)
+// Phase two: coefficients times B, 64 channels at a time, every W-th of them from `first` to `end`.  A lane puts B's columns together from four neighbouring channels of its rows, once for
+// all of the item's rows.  The next channels' operands are requested as soon as this one's registers are free.
+template <class S, int WDT, int ODT, bool Y, int W, int MT>
+__device__ inline void expand_rows(const AdapterArgs &p, const uint8_t *lds, int e, int rows, int wave, int first, int end)
 {
-    using S = AdapterShape<XDT, WDT, ODT, W, MT, NT>;
-    if (!p.out) slices = 1;
-    p.width = (int)round_up(((size_t)p.N + slices - 1) / slices, 64);
-    p.ncol = (p.N + p.width - 1) / p.width;
-    const long slots = (long)p.R / S::BM + (p.E < p.R ? p.E : p.R);
-    const long items = (slots * p.ncol + kXcds - 1) / kXcds * kXcds;             // upper bound of the work items, whole rounds of XCDs
-    const long copies = p.y == p.out || !p.out ? 0 : (p.R + W - 1) / W < 256 ? (p.R + W - 1) / W : 256;
+    constexpr int J = S::J, KI = S::KI, NC = S::NC, JL = S::JL;
+    typedef uint32_t operand_t __attribute__((ext_vector_type(JL / 2)));
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, N = p.N, rank = p.rank;
+    const uint16_t *terms = reinterpret_cast<const uint16_t *>(lds + S::kTerms), *b = reinterpret_cast<const uint16_t *>(p.b) + (size_t)e * rank * N;
+    const float *unit = reinterpret_cast<const float *>(lds + S::kUnit);
+    const size_t *place = reinterpret_cast<const size_t *>(lds + S::kPlace);                // of the rows in y and in out
+    const int groups = (end - first + 63) / 64;
+    if (wave >= groups) return;
+    Raw<ODT, 4> y[MT][4];
+    uint2 raw[NC][JL];
+    auto channel = [&](int group) { return min(first + group * 64 + 4 * l, end - 4); };     // (past the end: the last ones again, which are not stored)
+    auto request_b = [&](int group) {
+        const int c = channel(group);
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int i = 0; i < JL; ++i) raw[n][i] = *reinterpret_cast<const uint2 *>(b + (size_t)(uint32_t)(min(KI * n + JL * g + i, rank - 1) * N + c));
+        requested();
+    };
+    auto request_y = [&](auto m_c, int group) {
+        constexpr int M = decltype(m_c)::value;
+        if constexpr (Y) {
+            const int c = channel(group);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[M][i].load(p.y, place[2 * (16 * M + 4 * g + i)] + c);
+            requested();
+        }
+    };
+    auto step = [&](int group, auto more_c) {
+        constexpr bool MORE = decltype(more_c)::value;
+        const int c = first + group * 64 + 4 * l;
+        operand_t column[NC][4];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+#pragma unroll
+            for (int i = 0; i < JL; ++i) {
+                const bool in = KI * n + JL * g + i < rank;     // (past the rank coefficients are 0, and 0 times an infinity is none)
+                raw[n][i] = make_uint2(in ? raw[n][i].x : 0, in ? raw[n][i].y : 0);
+            }
+            transpose_columns(raw[n], column[n]);
+        }
+        if constexpr (MORE) request_b(group + W);
+        unrolled<MT>([&](auto m_c) {
+            constexpr int M = decltype(m_c)::value;
+            float4_t sum[4] = {};                               // [t]: column c + t
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int i = 0; i < S::TERMS; ++i) {
+                    const operand_t coef = *reinterpret_cast<const operand_t *>(terms + (16 * M + l) * S::kTermRow + i * J + KI * n + JL * g);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) sum[t] = product16<WDT>(coef, column[n][t], sum[t]);
+                }
+            Raw<ODT, 4> out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    v[t] = WDT == MOE_F16 ? sum[t][i] * unit[16 * M + 4 * g + i] : sum[t][i];
+                    if constexpr (Y) v[t] += y[M][i].get(t);
+                }
+                out[i].set(v);
+            }
+            if constexpr (MORE) request_y(m_c, group + W);
+            if (16 * M + 16 <= rows && first + group * 64 + 64 <= end) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[i].store(p.out, place[2 * (16 * M + 4 * g + i) + 1] + c);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (16 * M + 4 * g + i < rows && c < end) out[i].store(p.out, place[2 * (16 * M + 4 * g + i) + 1] + c);
+            }
+            requested();
+        });
+    };
+    int t = wave;
+    request_b(t);
+    unrolled<MT>([&](auto m) { request_y(m, t); });
+    for (; t + W < groups; t += W) step(t, std::true_type{});
+    step(t, std::false_type{});
+}
+
+// Where the item's rows are in y and in out, for phase two.
+template <class S>
+__device__ inline void find_places(const AdapterArgs &p, uint8_t *lds, int row0, int rows)
+{
+    size_t *place = reinterpret_cast<size_t *>(lds + S::kPlace);
+    for (int i = threadIdx.x; i < S::BM; i += blockDim.x) {
+        int r[1] = {row0 + min(i, rows - 1)};
+        p.out_map.find(r);
+        place[2 * i] = (size_t)r[0] * p.y_stride, place[2 * i + 1] = (size_t)r[0] * p.out_map.stride;
+    }
+}
+
+// Rows of no adapter: y's, or 0.
+template <int ODT, bool Y>
+__device__ inline void copy_rows(const AdapterArgs &p, int block, int waves)
+{
+    const int lane = threadIdx.x & 63, active = min(max(p.offsets[p.E], 0), p.R);
+    for (int r = active + block * waves + (threadIdx.x >> 6); r < p.R; r += (gridDim.x - p.items) * waves) {
+        int at[1] = {r};
+        p.out_map.find(at);
+        const size_t row = at[0];
+        for (int c = lane * 8; c < p.N; c += 512) {
+            Raw<ODT, 8> y;
+            if (Y) y.load(p.y, row * p.y_stride + c);
+            else y.clear();
+            y.store(p.out, row * p.out_map.stride + c);
+        }
+    }
+}
+
+// ---- few rows: a block takes up to 16 rows of an adapter and a slice of N, its W wavefronts split K and the slice ------------------------------------
+
+template <int XDT, int WDT, int ODT, bool Y, int W, int NT>
+__global__ __launch_bounds__(64 * W) void adapter_few_kernel(AdapterArgs p)
+{
+    using S = AdapterShape<WDT, ODT, W, 1, NT>;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x >= p.items) return copy_rows<ODT, Y>(p, blockIdx.x - p.items, W);
+    int e, col, row0, rows;
+    if (!find_item<16>(p.offsets, p.E, p.R, 16, p.ncol, blockIdx.x, &e, &col, &row0, &rows)) return;
+    e = __builtin_amdgcn_readfirstlane(e), col = __builtin_amdgcn_readfirstlane(col);
+    row0 = __builtin_amdgcn_readfirstlane(row0), rows = __builtin_amdgcn_readfirstlane(rows);
+    find_places<S>(p, lds, row0, rows);
+    float4_t acc[1][NT] = {};
+    multiply_rows<XDT, WDT, S::D, W, 1, NT>(p, e, row0, rows, wave, acc);
+    make_terms<S, WDT, W, 1, NT>(p, lds, acc, e, row0, rows, wave, p.coef && col == 0);
+    if (!p.out) return;                                         // (coefficients alone)
+    __syncthreads();
+    expand_rows<S, WDT, ODT, Y, W, 1>(p, lds, e, rows, wave, col * p.width, min(p.N, (col + 1) * p.width));
+}
+
+// ---- many rows -------------------------------------------------------------------------------------------------------------------------------------
+//
+// All blocks run at once, one per compute unit, and share the memory's rate, so the one with the most to read is waited for: an adapter's rows are cut into as many blocks of `share` rows
+// as come nearest, evenly, rather than into full ones and a rest.
+
+// The block's adapter and rows.  Every wavefront computes the same.
+__device__ inline bool find_share(const AdapterArgs &p, int most, int *e, int *row0, int *rows)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int e0 = 0; e0 < p.E; e0 += 64) {
+        int lo = 0, hi = 0;
+        if (e0 + lane < p.E) expert_range(p.offsets, e0 + lane, p.R, &lo, &hi);
+        const int n = hi - lo, parts = n ? max(max((n + p.share / 2) / p.share, (n + most - 1) / most), 1) : 0, incl = wave_inclusive_sum(parts);
+        const uint64_t hit = __ballot(base + incl > (int)blockIdx.x);
+        if (hit) {
+            const int src = __ffsll((unsigned long long)hit) - 1;
+            const int count = __shfl(parts, src), i = blockIdx.x - base - __shfl(incl - parts, src), size = __shfl(n, src), first = __shfl(lo, src);
+            const int per = size / count, extra = size % count;
+            *e = __builtin_amdgcn_readfirstlane(e0 + src);
+            *row0 = __builtin_amdgcn_readfirstlane(first + i * per + min(i, extra));
+            *rows = __builtin_amdgcn_readfirstlane(per + (i < extra ? 1 : 0));
+            return true;
+        }
+        base += __shfl(incl, 63);
+    }
+    return false;
+}
+
+template <int XDT, int WDT, int ODT, bool Y, int MT, int NT>
+__global__ __launch_bounds__(512, 2) void adapter_many_kernel(AdapterArgs p)
+{
+    constexpr int W = 8;
+    using S = AdapterShape<WDT, ODT, W, MT, NT>;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x >= p.items) return copy_rows<ODT, Y>(p, blockIdx.x - p.items, W);
+    int e, row0, rows;
+    if (!find_share(p, S::BM, &e, &row0, &rows)) return;
+    find_places<S>(p, lds, row0, rows);
+    float4_t acc[MT][NT] = {};
+    multiply_rows<XDT, WDT, S::D, W, MT, NT>(p, e, row0, rows, wave, acc);
+    make_terms<S, WDT, W, MT, NT>(p, lds, acc, e, row0, rows, wave, true);
+    if (!p.out) return;
+    __syncthreads();
+    expand_rows<S, WDT, ODT, Y, W, MT>(p, lds, e, rows, wave, 0, p.N);
+}
+
+// ---- launches --------------------------------------------------------------------------------------------------------------------------------------
+
+template <class Kernel>
+static int launch_blocks(Kernel kernel, std::atomic<uint64_t> &raised, AdapterArgs p, long items, int W, int lds, hipStream_t s, const char *what)
+{
+    const int need = p.y == p.out || !p.out ? 0 : (p.R + W - 1) / W, copies = need < 256 ? need : 256;          // blocks for rows of no adapter
     if ((items + copies) * W > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %ld workgroups exceed one launch", what, items);
     p.items = (int)items;
-    static std::atomic<uint64_t> raised;
-    const auto kernel = &adapter_kernel<XDT, WDT, ODT, W, MT, NT>;
-    if (S::kLds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(kernel), S::kLds, raised);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(items + copies)), dim3(64 * W), S::kLds, s, p);
+    if (lds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(kernel), lds, raised);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(items + copies)), dim3(64 * W), lds, s, p);
     return check_launch(what);
 }
 
-template <int XDT, int WDT, int ODT>
-static int launch_adapter_types(const AdapterArgs &p, hipStream_t s, const char *what)
+template <int XDT, int WDT, int ODT, bool Y, int NT>
+static int launch_few(AdapterArgs p, int slices, hipStream_t s, const char *what)
 {
-    auto shape = [&](auto w_c, auto mt_c, int slices) {
-        constexpr int W = decltype(w_c)::value, MT = decltype(mt_c)::value;
-        if (p.rank <= 16) return launch_adapter_shape<XDT, WDT, ODT, W, MT, 1>(p, slices, s, what);
-        if (p.rank <= 32) return launch_adapter_shape<XDT, WDT, ODT, W, MT, 2>(p, slices, s, what);
-        if (p.rank <= 64) return launch_adapter_shape<XDT, WDT, ODT, W, MT, 4>(p, slices, s, what);
-        return launch_adapter_shape<XDT, WDT, ODT, W, MT, 8>(p, slices, s, what);
-    };
-    using std::integral_constant;
-    // tiles that rows spread evenly over the adapters would make
-    const long few = p.R / 16 + (p.E < p.R ? p.E : p.R);
-    if (few <= 256) return shape(integral_constant<int, 16>{}, integral_constant<int, 1>{}, (int)(256 / few < 8 ? 256 / few : 8));
-    return shape(integral_constant<int, 4>{}, integral_constant<int, 2>{}, 1);
+    constexpr int W = NT <= 2 ? 16 : 8;
+    if (!p.out) slices = 1;
+    p.width = (int)round_up(((size_t)p.N + slices - 1) / slices, 64);
+    p.ncol = (p.N + p.width - 1) / p.width;
+    const long slots = (long)p.R / 16 + (p.E < p.R ? p.E : p.R);                 // upper bound of the work items, whole rounds of XCDs
+    static std::atomic<uint64_t> raised;
+    return launch_blocks(&adapter_few_kernel<XDT, WDT, ODT, Y, W, NT>, raised, p, (slots * p.ncol + kXcds - 1) / kXcds * kXcds, W, AdapterShape<WDT, ODT, W, 1, NT>::kLds, s, what);
 }
 
-// Rows of x and y in the adapters' own type or fp32, and, of backward passes, the other way round; other pairs of 16-bit types as well.
-template <int WDT>
-static int launch_adapter(const AdapterArgs &p, int x_dtype, int out_dtype, hipStream_t s, const char *what)
+template <int XDT, int WDT, int ODT, bool Y, int MT, int NT>
+static int launch_many(const AdapterArgs &p, int blocks, hipStream_t s, const char *what)
 {
-    if (x_dtype == WDT) return with_dtype(out_dtype, [&](auto o) { return launch_adapter_types<WDT, WDT, decltype(o)::value>(p, s, what); });
-    return with_dtype(x_dtype, [&](auto x) {
-        constexpr int X = decltype(x)::value;
-        if constexpr (X == WDT) return (int)MOE_ERR_UNSUPPORTED;
-        else return launch_adapter_types<X, WDT, WDT>(p, s, what);              // (backward: dx has the adapters' type)
-    });
+    static std::atomic<uint64_t> raised;
+    return launch_blocks(&adapter_many_kernel<XDT, WDT, ODT, Y, MT, NT>, raised, p, blocks, 8, AdapterShape<WDT, ODT, 8, MT, NT>::kLds, s, what);
+}
+
+template <int XDT, int WDT, int ODT, bool Y, int NT>
+static int launch_rank(AdapterArgs p, hipStream_t s, const char *what)
+{
+    constexpr int kUnits = 256, kMost = NT <= 2 ? 80 : NT == 4 ? 64 : 48;       // compute units; rows that a block can hold
+    const int used = p.E < p.R ? p.E : p.R;
+    const long tiles = p.R / 16 + used;                         // that rows spread evenly over the adapters would make
+    if (!p.coef || tiles <= 256) return launch_few<XDT, WDT, ODT, Y, NT>(p, (int)(256 / tiles < 1 ? 1 : 256 / tiles > 8 ? 8 : 256 / tiles), s, what);
+    // rounds of blocks; in each a few fewer than compute units, as parts are rounded one way or the other
+    const long rounds = ((long)p.R + (kUnits - 8) * (kMost - 8) - 1) / ((kUnits - 8) * (kMost - 8));
+    p.share = (int)((p.R + (kUnits - 8) * rounds - 1) / ((kUnits - 8) * rounds));
+    const long slots = (long)p.R / p.share + used;              // an upper bound: of n rows at most n / share + 1
+    if (slots > 0x7fffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows of %d adapters are too many", what, p.R, p.E);
+    if constexpr (NT <= 2) {
+        if (p.share <= 24) return launch_many<XDT, WDT, ODT, Y, 2, NT>(p, (int)slots, s, what);
+    }
+    return launch_many<XDT, WDT, ODT, Y, kMost / 16, NT>(p, (int)slots, s, what);
+}
+
+template <int XDT, int WDT, int ODT, bool Y>
+static int launch_types(const AdapterArgs &p, hipStream_t s, const char *what)
+{
+    if (p.rank <= 16) return launch_rank<XDT, WDT, ODT, Y, 1>(p, s, what);
+    if (p.rank <= 32) return launch_rank<XDT, WDT, ODT, Y, 2>(p, s, what);
+    if (p.rank <= 64) return launch_rank<XDT, WDT, ODT, Y, 4>(p, s, what);
+    return launch_rank<XDT, WDT, ODT, Y, 8>(p, s, what);
 }
 
 }  // namespace moe

@@ -42,30 +42,54 @@ __device__ inline void store_gradient(void *out, int dtype, size_t at, const flo
 }
 
 // A wavefront: 64 channels, four neighbouring ones per lane, of up to `chunk` rows of an adapter, 32 rows a step (the products' inner axis).  16-bit rows meet the coefficients as two
-// 16-bit terms; fp16 ones in units of a power of two that grows with them.  fp32 rows and coefficients are multiplied in fp32.
-template <int DT, int NT>
+// 16-bit terms, three of bf16 where the gradient is fp32 (TERMS); fp16 ones in units of a power of two that grows with them.  fp32 rows and coefficients are multiplied in fp32.
+// Two steps' rows are under way at a time, and the places of the next two.
+template <int DT, int NT, int TERMS>
 __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int item)
 {
     const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, rank = p.rank, C = job.C;
     int e, lo, hi, slot;
     if (!find_chunk(p.offsets, p.E, p.R, job.chunk, item / job.ncol, &e, &lo, &hi, &slot)) return;
-    const int c = item % job.ncol * 64 + 4 * l;
-    const bool in = c < C;
+    lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+    const bool in = item % job.ncol * 64 + 4 * l < C;
+    const int c = min(item % job.ncol * 64 + 4 * l, C - 4);     // (past the end: the last channels again, which are not stored)
     float4_t acc[NT][4] = {};
     int unit = -100;                                            // fp16: the accumulators are in units of 2^unit
-    for (int r0 = lo; r0 < hi; r0 += 32) {
-        // row i of a lane: the 16-bit products take eight neighbouring ones of a lane, the fp32 ones one of every four
-        auto row_of = [&](int i) { return DT == MOE_F32 ? r0 + 4 * i + g : r0 + 8 * g + i; };
-        Raw<DT, 4> x[8];
-        float f[NT][8];
+    // row i of a lane in a step: the 16-bit products take eight neighbouring ones of a lane, the fp32 ones one of every four
+    auto row_of = [&](int step, int i) { return lo + 32 * step + (DT == MOE_F32 ? 4 * i + g : 8 * g + i); };
+    Raw<DT, 4> x[2][8];
+    float f[2][NT][8];
+    int id[2][8];
+    auto find = [&](auto s_c, int step) {
+        constexpr int B = decltype(s_c)::value;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) id[B][i] = min(row_of(step, i), hi - 1);
+        job.map.find(id[B]);
+    };
+    auto request = [&](auto s_c, int step) {
+        constexpr int B = decltype(s_c)::value;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[B][i].load(job.rows, (size_t)id[B][i] * job.map.stride + c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = row_of(i);
-            const bool live = r < hi;
-            if (live && in) x[i].load(job.rows, (size_t)job.map.row(r) * job.map.stride + c);
-            else x[i].clear();
+            const float *at = job.coef + (size_t)min(row_of(step, i), hi - 1) * rank;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) f[n][i] = live && 16 * n + l < rank ? job.coef[(size_t)r * rank + 16 * n + l] : 0.0f;
+            for (int n = 0; n < NT; ++n) f[B][n][i] = at[min(16 * n + l, rank - 1)];        // (past the rank: rows of the result that are not stored)
+        }
+        find(s_c, step + 2);
+        requested();
+    };
+    auto use = [&](auto s_c, int step) {
+        constexpr int B = decltype(s_c)::value;
+        if (lo + 32 * step + 32 > hi) {                         // rows behind the last: 0, on both sides
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool live = row_of(step, i) < hi;
+#pragma unroll
+                for (int w = 0; w < Raw<DT, 4>::WORDS; ++w) x[B][i].w[w] = live ? x[B][i].w[w] : 0;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) f[B][n][i] = live ? f[B][n][i] : 0.0f;
+            }
         }
         if constexpr (DT == MOE_F32) {
 #pragma unroll
@@ -73,7 +97,7 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[n][i], x[i].get(t), acc[n][t], 0, 0, 0);
+                    for (int t = 0; t < 4; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[B][n][i], x[B][i].get(t), acc[n][t], 0, 0, 0);
         } else {
             float back = 1.0f;
             if constexpr (DT == MOE_F16) {
@@ -81,7 +105,7 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(f[n][i]));
+                    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(f[B][n][i]));
 #pragma unroll
                 for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
                 const int ex = split_exponent(most);
@@ -98,23 +122,34 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
             uint2 row[8];
             u32x4_t column[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) row[i] = make_uint2(x[i].w[0], x[i].w[1]);
-            transpose_8x4(row, column);
+            for (int i = 0; i < 8; ++i) row[i] = make_uint2(x[B][i].w[0], x[B][i].w[1]);
+            transpose_columns(row, column);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                u32x4_t hi16, lo16;
+                u32x4_t term[3];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const Split<DT> a(DT == MOE_F16 ? f[n][2 * i] * back : f[n][2 * i]), b(DT == MOE_F16 ? f[n][2 * i + 1] * back : f[n][2 * i + 1]);
-                    hi16[i] = a.hi | (uint32_t)b.hi << 16, lo16[i] = a.lo | (uint32_t)b.lo << 16;
+                    const Split<DT> s0(DT == MOE_F16 ? f[B][n][2 * i] * back : f[B][n][2 * i]), s1(DT == MOE_F16 ? f[B][n][2 * i + 1] * back : f[B][n][2 * i + 1]);
+                    term[0][i] = s0.hi | (uint32_t)s1.hi << 16, term[1][i] = s0.lo | (uint32_t)s1.lo << 16, term[2][i] = s0.rest | (uint32_t)s1.rest << 16;
                 }
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    acc[n][t] = product16<DT>(hi16, column[t], acc[n][t]);
-                    acc[n][t] = product16<DT>(lo16, column[t], acc[n][t]);
-                }
+                for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) acc[n][t] = product16<DT>(term[i], column[t], acc[n][t]);
             }
         }
+        requested();
+    };
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    const int steps = (hi - lo + 31) / 32;
+    if (steps > 0) {
+        find(even, 0), find(odd, 1);
+        request(even, 0);
+        int t = 0;
+        for (; t + 2 < steps; t += 2) request(odd, t + 1), use(even, t), request(even, t + 2), use(odd, t + 1);
+        if (t + 1 < steps) request(odd, t + 1), use(even, t), use(odd, t + 1);
+        else use(even, t);
     }
     if (!in || slot >= job.slots) return;                       // (no partition makes that many: offsets that are none must not write elsewhere)
     const float s = (job.scale ? job.scale[e] : 1.0f), whole = DT == MOE_F16 ? exp2i(unit) : 1.0f;
@@ -137,11 +172,11 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
         }
 }
 
-template <int DT0, int DT1, int NT>
-__global__ __launch_bounds__(64) void adapter_outer_kernel(OuterArgs p)
+template <int DT0, int DT1, int NT, int TERMS>
+__global__ __launch_bounds__(64, NT <= 2 ? 3 : 1) void adapter_outer_kernel(OuterArgs p)
 {
-    if ((int)blockIdx.x < p.first) outer_item<DT0, NT>(p, p.job[0], blockIdx.x);
-    else outer_item<DT1, NT>(p, p.job[1], blockIdx.x - p.first);
+    if ((int)blockIdx.x < p.first) outer_item<DT0, NT, DT0 == MOE_BF16 ? TERMS : 2>(p, p.job[0], blockIdx.x);
+    else outer_item<DT1, NT, DT1 == MOE_BF16 ? TERMS : 2>(p, p.job[1], blockIdx.x - p.first);
 }
 
 // Sums of the chunks of adapters that have more than one, in their order.  blockIdx.y: the how manieth such adapter, blockIdx.z: the job.
@@ -196,7 +231,9 @@ int launch_adapter_outer(const OuterArgs &args, int dtype0, int dtype1, hipStrea
     auto run = [&](auto d0, auto d1) {
         constexpr int D0 = decltype(d0)::value, D1 = decltype(d1)::value;
         auto start = [&](auto nt) {
-            hipLaunchKernelGGL((adapter_outer_kernel<D0, D1, decltype(nt)::value>), dim3((unsigned)(blocks[0] + blocks[1])), dim3(64), 0, s, p);
+            constexpr int NT = decltype(nt)::value;
+            const auto kernel = p.out_dtype == MOE_F32 ? &adapter_outer_kernel<D0, D1, NT, 3> : &adapter_outer_kernel<D0, D1, NT, 2>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks[0] + blocks[1])), dim3(64), 0, s, p);
             return check_launch(what);
         };
         using std::integral_constant;

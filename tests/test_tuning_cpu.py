@@ -56,6 +56,7 @@ def test_adapter_refusals(lib):
             assert call(lib, **bad) == ARG, (call.__name__, bad, lib.moe_last_error())
         for bad in (dict(rank=129), dict(E=4097), dict(dt=F32), dict(ydt=4), dict(K=2 ** 20 + 8, xs=2 ** 20 + 8)):
             assert call(lib, **bad) == UNSUPPORTED, (call.__name__, bad)
+    assert _adapters(lib, v=ODD) == ARG and _adapters(lib, v=None, R=514, T=257, y=ODD) == ARG and _adapters(lib, v=None, R=514, T=257) == ARG and b"NULL" in lib.moe_last_error()
     for bad in (dict(y=ODD), dict(out=ODD), dict(out=None), dict(ys=64), dict(os=64), dict(ys=76), dict(ys=80)):      # (the last: in place with two strides)
         assert _adapters(lib, **bad) == ARG, bad
     for bad in (dict(dy=None), dict(dy=ODD), dict(dys=64), dict(v=None), dict(v=ODD), dict(ws=ODD), dict(dx=ODD), dict(dxs=56), dict(da=ODD), dict(db=ODD)):
