@@ -64,9 +64,9 @@ struct AdapterArgs {
     float *coef;                // [R, rank], or null (one launch does without)
     int coef_scaled;            // coef holds scale * (A x)
     int ncol;                   // slices of N, each a block's
-    int width;                  // channels of a slice, a multiple of 64 (one launch)
+    int width;                  // channels of a slice, a multiple of 64
     int items;                  // blocks for rows of adapters; those behind them copy the others
-    int share;                  // many rows: those of a block, about
+    int share;                  // rows of a block, about
 };
 
 // out[e][j] = scale sum_r coef[r][j] rows[r]

@@ -278,48 +278,40 @@ __device__ inline void copy_rows(const AdapterArgs &p, int block, int waves)
     }
 }
 
-// ---- few rows: a block takes up to 16 rows of an adapter and a slice of N, its W wavefronts split K and the slice ------------------------------------
-
-template <int XDT, int WDT, int ODT, bool Y, int W, int NT>
-__global__ __launch_bounds__(64 * W) void adapter_few_kernel(AdapterArgs p)
-{
-    using S = AdapterShape<WDT, ODT, W, 1, NT>;
-    extern __shared__ __align__(16) uint8_t lds[];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if ((int)blockIdx.x >= p.items) return copy_rows<ODT, Y>(p, blockIdx.x - p.items, W);
-    int e, col, row0, rows;
-    if (!find_item<16>(p.offsets, p.E, p.R, 16, p.ncol, blockIdx.x, &e, &col, &row0, &rows)) return;
-    e = __builtin_amdgcn_readfirstlane(e), col = __builtin_amdgcn_readfirstlane(col);
-    row0 = __builtin_amdgcn_readfirstlane(row0), rows = __builtin_amdgcn_readfirstlane(rows);
-    find_places<S>(p, lds, row0, rows);
-    float4_t acc[1][NT] = {};
-    multiply_rows<XDT, WDT, S::D, W, 1, NT>(p, e, row0, rows, wave, acc);
-    make_terms<S, WDT, W, 1, NT>(p, lds, acc, e, row0, rows, wave, p.coef && col == 0);
-    if (!p.out) return;                                         // (coefficients alone)
-    __syncthreads();
-    expand_rows<S, WDT, ODT, Y, W, 1>(p, lds, e, rows, wave, col * p.width, min(p.N, (col + 1) * p.width));
-}
-
-// ---- many rows -------------------------------------------------------------------------------------------------------------------------------------
+// ---- one launch: a block takes rows of an adapter and a slice of N, its W wavefronts split K and the slice ---------------------------------------------
 //
-// All blocks run at once, one per compute unit, and share the memory's rate, so the one with the most to read is waited for: an adapter's rows are cut into as many blocks of `share` rows
-// as come nearest, evenly, rather than into full ones and a rest.
+// All blocks run at once, one per compute unit where there are as many, and share the memory's rate, so the one with the most to read is waited for: an adapter's rows are cut into as many
+// parts of `share` rows as come nearest, evenly, rather than into full tiles and a rest.  Neighbouring parts lie on one XCD (as find_item deals them), whose cache then holds their adapter.
 
-// The block's adapter and rows.  Every wavefront computes the same.
-__device__ inline bool find_share(const AdapterArgs &p, int most, int *e, int *row0, int *rows)
+// The block's adapter, slice and rows.  Every wavefront computes the same.
+__device__ inline bool find_share(const AdapterArgs &p, int most, int *e, int *col, int *row0, int *rows)
 {
     const int lane = threadIdx.x & 63;
+    int lo, hi, parts, incl;                                    // this lane's adapter of a chunk of 64: its rows, its parts, and the chunk's parts up to its own
+    auto load = [&](int e0) {
+        lo = hi = 0;
+        if (e0 + lane < p.E) expert_range(p.offsets, e0 + lane, p.R, &lo, &hi);
+        const int n = hi - lo;
+        parts = n ? max(max((n + p.share / 2) / p.share, (n + most - 1) / most), 1) : 0;
+        incl = wave_inclusive_sum(parts);
+    };
+    load(0);
+    const int lo0 = lo, hi0 = hi, parts0 = parts, incl0 = incl;             // (with up to 64 adapters the offsets are read once)
+    int total = __shfl(incl, 63);
+    for (int e0 = 64; e0 < p.E; e0 += 64) load(e0), total += __shfl(incl, 63);
+    const int chunk = (total * p.ncol + kXcds - 1) / kXcds, within = blockIdx.x / kXcds, item = blockIdx.x % kXcds * chunk + within;
+    if (within >= chunk || item >= total * p.ncol) return false;
+    const int part = item / p.ncol;
     int base = 0;
     for (int e0 = 0; e0 < p.E; e0 += 64) {
-        int lo = 0, hi = 0;
-        if (e0 + lane < p.E) expert_range(p.offsets, e0 + lane, p.R, &lo, &hi);
-        const int n = hi - lo, parts = n ? max(max((n + p.share / 2) / p.share, (n + most - 1) / most), 1) : 0, incl = wave_inclusive_sum(parts);
-        const uint64_t hit = __ballot(base + incl > (int)blockIdx.x);
+        if (p.E > 64) load(e0);
+        else lo = lo0, hi = hi0, parts = parts0, incl = incl0;
+        const uint64_t hit = __ballot(base + incl > part);
         if (hit) {
             const int src = __ffsll((unsigned long long)hit) - 1;
-            const int count = __shfl(parts, src), i = blockIdx.x - base - __shfl(incl - parts, src), size = __shfl(n, src), first = __shfl(lo, src);
+            const int count = __shfl(parts, src), i = part - base - __shfl(incl - parts, src), size = __shfl(hi - lo, src), first = __shfl(lo, src);
             const int per = size / count, extra = size % count;
-            *e = __builtin_amdgcn_readfirstlane(e0 + src);
+            *e = __builtin_amdgcn_readfirstlane(e0 + src), *col = __builtin_amdgcn_readfirstlane(item % p.ncol);
             *row0 = __builtin_amdgcn_readfirstlane(first + i * per + min(i, extra));
             *rows = __builtin_amdgcn_readfirstlane(per + (i < extra ? 1 : 0));
             return true;
@@ -329,73 +321,77 @@ __device__ inline bool find_share(const AdapterArgs &p, int most, int *e, int *r
     return false;
 }
 
-template <int XDT, int WDT, int ODT, bool Y, int MT, int NT>
-__global__ __launch_bounds__(512, 2) void adapter_many_kernel(AdapterArgs p)
+template <int XDT, int WDT, int ODT, bool Y, int W, int MT, int NT>
+__global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void adapter_kernel(AdapterArgs p)
 {
-    constexpr int W = 8;
     using S = AdapterShape<WDT, ODT, W, MT, NT>;
     extern __shared__ __align__(16) uint8_t lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if ((int)blockIdx.x >= p.items) return copy_rows<ODT, Y>(p, blockIdx.x - p.items, W);
-    int e, row0, rows;
-    if (!find_share(p, S::BM, &e, &row0, &rows)) return;
+    int e, col, row0, rows;
+    if (!find_share(p, S::BM, &e, &col, &row0, &rows)) return;
     find_places<S>(p, lds, row0, rows);
     float4_t acc[MT][NT] = {};
     multiply_rows<XDT, WDT, S::D, W, MT, NT>(p, e, row0, rows, wave, acc);
-    make_terms<S, WDT, W, MT, NT>(p, lds, acc, e, row0, rows, wave, true);
-    if (!p.out) return;
+    make_terms<S, WDT, W, MT, NT>(p, lds, acc, e, row0, rows, wave, p.coef && col == 0);
+    if (!p.out) return;                                         // (coefficients alone)
     __syncthreads();
-    expand_rows<S, WDT, ODT, Y, W, MT>(p, lds, e, rows, wave, 0, p.N);
+    expand_rows<S, WDT, ODT, Y, W, MT>(p, lds, e, rows, wave, col * p.width, min(p.N, (col + 1) * p.width));
 }
 
 // ---- launches --------------------------------------------------------------------------------------------------------------------------------------
 
-template <class Kernel>
-static int launch_blocks(Kernel kernel, std::atomic<uint64_t> &raised, AdapterArgs p, long items, int W, int lds, hipStream_t s, const char *what)
+template <int XDT, int WDT, int ODT, bool Y, int W, int MT, int NT>
+static int launch_shape(AdapterArgs p, int share, int slices, hipStream_t s, const char *what)
 {
+    constexpr int kLds = AdapterShape<WDT, ODT, W, MT, NT>::kLds;
+    p.share = share;
+    p.width = p.out ? (int)round_up(((size_t)p.N + slices - 1) / slices, 64) : p.N;
+    p.ncol = (p.N + p.width - 1) / p.width;
+    const long parts = (long)p.R / share + (p.E < p.R ? p.E : p.R);             // an upper bound: of n rows at most n / share + 1
+    const long items = (parts * p.ncol + kXcds - 1) / kXcds * kXcds;
     const int need = p.y == p.out || !p.out ? 0 : (p.R + W - 1) / W, copies = need < 256 ? need : 256;          // blocks for rows of no adapter
     if ((items + copies) * W > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %ld workgroups exceed one launch", what, items);
     p.items = (int)items;
-    if (lds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(kernel), lds, raised);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(items + copies)), dim3(64 * W), lds, s, p);
+    static std::atomic<uint64_t> raised;
+    const auto kernel = &adapter_kernel<XDT, WDT, ODT, Y, W, MT, NT>;
+    if (kLds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(kernel), kLds, raised);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(items + copies)), dim3(64 * W), kLds, s, p);
     return check_launch(what);
 }
 
 template <int XDT, int WDT, int ODT, bool Y, int NT>
-static int launch_few(AdapterArgs p, int slices, hipStream_t s, const char *what)
+static int launch_rank(const AdapterArgs &p, hipStream_t s, const char *what)
 {
-    constexpr int W = NT <= 2 ? 16 : 8;
-    if (!p.out) slices = 1;
-    p.width = (int)round_up(((size_t)p.N + slices - 1) / slices, 64);
-    p.ncol = (p.N + p.width - 1) / p.width;
-    const long slots = (long)p.R / 16 + (p.E < p.R ? p.E : p.R);                 // upper bound of the work items, whole rounds of XCDs
-    static std::atomic<uint64_t> raised;
-    return launch_blocks(&adapter_few_kernel<XDT, WDT, ODT, Y, W, NT>, raised, p, (slots * p.ncol + kXcds - 1) / kXcds * kXcds, W, AdapterShape<WDT, ODT, W, 1, NT>::kLds, s, what);
-}
-
-template <int XDT, int WDT, int ODT, bool Y, int MT, int NT>
-static int launch_many(const AdapterArgs &p, int blocks, hipStream_t s, const char *what)
-{
-    static std::atomic<uint64_t> raised;
-    return launch_blocks(&adapter_many_kernel<XDT, WDT, ODT, Y, MT, NT>, raised, p, blocks, 8, AdapterShape<WDT, ODT, 8, MT, NT>::kLds, s, what);
-}
-
-template <int XDT, int WDT, int ODT, bool Y, int NT>
-static int launch_rank(AdapterArgs p, hipStream_t s, const char *what)
-{
-    constexpr int kUnits = 256, kMost = NT <= 2 ? 80 : NT == 4 ? 64 : 48;       // compute units; rows that a block can hold
-    const int used = p.E < p.R ? p.E : p.R;
-    const long tiles = p.R / 16 + used;                         // that rows spread evenly over the adapters would make
-    if (!p.coef || tiles <= 256) return launch_few<XDT, WDT, ODT, Y, NT>(p, (int)(256 / tiles < 1 ? 1 : 256 / tiles > 8 ? 8 : 256 / tiles), s, what);
-    // rounds of blocks; in each a few fewer than compute units, as parts are rounded one way or the other
-    const long rounds = ((long)p.R + (kUnits - 8) * (kMost - 8) - 1) / ((kUnits - 8) * (kMost - 8));
-    p.share = (int)((p.R + (kUnits - 8) * rounds - 1) / ((kUnits - 8) * rounds));
-    const long slots = (long)p.R / p.share + used;              // an upper bound: of n rows at most n / share + 1
-    if (slots > 0x7fffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows of %d adapters are too many", what, p.R, p.E);
-    if constexpr (NT <= 2) {
-        if (p.share <= 24) return launch_many<XDT, WDT, ODT, Y, 2, NT>(p, (int)slots, s, what);
+    constexpr int kUnits = 248, kMost = NT <= 2 ? 80 : NT == 4 ? 64 : 48;       // a few fewer than compute units, as parts are rounded one way or the other; rows that a block can hold
+    const long even = ((long)p.R + kUnits - 1) / kUnits;
+    if (!p.coef || even <= 16) {
+        // Few rows: parts of an adapter's rows and slices of N such that what a block moves (its rows of x, A, and its slice of y, out and B), times the rounds of blocks, is least.  What a
+        // block takes to begin and to join its sums is as long as 96 KB.
+        constexpr int W = NT <= 2 ? 16 : 8;
+        constexpr int kParts[] = {16, 12, 10, 8, 6, 4, 3, 2, 1};
+        const int used = p.E < p.R ? p.E : p.R, mean = (p.R + used - 1) / used;
+        const float per_row = (float)p.K * size_of(XDT), per_slice = p.out ? (float)p.N * size_of(ODT) * (Y ? 2 : 1) : 0, a_bytes = 2.0f * p.rank * p.K, b_bytes = p.out ? 2.0f * p.rank * p.N : 0;
+        int slices = 1, share = 16;
+        float least = 0;
+        for (const int rows : kParts) {
+            if (rows < 16 && rows >= mean) continue;            // (an adapter's rows in one part, as with sixteen)
+            const int held = rows < mean ? rows : mean, parts = rows < mean ? p.R / rows + used / 2 : used;
+            for (int n = 1; n <= (p.out ? 8 : 1); ++n) {
+                const int rounds = (parts * n + kUnits - 1) / kUnits;
+                const float cost = rounds * (96e3f + held * per_row + a_bytes + (held * per_slice + b_bytes) / n);
+                if (least == 0 || cost < least) least = cost, slices = n, share = rows;
+            }
+        }
+        return launch_shape<XDT, WDT, ODT, Y, W, 1, NT>(p, share, slices, s, what);
     }
-    return launch_many<XDT, WDT, ODT, Y, kMost / 16, NT>(p, (int)slots, s, what);
+    const long rounds = ((long)p.R + kUnits * (kMost - 8) - 1) / (kUnits * (kMost - 8));
+    const int share = (int)((p.R + kUnits * rounds - 1) / (kUnits * rounds));
+    if constexpr (NT <= 2) {
+        if (share <= 26) return launch_shape<XDT, WDT, ODT, Y, 8, 2, NT>(p, share, 1, s, what);
+        if (share <= 42) return launch_shape<XDT, WDT, ODT, Y, 8, 3, NT>(p, share, 1, s, what);
+    }
+    return launch_shape<XDT, WDT, ODT, Y, 8, kMost / 16, NT>(p, share, 1, s, what);
 }
 
 template <int XDT, int WDT, int ODT, bool Y>
