@@ -425,7 +425,8 @@ int moe_balance_loss_backward(const void *logits, int dtype, const int32_t *expe
 /*
  * Gradient of sorting tokens by expert and back (moe_permute, moe_combine):
  *   moe_combine_backward: dy_perm[inv_perm[a]] = expert_scale[a] * dout[a / k], dscale[a] = <dout[a / k], y_perm[inv_perm[a]]>, a = t*k + j < T*k
- *     dout [T,d] out_dtype; y_perm, dy_perm [R,d] y_dtype; inv_perm, expert_scale [T*k] as for moe_combine; dscale [T,k] fp32
+ *     dout [T,d] out_dtype; y_perm, dy_perm [R,d] y_dtype; inv_perm, expert_scale [T*k] as for moe_combine; dscale [T,k] fp32.  dy_perm or dscale may be NULL (not wanted; without dscale
+ *     y_perm is not read).
  *   moe_permute_backward: dx[t] = sum_j dx_perm[inv_perm[t*k+j]]  (fp32, j ascending; one rounding)
  *     dx_perm [R,d] perm_dtype; dx [T,d] dx_dtype
  * Types MOE_F16 | MOE_BF16 | MOE_F32.  active_rows: as for moe_combine, or NULL.  An assignment whose row is at or past it (or outside [0, R)) belongs to a pruned token: its

@@ -5,10 +5,13 @@ device pointers into its C entry points (loaded on first use, and failing loudly
 library has not been built).  ``workloads`` holds the seeded synthetic input generators.
 """
 
-from . import binding, layer, mx4_layer, router, workloads  # noqa: E402,F401
+from . import adapters, binding, exchange, layer, mx4_layer, optimizer, router, workloads  # noqa: E402,F401
 from .layer import MoEExpertLayer  # noqa: E402,F401
 from .mx4_layer import MoEMx4Layer  # noqa: E402,F401
 from .router import balance_loss  # noqa: E402,F401
+from .exchange import combine_tokens, permute_tokens  # noqa: E402,F401
+from .adapters import AdapterIndex, LowRankAdapters, adapt, adapter_index  # noqa: E402,F401
+from .optimizer import AdamW  # noqa: E402,F401
 from .binding import (MoeError, moe_combine, moe_gate_topk, moe_grouped_ffn_wq,  # noqa: E402,F401
                       moe_grouped_ffn_wq_workspace_bytes, moe_permute, moe_permute_workspace_bytes,
                       moe_quantize_experts)

@@ -670,23 +670,23 @@ def _check_device(*tensors):
             raise MoeError("a tensor is on device %d, the current device is %d" % (t.get_device(), here))
 
 
-def moe_combine_backward(dout, y_perm, inv_perm, expert_scale, active_rows=None, out=None):
-    """Gradient of moe_combine: (dy_perm like y_perm, dscale fp32 [T, k]) of dout [T, d]; rows of pruned assignments are 0."""
+def moe_combine_backward(dout, y_perm, inv_perm, expert_scale, active_rows=None, out=None, need=(True, True)):
+    """Gradient of moe_combine: (dy_perm like y_perm, dscale fp32 [T, k]) of dout [T, d]; rows of pruned assignments are 0.  `need` says which of the two (None for the other)."""
     if dout.dim() != 2 or expert_scale.dim() != 2 or y_perm.dim() != 2:
         raise MoeError("dout must be [T, d], y_perm [R, d] and expert_scale [T, k]")
     (T, d), (R, width), k = dout.shape, y_perm.shape, expert_scale.shape[1]
     if width != d or expert_scale.shape[0] != T or inv_perm.numel() != T * k or (active_rows is not None and active_rows.numel() < 1):
         raise MoeError("y_perm must be [R, %d], expert_scale [%d, k] and inv_perm [T * k]" % (d, T))
     if out is None:
-        if R == T * k:
-            dy = torch.empty_like(y_perm)
-        else:
-            dy = torch.zeros_like(y_perm)                               # (rows that belong to none of these tokens)
-        dscale = torch.empty(T, k, dtype=torch.float32, device=dout.device)
+        # (rows that belong to none of these tokens, where there are more, are 0)
+        dy = None if not need[0] else torch.empty_like(y_perm) if R == T * k else torch.zeros_like(y_perm)
+        dscale = torch.empty(T, k, dtype=torch.float32, device=dout.device) if need[1] else None
     else:
-        dy, dscale = out
-        if dy.shape != y_perm.shape or dscale.shape != (T, k):
+        dy, dscale = (t if n else None for t, n in zip(out, need))
+        if (dy is not None and dy.shape != y_perm.shape) or (dscale is not None and dscale.shape != (T, k)):
             raise MoeError("out must be [R, d] and [T, k]")
+    if dy is None and dscale is None:
+        return None, None
     _check_device(dout, y_perm, inv_perm, expert_scale, active_rows, dy, dscale)
     rc = load().moe_combine_backward(_ptr(dout, _FLOATS, "dout"), _DT[dout.dtype], _ptr(y_perm, _FLOATS, "y_perm"), _DT[y_perm.dtype], _ptr(inv_perm, torch.int32, "inv_perm"),
                                      _ptr(expert_scale, torch.float32, "expert_scale"), _ptr(active_rows, torch.int32, "active_rows"), T, k, d, R,

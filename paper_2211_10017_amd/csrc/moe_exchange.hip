@@ -15,41 +15,52 @@ struct ExchangeArgs {
     const float *scale;             // [T k]
     const int32_t *active_rows;     // [1] or null
     int T, k, d, R;
-    void *dy;                       // [R, d]
-    float *dscale;                  // [T k]
+    void *dy;                       // [R, d] or null
+    float *dscale;                  // [T k] or null
     void *dx;                       // [T, d]
 };
 
-// A wavefront per token; ds is summed over its lanes.
-template <int ODT, int YDT>
+// A wavefront per token; ds is summed over its lanes.  K: rows of a token, 0 for any number, one after the other.  With K known a step's loads of all of its rows are requested together.
+template <int ODT, int YDT, int K>
 __global__ __launch_bounds__(256) void combine_backward_kernel(ExchangeArgs p)
 {
-    constexpr int V = ODT == MOE_F32 || YDT == MOE_F32 ? 4 : 8;
+    constexpr int V = ODT == MOE_F32 || YDT == MOE_F32 ? 4 : 8, N = K ? K : 1;
     const int lane = threadIdx.x & 63, steps = p.d / V;
     const int active = min(p.active_rows ? *p.active_rows : p.R, p.R);
     for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < p.T; t += gridDim.x * 4) {
-        for (int j = 0; j < p.k; ++j) {
-            const size_t a = (size_t)t * p.k + j;
-            const int r = p.inv[a];
-            const bool live = r >= 0 && r < active;
-            const float s = live ? p.scale[a] : 0.0f;
-            float sum = 0.0f;
+        for (int j0 = 0; j0 < (K ? 1 : p.k); ++j0) {
+            const size_t a = (size_t)t * (K ? K : p.k) + j0;
+            int r[N];
+            float s[N], sum[N] = {};
+            bool live[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) r[j] = p.inv[a + j], s[j] = p.scale[a + j];
+#pragma unroll
+            for (int j = 0; j < N; ++j) live[j] = r[j] >= 0 && r[j] < active;
+#pragma unroll 2
             for (int c = lane; c < steps; c += 64) {
                 Raw<ODT, V> o;
-                Raw<YDT, V> y, dy;
-                dy.clear();
-                if (live) {
-                    o.load(p.dout, (size_t)t * p.d + c * V);
-                    y.load(p.y, (size_t)r * p.d + c * V);
+                Raw<YDT, V> y[N];
+                o.load(p.dout, (size_t)t * p.d + c * V);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    if (p.dscale && live[j]) y[j].load(p.y, (size_t)r[j] * p.d + c * V);
+                    else y[j].clear();
+                }
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
                     float v[V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) sum = fmaf(o.get(i), y.get(i), sum), v[i] = s * o.get(i);
-                    dy.set(v);
+                    for (int i = 0; i < V; ++i) sum[j] = live[j] ? fmaf(o.get(i), y[j].get(i), sum[j]) : 0.0f, v[i] = live[j] ? s[j] * o.get(i) : 0.0f;
+                    if (p.dy && r[j] >= 0 && r[j] < p.R) y[j].set(v), y[j].store(p.dy, (size_t)r[j] * p.d + c * V);
                 }
-                if (r >= 0 && r < p.R) dy.store(p.dy, (size_t)r * p.d + c * V);
             }
-            sum = wave_sum(sum);
-            if (lane == 0) p.dscale[a] = sum;
+            if (!p.dscale) continue;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                sum[j] = wave_sum(sum[j]);
+                if (lane == 0) p.dscale[a + j] = sum[j];
+            }
         }
     }
 }
@@ -94,13 +105,15 @@ extern "C" int moe_combine_backward(const void *dout, int out_dtype, const void 
     const char *what = "moe_combine_backward";
     if (const int rc = check_exchange(what, T, k, d, R, out_dtype, y_dtype)) return rc;
     if (T == 0) return MOE_OK;                                      // empty buffers may be NULL
-    if (!dout || !inv_perm || !expert_scale || !dscale || (R > 0 && (!y_perm || !dy_perm))) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!dout || !inv_perm || !expert_scale || (!dscale && !dy_perm) || (R > 0 && dscale && !y_perm)) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(dout) || !aligned16(y_perm) || !aligned16(dy_perm)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
     const ExchangeArgs p{dout, y_perm, inv_perm, expert_scale, active_rows, T, k, d, R, dy_perm, dscale, nullptr};
     const int blocks = (int)(((long)T + 3) / 4 < 0x100000 ? ((long)T + 3) / 4 : 0x100000);
     return with_dtype(out_dtype, [&](auto o) {
         return with_dtype(y_dtype, [&](auto y) {
-            hipLaunchKernelGGL((combine_backward_kernel<decltype(o)::value, decltype(y)::value>), dim3(blocks), dim3(256), 0, as_stream(stream), p);
+            constexpr int O = decltype(o)::value, Y = decltype(y)::value;
+            const auto kernel = k == 1 ? &combine_backward_kernel<O, Y, 1> : k == 2 ? &combine_backward_kernel<O, Y, 2> : &combine_backward_kernel<O, Y, 0>;
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, as_stream(stream), p);
             return check_launch(what);
         });
     });

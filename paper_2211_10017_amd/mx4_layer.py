@@ -5,6 +5,7 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
+from .adapters import AdapterIndex
 
 
 class MoEMx4Layer:
@@ -25,6 +26,7 @@ class MoEMx4Layer:
         shapes = B.moe_mx4_shapes
         self.w1, self.w2 = (tuple(torch.empty((E,) + s, **u8) for s in shapes(n, K)) for n, K in ((F, d), (d, F)))      # (codes, scales)
         self.b1 = self.b2 = self.gate_bias = None
+        self.adapters = None                                                # LowRankAdapters(E, rank, d, d, act_dtype): an adapter beside each expert
         self.wg = torch.empty((d, E), dtype=act_dtype, device=dev)
         # per-call buffers; y is kept in fp32 for bf16 rows, as in MoEExpertLayer
         self.expert_idx = torch.empty((T, k), **i32)
@@ -52,8 +54,17 @@ class MoEMx4Layer:
 
     def experts(self, x):
         """y of every assignment, [T * k, d], in the sorted order of the last route()."""
-        return B.moe_grouped_ffn_mx4(x, self.expert_offsets, *self.w1, *self.w2, b1=self.b1, b2=self.b2, perm_src=self.perm_src, k=self.k, y_perm=self.y_perm,
-                                     activation=self.activation, max_rows_per_expert=self.T, workspace=self.ws_ffn)
+        B.moe_grouped_ffn_mx4(x, self.expert_offsets, *self.w1, *self.w2, b1=self.b1, b2=self.b2, perm_src=self.perm_src, k=self.k, y_perm=self.y_perm,
+                              activation=self.activation, max_rows_per_expert=self.T, workspace=self.ws_ffn)
+        if self.adapters is not None:
+            self.adapters.add(x, self.y_perm, self.index(), by_assignment=False)
+        # (written through a pointer: a backward pass that still needs the last call's rows raises)
+        torch.autograd.graph.increment_version(self.y_perm)
+        return self.y_perm
+
+    def index(self):
+        """The last route()'s index, as adapters take it; the next one writes it again."""
+        return AdapterIndex(self.perm_src, self.inv_perm, self.expert_offsets, self.k)
 
     def forward(self, x, finished=None):
         self.route(x, finished)

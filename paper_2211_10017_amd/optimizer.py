@@ -1,0 +1,68 @@
+"""AdamW over many tensors in one launch, states in 32 or 8 bits (moe_adamw, include/moe_wq.h)."""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+_HALVES = (torch.float16, torch.bfloat16)
+
+
+class AdamW:
+    """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass.  step() takes the gradients that are there; a parameter
+    without one stays as it is."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, bits=32):
+        self.params = list(params)
+        if bits not in (8, 32):
+            raise B.MoeError("states have 8 or 32 bits")
+        if not self.params or any(p.dtype not in _HALVES + (torch.float32,) or not p.is_contiguous() for p in self.params):
+            raise B.MoeError("parameters must be contiguous tensors of fp16, bf16 or fp32")
+        if len({p.data_ptr() for p in self.params if p.numel()}) < sum(p.numel() > 0 for p in self.params):
+            raise B.MoeError("a parameter is in the list twice")
+        self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.steps = lr, tuple(betas), eps, weight_decay, bits, 0
+        self.masters = [p.detach().float() if p.dtype in _HALVES else None for p in self.params]
+
+        def state(p):
+            if bits == 32:
+                return torch.zeros(p.numel(), dtype=torch.float32, device=p.device)
+            return tuple(torch.zeros(n, dtype=torch.uint8, device=p.device) for n in (p.numel(), (p.numel() + 31) // 32))
+
+        self.exp_avg, self.exp_avg_sq = ([state(p) for p in self.params] for _ in range(2))
+
+    def step(self, grad_scale: float = 1.0):
+        self.steps += 1
+        groups = {}
+        for i, p in enumerate(self.params):
+            if p.grad is not None:
+                if p.grad.is_sparse:
+                    raise B.MoeError("gradients must be dense")
+                groups.setdefault((p.dtype if self.masters[i] is not None else None, p.grad.dtype), []).append(i)
+        for (half, _), at in groups.items():
+            params = [self.params[i].detach() for i in at]
+            B.moe_adamw([self.masters[i] for i in at] if half else params, [self.params[i].grad.contiguous() for i in at], [self.exp_avg[i] for i in at], [self.exp_avg_sq[i] for i in at],
+                        self.steps, self.lr, self.betas, self.eps, self.weight_decay, grad_scale, copies=params if half else None)
+            # (written through pointers: a backward pass that still needs the old values raises)
+            torch.autograd.graph.increment_version(params)
+
+    def zero_grad(self, set_to_none: bool = True):
+        for p in self.params:
+            if p.grad is not None:
+                if set_to_none:
+                    p.grad = None
+                else:
+                    p.grad.zero_()
+
+    def state_dict(self):
+        return dict(steps=self.steps, bits=self.bits, masters=self.masters, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq)
+
+    def load_state_dict(self, state):
+        if state["bits"] != self.bits or len(state["exp_avg"]) != len(self.params):
+            raise B.MoeError("the state belongs to other parameters, or has other bits")
+        flat = lambda s: [t for x in s for t in (x if isinstance(x, tuple) else (x,)) if t is not None]  # noqa: E731
+        mine, theirs = (flat(s["masters"]) + flat(s["exp_avg"]) + flat(s["exp_avg_sq"]) for s in (self.state_dict(), state))
+        if [t.shape for t in mine] != [t.shape for t in theirs]:
+            raise B.MoeError("the state belongs to other parameters")
+        for m, t in zip(mine, theirs):
+            m.copy_(t)
+        self.steps = state["steps"]

@@ -34,6 +34,10 @@ def test_combine_backward(T, k, d, out_dt, y_dt, load):
     within(dscale, (o * rows).sum(1).view(T, k), (d + 1) * U * (o * rows).abs().sum(1).view(T, k))
     assert bool((dy[active:] == 0).all()) and bool((dscale[~live.view(T, k)] == 0).all())
     assert torch.equal(again[0], dy) and torch.equal(again[1], dscale)
+    only = B.moe_combine_backward(dout, y, inv, scale, active_rows=offsets[E:], need=(True, False))
+    assert torch.equal(only[0], dy) and only[1] is None
+    only = B.moe_combine_backward(dout, y, inv, scale, active_rows=offsets[E:], need=(False, True))
+    assert only[0] is None and torch.equal(only[1], dscale)
 
 
 @pytest.mark.parametrize("in_dt,out_dt", [(F16, F16), (BF16, BF16), (F32, F32), (F32, BF16), (F16, F32), (BF16, F32), (F32, F16), (F16, BF16), (BF16, F16)])

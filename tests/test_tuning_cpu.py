@@ -25,8 +25,9 @@ def test_exchange_refusals(lib):
     def permute(g=P, gdt=F16, inv=P, T=4, k=2, d=64, R=8, dx=P, dt=F32):
         return lib.moe_permute_backward(g, gdt, inv, None, T, k, d, R, dx, dt, None)
 
-    for name in ("dout", "y", "inv", "scale", "dy", "ds"):
+    for name in ("dout", "y", "inv", "scale"):
         assert combine(**{name: None}) == ARG and b"NULL" in lib.moe_last_error(), name
+    assert combine(dy=None, ds=None) == ARG and combine(dy=None, y=None) == ARG
     for name in ("dout", "y", "dy"):
         assert combine(**{name: ODD}) == ARG and b"aligned" in lib.moe_last_error(), name
     for name in ("g", "inv", "dx"):
