@@ -85,6 +85,7 @@ struct AdapterShape {
     static constexpr int BM = 16 * MT, J = 16 * NT;             // rows, and the rank in whole products
     static constexpr int D = (W == 16 ? 40 : 96) / (4 * (MT + NT)) < 2 ? 2 : (W == 16 ? 40 : 96) / (4 * (MT + NT)) > 6 ? 6 : (W == 16 ? 40 : 96) / (4 * (MT + NT));
     static constexpr int kParts = W == 8 && NT >= 4 ? W / 2 : W, kRed = J + 4;              // wavefronts' sums at a time; rows padded against bank conflicts
+    static constexpr int CL = ODT != MOE_F32 && W == 8 && NT <= 2 ? 8 : 4;                   // channels of a lane in phase two
     static constexpr int KI = NT == 1 ? 16 : 32, NC = J / KI, JL = KI / 4;                  // phase two: inner size of a product, products over the rank, rank of a lane in one
     static constexpr int TERMS = WDT == MOE_BF16 && ODT == MOE_F32 ? 3 : 2, kTermRow = TERMS * J + 8;
     static constexpr int kTerms = kParts * BM * kRed * 4, kUnit = kTerms + BM * kTermRow * 2, kPlace = kUnit + BM * 4, kLds = kPlace + BM * 16;
@@ -160,28 +161,28 @@ __device__ inline void make_terms(const AdapterArgs &p, uint8_t *lds, float4_t (
     }
 }
 
-// Phase two: coefficients times B, 64 channels at a time, every W-th of them from `first` to `end`.  A lane puts B's columns together from four neighbouring channels of its rows, once for
+// Phase two: coefficients times B, 16 CL channels at a time, every W-th of them from `first` to `end`.  A lane puts B's columns together from CL neighbouring channels of its rows, once for
 // all of the item's rows.  The next channels' operands are requested as soon as this one's registers are free.
 template <class S, int WDT, int ODT, bool Y, int W, int MT>
 __device__ inline void expand_rows(const AdapterArgs &p, const uint8_t *lds, int e, int rows, int wave, int first, int end)
 {
-    constexpr int J = S::J, KI = S::KI, NC = S::NC, JL = S::JL;
+    constexpr int J = S::J, KI = S::KI, NC = S::NC, JL = S::JL, CL = S::CL;
     typedef uint32_t operand_t __attribute__((ext_vector_type(JL / 2)));
     const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, N = p.N, rank = p.rank;
     const uint16_t *terms = reinterpret_cast<const uint16_t *>(lds + S::kTerms), *b = reinterpret_cast<const uint16_t *>(p.b) + (size_t)e * rank * N;
     const float *unit = reinterpret_cast<const float *>(lds + S::kUnit);
     const size_t *place = reinterpret_cast<const size_t *>(lds + S::kPlace);                // of the rows in y and in out
-    const int groups = (end - first + 63) / 64;
+    const int groups = (end - first + 16 * CL - 1) / (16 * CL);
     if (wave >= groups) return;
-    Raw<ODT, 4> y[MT][4];
-    uint2 raw[NC][JL];
-    auto channel = [&](int group) { return min(first + group * 64 + 4 * l, end - 4); };     // (past the end: the last ones again, which are not stored)
+    Raw<ODT, CL> y[MT][4];
+    Raw<WDT, CL> raw[NC][JL];
+    auto channel = [&](int group) { return min(first + (group * 16 + l) * CL, end - CL); };          // (past the end: the last ones again, which are not stored)
     auto request_b = [&](int group) {
         const int c = channel(group);
 #pragma unroll
         for (int n = 0; n < NC; ++n)
 #pragma unroll
-            for (int i = 0; i < JL; ++i) raw[n][i] = *reinterpret_cast<const uint2 *>(b + (size_t)(uint32_t)(min(KI * n + JL * g + i, rank - 1) * N + c));
+            for (int i = 0; i < JL; ++i) raw[n][i].load(b, (size_t)(uint32_t)(min(KI * n + JL * g + i, rank - 1) * N + c));
         requested();
     };
     auto request_y = [&](auto m_c, int group) {
@@ -195,42 +196,48 @@ __device__ inline void expand_rows(const AdapterArgs &p, const uint8_t *lds, int
     };
     auto step = [&](int group, auto more_c) {
         constexpr bool MORE = decltype(more_c)::value;
-        const int c = first + group * 64 + 4 * l;
-        operand_t column[NC][4];
+        const int c = first + (group * 16 + l) * CL;
+        operand_t column[NC][CL];
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
+        for (int n = 0; n < NC; ++n)
 #pragma unroll
-            for (int i = 0; i < JL; ++i) {
-                const bool in = KI * n + JL * g + i < rank;     // (past the rank coefficients are 0, and 0 times an infinity is none)
-                raw[n][i] = make_uint2(in ? raw[n][i].x : 0, in ? raw[n][i].y : 0);
+            for (int q = 0; q < CL / 4; ++q) {
+                uint2 four[JL];
+                operand_t out[4];
+#pragma unroll
+                for (int i = 0; i < JL; ++i) {
+                    const bool in = KI * n + JL * g + i < rank;                 // (past the rank coefficients are 0, and 0 times an infinity is none)
+                    four[i] = make_uint2(in ? raw[n][i].w[2 * q] : 0, in ? raw[n][i].w[2 * q + 1] : 0);
+                }
+                transpose_columns(four, out);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) column[n][4 * q + t] = out[t];
             }
-            transpose_columns(raw[n], column[n]);
-        }
         if constexpr (MORE) request_b(group + W);
         unrolled<MT>([&](auto m_c) {
             constexpr int M = decltype(m_c)::value;
-            float4_t sum[4] = {};                               // [t]: column c + t
+            float4_t sum[CL] = {};                              // [t]: column c + t
 #pragma unroll
             for (int n = 0; n < NC; ++n)
 #pragma unroll
                 for (int i = 0; i < S::TERMS; ++i) {
                     const operand_t coef = *reinterpret_cast<const operand_t *>(terms + (16 * M + l) * S::kTermRow + i * J + KI * n + JL * g);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) sum[t] = product16<WDT>(coef, column[n][t], sum[t]);
+                    for (int t = 0; t < CL; ++t) sum[t] = product16<WDT>(coef, column[n][t], sum[t]);
                 }
-            Raw<ODT, 4> out[4];
+            Raw<ODT, CL> out[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float v[4];
+                float v[CL];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
+                for (int t = 0; t < CL; ++t) {
                     v[t] = WDT == MOE_F16 ? sum[t][i] * unit[16 * M + 4 * g + i] : sum[t][i];
                     if constexpr (Y) v[t] += y[M][i].get(t);
                 }
                 out[i].set(v);
             }
             if constexpr (MORE) request_y(m_c, group + W);
-            if (16 * M + 16 <= rows && first + group * 64 + 64 <= end) {
+            if (16 * M + 16 <= rows && first + group * 16 * CL + 16 * CL <= end) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) out[i].store(p.out, place[2 * (16 * M + 4 * g + i) + 1] + c);
             } else {
