@@ -54,7 +54,9 @@ class _Adapt(torch.autograd.Function):
 
 def adapt(x, y, a, b, index, scale=None, by_assignment: bool = False, y_dtype=None):
     """moe_adapters as a function with gradients for x [T, K], y, a [E, rank, K] and b [E, rank, N]: y[r] + scale[e] * (A[e] x[t]) B[e], in a tensor of its own (y None: the second term).
-    The index may be written again before the backward pass; the others may not."""
+    The index may be written again before the backward pass; the others may not.  scale takes no gradient."""
+    if scale is not None and scale.requires_grad:
+        raise B.MoeError("an adapter's scale takes no gradient")
     return _Adapt.apply(x, y, a, b, scale, index, by_assignment, y_dtype)
 
 

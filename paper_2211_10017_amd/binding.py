@@ -7,7 +7,9 @@ raises: there is no fallback path.
 """
 from __future__ import annotations
 
+import array
 import ctypes
+import operator
 import os
 
 import torch
@@ -750,7 +752,7 @@ def moe_adapters(x, a, b, expert_offsets, perm_src=None, k: int = 1, scale=None,
     yp, ys = (None, N) if y is None else _rows(y, "y", N, (out.dtype,))
     if out.shape[0] != R or (y is not None and y.shape[0] != R) or (v is not None and v.shape != (R, rank)):
         raise MoeError("y and out must have %d rows, v [%d, %d]" % (R, R, rank))
-    if v is None and R > 512:                                           # (more rows than a call keeps on chip between its products)
+    if v is None and (R > 512 or rank > 32):                            # (more than a call keeps on chip between its products)
         v = torch.empty(R, rank, dtype=torch.float32, device=x.device)
     _check_device(x, a, b, expert_offsets, perm_src, scale, y, out, v)
     rc = load().moe_adapters(xp, _DT[x.dtype], xs, x.shape[0], _ptr(perm_src, torch.int32, "perm_src"), k, _ptr(expert_offsets, torch.int32, "expert_offsets"), R, E, K, N, rank,
@@ -803,6 +805,16 @@ def moe_adapters_backward(dy, x, a, b, v, expert_offsets, perm_src=None, k: int 
 
 # ---- AdamW -----------------------------------------------------------------------------------------------------------------------------
 
+_numel, _device, _contiguous, _address, _dtype = torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous, torch.Tensor.data_ptr, operator.attrgetter("dtype")
+
+
+def _pairs(states):
+    """Codes and scales of states in 8 bits."""
+    if any(len(s) != 2 for s in states):
+        raise MoeError("states in 8 bits are pairs of codes and scales")
+    return [s[0] for s in states], [s[1] for s in states]
+
+
 def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, copies=None):
     """An AdamW step over lists of tensors, in place (include/moe_wq.h).
 
@@ -815,50 +827,48 @@ def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=
         return
     bits = 8 if isinstance(exp_avg[0], (tuple, list)) else 32
     pd, gd, cd = params[0].dtype, grads[0].dtype, copies[0].dtype if copies is not None else None
+    if pd not in _DT or gd not in _DT or (cd is not None and cd not in (torch.float16, torch.bfloat16)):
+        raise MoeError("parameters and gradients must be fp16, bf16 or fp32, copies fp16 or bf16")
+    # All buffers in one list, kind by kind, and each check over all of it: with a hundred small tensors the checks are most of a step.
+    sizes = list(map(_numel, params))
+    names, buffers, want, types = ["parameter", "gradient"], [*params, *grads], sizes * 2, [pd] * count + [gd] * count
+    if bits == 8:
+        (m, ms), (v, vs) = _pairs(exp_avg), _pairs(exp_avg_sq)
+        names += ["codes", "codes", "scales", "scales"]
+        buffers += [*m, *v, *ms, *vs]
+        want += sizes * 2 + [(n + 31) // 32 for n in sizes] * 2
+        types += [torch.uint8] * (4 * count)
+    else:
+        names += ["moment", "moment"]
+        buffers += [*exp_avg, *exp_avg_sq]
+        want += sizes * 2
+        types += [torch.float32] * (2 * count)
+    if copies is not None:
+        names.append("copy")
+        buffers += copies
+        want += sizes
+        types += [cd] * count
     here = torch.cuda.current_device() if _raw_device is None else _raw_device()
-    flat, seen = [], set()
-    for i in range(count):
-        p, g = params[i], grads[i]
-        n = p.numel()
-        buffers = [p, g]
-        if bits == 8:
-            (mc, ms), (vc, vs) = exp_avg[i], exp_avg_sq[i]
-            blocks = (n + 31) // 32
-            if mc.numel() != n or vc.numel() != n or ms.numel() != blocks or vs.numel() != blocks:
-                raise MoeError("states of tensor %d must be %d codes and %d scales" % (i, n, blocks))
-            if not (mc.dtype is vc.dtype is ms.dtype is vs.dtype is torch.uint8):
-                raise MoeError("states of tensor %d must be uint8" % i)
-            buffers += (mc, vc, ms, vs)
-        else:
-            m, v = exp_avg[i], exp_avg_sq[i]
-            if m.numel() != n or v.numel() != n or m.dtype is not torch.float32 or v.dtype is not torch.float32:
-                raise MoeError("states of tensor %d must be fp32 and have its %d values" % (i, n))
-            buffers += (m, v)
-        if g.numel() != n or p.dtype is not pd or g.dtype is not gd:
-            raise MoeError("tensor %d: parameters must be of one type, and gradients, of the same sizes" % i)
-        if copies is not None:
-            if copies[i].numel() != n or copies[i].dtype is not cd:
-                raise MoeError("copy %d must have %d values, and the type of the others" % (i, n))
-            buffers.append(copies[i])
-        at = [t.data_ptr() for t in buffers]
-        for t in buffers:
-            if t.get_device() != here or not t.is_contiguous():
-                raise MoeError("tensor %d: buffers must be contiguous and on the current CUDA device" % i)
-        flat += at[:4]
-        flat += (at[4], at[5]) if bits == 8 else (0, 0)
-        flat += (at[-1] if copies is not None else 0, n)
-        if n and at[0] in seen:
-            raise MoeError("tensor %d is in the list twice" % i)
-        seen.add(at[0])
+    if list(map(_numel, buffers)) != want or list(map(_dtype, buffers)) != types or set(map(_device, buffers)) != {here} or not all(map(_contiguous, buffers)):
+        for i, t in enumerate(buffers):
+            if t.numel() != want[i] or t.dtype is not types[i] or t.get_device() != here or not t.is_contiguous():
+                raise MoeError("%s of tensor %d must be contiguous, on the current CUDA device, of %s with %d values, not %s with %d" % (names[i // count], i % count, types[i], want[i], t.dtype, t.numel()))
+    at = list(map(_address, buffers))
+    if len(set(at[:count])) < count and len({a for a, n in zip(at, sizes) if n}) < sum(n > 0 for n in sizes):
+        raise MoeError("a parameter is in the list twice")
+    # (the library's table has a tensor's fields side by side: p, g, m, v, scales of m and v, copy, n)
+    table = array.array("q", bytes(64 * count))
+    for k in range(6 if bits == 8 else 4):
+        table[k::8] = array.array("q", at[k * count:(k + 1) * count])
+    if copies is not None:
+        table[6::8] = array.array("q", at[-count:])
+    table[7::8] = array.array("q", sizes)
     on_device = isinstance(step, torch.Tensor)
     if on_device:
         if step.numel() != 1:
             raise MoeError("step must be one number")
         _check_device(step)
-    if pd not in _DT or gd not in _DT or (cd is not None and cd not in (torch.float16, torch.bfloat16)):
-        raise MoeError("parameters and gradients must be fp16, bf16 or fp32, copies fp16 or bf16")
-    table = (ctypes.c_int64 * len(flat))(*flat)
-    rc = load().moe_adamw(ctypes.addressof(table), count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits, lr, betas[0], betas[1], eps, weight_decay, grad_scale,
+    rc = load().moe_adamw(table.buffer_info()[0], count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits, lr, betas[0], betas[1], eps, weight_decay, grad_scale,
                           1 if on_device else step, _ptr(step, torch.int32, "step") if on_device else None, _stream())
     _check(rc, "moe_adamw")
 

@@ -7,10 +7,10 @@ namespace moe {
 
 // ---- phase one: rows times A ---------------------------------------------------------------------------------------------------------------------
 
-// acc[m][n] += rows 16 m.. of the item times the rows 16 n.. of A[e], over this wavefront's share of K: of every 4 W steps the four that are its own.  Operands come straight from memory
+// acc[m][n] += rows 16 m.. of the item times the rows first + 16 n.. of A[e], over this wavefront's share of K: of every 4 W steps the four that are its own.  Operands come straight from memory
 // in the matrix cores' order (both lie along K) and stay D steps ahead of their products: a step's registers are requested anew as soon as it has been multiplied.
 template <int XDT, int WDT, int D, int W, int MT, int NT>
-__device__ inline void multiply_rows(const AdapterArgs &p, int e, int row0, int rows, int wave, float4_t (&acc)[MT][NT])
+__device__ inline void multiply_rows(const AdapterArgs &p, int e, int first, int row0, int rows, int wave, float4_t (&acc)[MT][NT])
 {
     constexpr bool kNarrow = XDT == WDT;                        // products in 16 bits; otherwise fp32 ones, 16 channels a step instead of 32
     constexpr int KS = kNarrow ? 32 : 16, LV = KS / 4;          // channels of a step, and of a lane
@@ -24,7 +24,7 @@ __device__ inline void multiply_rows(const AdapterArgs &p, int e, int row0, int 
 #pragma unroll
     for (int m = 0; m < MT; ++m) x_at[m] = (size_t)x_row[m] * p.x_map.stride + g * LV;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) w_at[n] = min(16 * n + l, rank - 1) * K + g * LV;      // (past the rank: the last row again, left out by the caller)
+    for (int n = 0; n < NT; ++n) w_at[n] = min(first + 16 * n + l, rank - 1) * K + g * LV;      // (past the rank: the last row again, left out by the caller)
     Raw<XDT, LV> x[D][MT];
     Raw<WDT, LV> a[D][NT];
     const int steps = K / KS, own = steps / (4 * W) * 4 + min(max(steps % (4 * W) - 4 * wave, 0), 4);
@@ -91,14 +91,40 @@ struct AdapterShape {
     static constexpr int kTerms = kParts * BM * kRed * 4, kUnit = kTerms + BM * kTermRow * 2, kPlace = kUnit + BM * 4, kLds = kPlace + BM * 16;
 };
 
+// A row's coefficients, TPR lanes' worth of them, as 16-bit terms in LDS.
+template <class S, int WDT, int TPR, int Q>
+__device__ inline void store_terms(uint8_t *lds, const float (&c)[Q], float most, int row, int j0)
+{
+    float *unit = reinterpret_cast<float *>(lds + S::kUnit);
+    uint16_t *terms = reinterpret_cast<uint16_t *>(lds + S::kTerms);
+    constexpr int J = S::J;
+    float back = 1.0f;
+    if constexpr (WDT == MOE_F16) {                         // fp16: a power of two per row
+#pragma unroll
+        for (int m = TPR / 2; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+        const int ex = split_exponent(most);
+        back = exp2i(-ex);
+        if (j0 == 0) unit[row] = exp2i(ex);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int j = j0 + q * TPR;
+        if (j >= J) continue;
+        const Split<WDT> s(WDT == MOE_F16 ? c[q] * back : c[q]);
+        uint16_t *to = terms + row * S::kTermRow + j;
+        to[0] = s.hi, to[J] = s.lo;
+        if constexpr (S::TERMS == 3) to[2 * J] = s.rest;
+    }
+}
+
 // The wavefronts' sums become coefficients: added in a fixed order, written to memory if they are wanted there, and left in LDS as 16-bit terms.
+// `first`: of the rank, where coefficients alone are wanted, a part of it.
 template <class S, int WDT, int W, int MT, int NT>
-__device__ inline void make_terms(const AdapterArgs &p, uint8_t *lds, float4_t (&acc)[MT][NT], int e, int row0, int rows, int wave, bool keep)
+__device__ inline void make_terms(const AdapterArgs &p, uint8_t *lds, float4_t (&acc)[MT][NT], int e, int first, int row0, int rows, int wave, bool keep)
 {
     constexpr int BM = S::BM, J = S::J, P = S::kParts, TPR = 64 * W / BM >= 64 ? 64 : 64 * W / BM >= 32 ? 32 : 64 * W / BM >= 16 ? 16 : 8, Q = (J + TPR - 1) / TPR;
     static_assert(64 * W >= BM * TPR || TPR == 8, "a row's threads are lanes of one wavefront");
-    float *red = reinterpret_cast<float *>(lds), *unit = reinterpret_cast<float *>(lds + S::kUnit);
-    uint16_t *terms = reinterpret_cast<uint16_t *>(lds + S::kTerms);
+    float *red = reinterpret_cast<float *>(lds);
     const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, rank = p.rank;
     auto at = [&](int part, int m, int n, int i) -> float & { return red[(part * BM + 16 * m + 4 * g + i) * S::kRed + 16 * n + l]; };
     auto put = [&](int part) {
@@ -136,28 +162,32 @@ __device__ inline void make_terms(const AdapterArgs &p, uint8_t *lds, float4_t (
 #pragma unroll
                 for (int w = 0; w < P; ++w) sum += red[(w * BM + row) * S::kRed + j];
             }
-            const bool in = j < rank && row < rows;
+            const bool in = j < J && first + j < rank && row < rows;
             c[q] = in ? scale * sum : 0.0f;
-            if (in && keep) p.coef[(size_t)(row0 + row) * rank + j] = p.coef_scaled ? c[q] : sum;
+            if (in && keep) p.coef[(size_t)(row0 + row) * rank + first + j] = p.coef_scaled ? c[q] : sum;
             most = fmaxf(most, fabsf(c[q]));
         }
-        float back = 1.0f;
-        if constexpr (WDT == MOE_F16) {                         // fp16: a power of two per row
-#pragma unroll
-            for (int m = TPR / 2; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
-            const int ex = split_exponent(most);
-            back = exp2i(-ex);
-            if (j0 == 0) unit[row] = exp2i(ex);
-        }
+        if (!p.out) continue;                                   // (coefficients alone)
+        store_terms<S, WDT, TPR, Q>(lds, c, most, row, j0);
+    }
+}
+
+// Coefficients that are in memory, as terms in LDS.
+template <class S, int WDT, int W>
+__device__ inline void load_terms(const AdapterArgs &p, uint8_t *lds, int e, int row0, int rows)
+{
+    constexpr int TPR = 64, Q = (S::J + TPR - 1) / TPR;
+    const float scale = p.scale && !p.coef_scaled ? p.scale[e] : 1.0f;
+    const int j0 = threadIdx.x % TPR;
+    for (int row = threadIdx.x / TPR; row < S::BM; row += 64 * W / TPR) {
+        float c[Q], most = 0.0f;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int j = j0 + q * TPR;
-            if (j >= J) continue;
-            const Split<WDT> s(WDT == MOE_F16 ? c[q] * back : c[q]);
-            uint16_t *to = terms + row * S::kTermRow + j;
-            to[0] = s.hi, to[J] = s.lo;
-            if constexpr (S::TERMS == 3) to[2 * J] = s.rest;
+            c[q] = j < p.rank && row < rows ? scale * p.coef[(size_t)(row0 + row) * p.rank + j] : 0.0f;
+            most = fmaxf(most, fabsf(c[q]));
         }
+        store_terms<S, WDT, TPR, Q>(lds, c, most, row, j0);
     }
 }
 
@@ -339,32 +369,68 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void adapter_kernel(Adapte
     if (!find_share(p, S::BM, &e, &col, &row0, &rows)) return;
     find_places<S>(p, lds, row0, rows);
     float4_t acc[MT][NT] = {};
-    multiply_rows<XDT, WDT, S::D, W, MT, NT>(p, e, row0, rows, wave, acc);
-    make_terms<S, WDT, W, MT, NT>(p, lds, acc, e, row0, rows, wave, p.coef && col == 0);
-    if (!p.out) return;                                         // (coefficients alone)
+    const int part = p.out ? 0 : col * S::J;                    // (coefficients alone: of a part of the rank, if there is a block for each)
+    multiply_rows<XDT, WDT, S::D, W, MT, NT>(p, e, part, row0, rows, wave, acc);
+    make_terms<S, WDT, W, MT, NT>(p, lds, acc, e, part, row0, rows, wave, p.coef && (!p.out || col == 0));
+    if (!p.out) return;
     __syncthreads();
     expand_rows<S, WDT, ODT, Y, W, MT>(p, lds, e, rows, wave, col * p.width, min(p.N, (col + 1) * p.width));
 }
 
+// Phase two alone, of coefficients that are in memory.
+template <int WDT, int ODT, bool Y, int NT>
+__global__ __launch_bounds__(512, 2) void adapter_expand_kernel(AdapterArgs p)
+{
+    constexpr int W = 8;
+    using S = AdapterShape<WDT, ODT, W, 1, NT>;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x >= p.items) return copy_rows<ODT, Y>(p, blockIdx.x - p.items, W);
+    int e, col, row0, rows;
+    if (!find_share(p, S::BM, &e, &col, &row0, &rows)) return;
+    find_places<S>(p, lds, row0, rows);
+    load_terms<S, WDT, W>(p, lds, e, row0, rows);
+    __syncthreads();
+    expand_rows<S, WDT, ODT, Y, W, 1>(p, lds, e, rows, wave, col * p.width, min(p.N, (col + 1) * p.width));
+}
+
 // ---- launches --------------------------------------------------------------------------------------------------------------------------------------
 
-template <int XDT, int WDT, int ODT, bool Y, int W, int MT, int NT>
-static int launch_shape(AdapterArgs p, int share, int slices, hipStream_t s, const char *what)
+template <class Kernel>
+static int launch_items(Kernel kernel, std::atomic<uint64_t> &raised, AdapterArgs p, int share, int W, int lds, hipStream_t s, const char *what)
 {
-    constexpr int kLds = AdapterShape<WDT, ODT, W, MT, NT>::kLds;
     p.share = share;
-    p.width = p.out ? (int)round_up(((size_t)p.N + slices - 1) / slices, 64) : p.N;
-    p.ncol = (p.N + p.width - 1) / p.width;
     const long parts = (long)p.R / share + (p.E < p.R ? p.E : p.R);             // an upper bound: of n rows at most n / share + 1
     const long items = (parts * p.ncol + kXcds - 1) / kXcds * kXcds;
     const int need = p.y == p.out || !p.out ? 0 : (p.R + W - 1) / W, copies = need < 256 ? need : 256;          // blocks for rows of no adapter
     if ((items + copies) * W > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %ld workgroups exceed one launch", what, items);
     p.items = (int)items;
-    static std::atomic<uint64_t> raised;
-    const auto kernel = &adapter_kernel<XDT, WDT, ODT, Y, W, MT, NT>;
-    if (kLds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(kernel), kLds, raised);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(items + copies)), dim3(64 * W), kLds, s, p);
+    if (lds > 64 * 1024) raise_lds_limit(reinterpret_cast<const void *>(kernel), lds, raised);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(items + copies)), dim3(64 * W), lds, s, p);
     return check_launch(what);
+}
+
+static void cut_channels(AdapterArgs &p, int slices)
+{
+    p.width = (int)round_up(((size_t)p.N + slices - 1) / slices, 64);
+    p.ncol = (p.N + p.width - 1) / p.width;
+}
+
+template <int XDT, int WDT, int ODT, bool Y, int W, int MT, int NT>
+static int launch_shape(AdapterArgs p, int share, int slices, hipStream_t s, const char *what)
+{
+    static std::atomic<uint64_t> raised;
+    if (p.out) cut_channels(p, slices);
+    else p.ncol = (p.rank + 16 * NT - 1) / (16 * NT);
+    return launch_items(&adapter_kernel<XDT, WDT, ODT, Y, W, MT, NT>, raised, p, share, W, AdapterShape<WDT, ODT, W, MT, NT>::kLds, s, what);
+}
+
+template <int WDT, int ODT, bool Y, int NT>
+static int launch_expand(AdapterArgs p, int share, int slices, hipStream_t s, const char *what)
+{
+    static std::atomic<uint64_t> raised;
+    cut_channels(p, slices);
+    return launch_items(&adapter_expand_kernel<WDT, ODT, Y, NT>, raised, p, share, 8, AdapterShape<WDT, ODT, 8, 1, NT>::kLds, s, what);
 }
 
 template <int XDT, int WDT, int ODT, bool Y, int NT>
@@ -388,6 +454,17 @@ static int launch_rank(const AdapterArgs &p, hipStream_t s, const char *what)
                 const int rounds = (parts * n + kUnits - 1) / kUnits;
                 const float cost = rounds * (96e3f + held * per_row + a_bytes + (held * per_slice + b_bytes) / n);
                 if (least == 0 || cost < least) least = cost, slices = n, share = rows;
+            }
+        }
+        if constexpr (NT >= 4) {
+            // Long matrices of a high rank, which one block after the other would read whole before it begins with its slice: two launches, each cut into many blocks, the first along
+            // the rank.  (One row, 4096 x 4096, rank 64 / 128: a call of 14.4 / 15.1 us, which is the host's, as one launch 19.9 / 35.4.)
+            if (p.coef && (!p.out || (long)p.rank * p.K >= 1 << 17)) {
+                AdapterArgs q = p;
+                q.out = nullptr, q.y = nullptr;
+                const int parts = p.R / 16 + used;
+                if (const int rc = launch_shape<XDT, WDT, WDT, false, 16, 1, 1>(q, 16, 1, s, what)) return rc;
+                return p.out ? launch_expand<WDT, ODT, Y, NT>(p, 16, kUnits / parts < 1 ? 1 : kUnits / parts > 32 ? 32 : kUnits / parts, s, what) : (int)MOE_OK;
             }
         }
         return launch_shape<XDT, WDT, ODT, Y, W, 1, NT>(p, share, slices, s, what);

@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 CASES = [(1, 1, 1, 8, 8, 1, "even"), (1, 1, 8, 1024, 1024, 16, "even"), (1, 2, 8, 64, 72, 3, "even"), (3, 1, 5, 16, 264, 8, "ends"), (17, 1, 3, 72, 8, 17, "even"),
          (64, 1, 32, 256, 512, 16, "pruned"), (65, 2, 130, 264, 136, 33, "even"), (128, 1, 1, 520, 64, 64, "even"), (200, 2, 16, 704, 1032, 12, "pruned"), (257, 1, 4, 128, 384, 128, "one"),
          (513, 2, 33, 136, 72, 5, "ends"), (96, 3, 7, 64, 64, 31, "pruned"), (40, 1, 6, 64, 64, 4, "none"), (1000, 1, 2, 1032, 200, 15, "one"), (700, 2, 600, 64, 128, 8, "even"),
-         (2100, 1, 3, 512, 576, 32, "even"), (4100, 2, 64, 72, 64, 16, "even"), (31, 1, 4, 4104, 24, 9, "even"), (30, 1, 3, 24, 4104, 9, "even")]
+         (2100, 1, 3, 512, 576, 32, "even"), (4100, 2, 64, 72, 64, 16, "even"), (31, 1, 4, 4104, 24, 9, "even"), (30, 1, 3, 24, 4104, 9, "even"),
+         (1, 1, 3, 4096, 136, 128, "even"), (45, 2, 5, 2056, 200, 65, "pruned"), (300, 1, 7, 1032, 4104, 127, "ends")]
 TYPES = [(F16, F16), (BF16, BF16), (BF16, F32), (F16, F32), (F16, BF16), (BF16, F16)]
 
 

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from launches import P as PTR, record
+from paper_2211_10017_amd import AdamW, LowRankAdapters, adapt
 from paper_2211_10017_amd import binding as B
 
 P, ODD = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1008)          # never dereferenced: validation fails first
@@ -195,3 +196,52 @@ def test_the_largest_batches_take_a_launch():
         for call in (("moe_combine_backward", [PTR, F32, PTR, F16, PTR, PTR, None, T, 1, d, T, PTR, PTR, None]), ("moe_permute_backward", [PTR, F16, PTR, None, T, 1, d, T, PTR, F16, None])):
             got = record([call])[0]
             assert got.rc == OK and len(got.launches) == 1 and 0 < got.launches[0].grid[0] * got.launches[0].block < 2 ** 32
+
+
+def _calls(T, k, E, K, N, rank, dt=F16, ydt=F16, v=PTR, y=PTR, out=PTR):
+    R = T * k
+    forward = ("moe_adapters", [PTR, dt, [K], T, PTR, k, PTR, R, E, K, N, rank, PTR, PTR, None, 0, y, [N], out, [N], ydt, v, None])
+    backward = ("moe_adapters_backward", [PTR, ydt, [N], PTR, dt, [K], T, PTR, k, PTR, R, E, K, N, rank, PTR, PTR, None, 0, PTR, PTR, [K], PTR, PTR, F32, PTR, [1 << 40], None])
+    return forward, backward
+
+
+def test_what_adapters_launch():
+    """One launch from rows to rows but for long matrices of a high rank; gradients of the matrices another, and a third where an adapter may have more than one part."""
+    sizes = {(1, 1, 8, 1024, 1024, 16): (1, 2), (64, 1, 32, 1024, 4096, 16): (1, 2), (512, 2, 16, 256, 256, 8): (1, 2), (513, 2, 16, 256, 256, 8): (1, 3), (1, 1, 8, 4096, 4096, 64): (2, 3),
+             (1, 1, 8, 1024, 1024, 128): (2, 3), (1, 1, 8, 1016, 1016, 128): (1, 2), (16384, 1, 32, 4096, 4096, 32): (1, 3), (8192, 2, 64, 4096, 4096, 16): (1, 3), (16384, 1, 32, 4096, 4096, 128): (1, 3)}
+    calls = [c for s in sizes for c in _calls(*s)]
+    got = record(calls)
+    for i, (size, (one, two)) in enumerate(sizes.items()):
+        for call, want in zip(got[2 * i:2 * i + 2], (one, two)):
+            assert call.rc == OK and len(call.launches) == want, (size, call)
+            assert all(0 < l.grid[0] * l.block < 2 ** 32 and l.shared <= 160 * 1024 for l in call.launches)
+    # without a place for the coefficients one launch keeps them on chip
+    assert len(record([_calls(1, 1, 8, 4096, 4096, 128, v=None)[0]])[0].launches) == 1
+    # rows of no adapter: blocks of their own, not in place (there y and out are one pointer)
+    in_place, apart = record([_calls(64, 1, 32, 1024, 1024, 16)[0], _calls(64, 1, 32, 1024, 1024, 16, y=None)[0]])
+    assert apart.launches[0].grid[0] == in_place.launches[0].grid[0] + 4
+
+
+def test_the_most_rows_and_adapters():
+    big = record([_calls(2 ** 24, 1, 4096, 64, 64, 16)[0], _calls(2 ** 24, 1, 4096, 64, 64, 16)[1], _calls(1, 1, 4096, 2 ** 20, 2 ** 20, 128)[0]])
+    assert all(c.rc == OK for c in big)
+    assert record([_calls(2 ** 31 - 1, 1, 1, 64, 64, 16)[0]])[0].rc in (OK, UNSUPPORTED)
+
+
+def test_objects_refuse_what_calls_would():
+    for bad in (dict(E=0), dict(rank=129), dict(K=60), dict(N=0), dict(dtype=torch.float32), dict(E=5000)):
+        with pytest.raises(B.MoeError):
+            LowRankAdapters(**dict(dict(E=2, rank=4, K=64, N=64, device="cpu"), **bad))
+    a = LowRankAdapters(2, 4, 64, 72, alpha=8, device="cpu")
+    assert a.a.shape == (2, 4, 64) and a.b.shape == (2, 4, 72) and bool((a.b == 0).all()) and a.scale.tolist() == [2.0, 2.0]
+    p = torch.zeros(4, requires_grad=True)
+    for bad in (dict(params=[]), dict(params=[p, p]), dict(params=[p], bits=16), dict(params=[torch.zeros(4, dtype=torch.float64)]), dict(params=[torch.zeros(4, 4)[:, 0]])):
+        with pytest.raises(B.MoeError):
+            AdamW(**bad)
+    one = AdamW([p])
+    with pytest.raises(B.MoeError):
+        one.load_state_dict(AdamW([torch.zeros(5)]).state_dict())
+    with pytest.raises(B.MoeError):
+        one.load_state_dict(AdamW([p], bits=8).state_dict())
+    with pytest.raises(B.MoeError, match="scale"):
+        adapt(None, None, a.a, a.b, None, a.scale.requires_grad_())
