@@ -86,6 +86,7 @@ struct OuterArgs {
     int R, E, rank, out_dtype;
     OuterJob job[2];
     int first;                  // blocks of job 0
+    int turns;                  // parts of the rank
     int join;                   // adapters that can have more than one chunk
 };
 

@@ -459,10 +459,10 @@ static int launch_rank(const AdapterArgs &p, hipStream_t s, const char *what)
         if constexpr (NT >= 4) {
             // Long matrices of a high rank, which one block after the other would read whole before it begins with its slice: two launches, each cut into many blocks, the first along
             // the rank.  (One row, 4096 x 4096, rank 64 / 128: a call of 14.4 / 15.1 us, which is the host's, as one launch 19.9 / 35.4.)
-            if (p.coef && (!p.out || (long)p.rank * p.K >= 1 << 17)) {
+            const int parts = p.R / 16 + used;
+            if (p.coef && (!p.out || ((long)p.rank * p.K >= 1 << 17 && parts * (p.rank + 15) / 16 <= 2 * kUnits))) {
                 AdapterArgs q = p;
                 q.out = nullptr, q.y = nullptr;
-                const int parts = p.R / 16 + used;
                 if (const int rc = launch_shape<XDT, WDT, WDT, false, 16, 1, 1>(q, 16, 1, s, what)) return rc;
                 return p.out ? launch_expand<WDT, ODT, Y, NT>(p, 16, kUnits / parts < 1 ? 1 : kUnits / parts > 32 ? 32 : kUnits / parts, s, what) : (int)MOE_OK;
             }

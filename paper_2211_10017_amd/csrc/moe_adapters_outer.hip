@@ -43,9 +43,9 @@ __device__ inline void store_gradient(void *out, int dtype, size_t at, const flo
 
 // A wavefront: 64 channels, four neighbouring ones per lane, of up to `chunk` rows of an adapter, 32 rows a step (the products' inner axis).  16-bit rows meet the coefficients as two
 // 16-bit terms, three of bf16 where the gradient is fp32 (TERMS); fp16 ones in units of a power of two that grows with them.  fp32 rows and coefficients are multiplied in fp32.
-// Two steps' rows are under way at a time, and the places of the next two.
+// Two steps' rows are under way at a time, and the places of the next two.  `first`: of the rank, of which a wavefront takes 16 NT at most.
 template <int DT, int NT, int TERMS>
-__device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int item)
+__device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int item, int first)
 {
     const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, rank = p.rank, C = job.C;
     int e, lo, hi, slot;
@@ -74,7 +74,7 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
         for (int i = 0; i < 8; ++i) {
             const float *at = job.coef + (size_t)min(row_of(step, i), hi - 1) * rank;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) f[B][n][i] = at[min(16 * n + l, rank - 1)];        // (past the rank: rows of the result that are not stored)
+            for (int n = 0; n < NT; ++n) f[B][n][i] = at[min(first + 16 * n + l, rank - 1)];        // (past the rank: rows of the result that are not stored)
         }
         find(s_c, step + 2);
         requested();
@@ -157,7 +157,7 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int j = 16 * n + 4 * g + i;
+            const int j = first + 16 * n + 4 * g + i;
             if (j >= rank) continue;
             float v[4];
 #pragma unroll
@@ -172,11 +172,13 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
         }
 }
 
+// Up to 32 of the rank are a wavefront's; those that take the same rows for more of it run on the same XCD, one after the other.
 template <int DT0, int DT1, int NT, int TERMS>
-__global__ __launch_bounds__(64, NT <= 2 ? 3 : 1) void adapter_outer_kernel(OuterArgs p)
+__global__ __launch_bounds__(64, 3) void adapter_outer_kernel(OuterArgs p)
 {
-    if ((int)blockIdx.x < p.first) outer_item<DT0, NT, DT0 == MOE_BF16 ? TERMS : 2>(p, p.job[0], blockIdx.x);
-    else outer_item<DT1, NT, DT1 == MOE_BF16 ? TERMS : 2>(p, p.job[1], blockIdx.x - p.first);
+    const int turn = blockIdx.x / kXcds, item = turn / p.turns * kXcds + blockIdx.x % kXcds, first = turn % p.turns * 16 * NT;
+    if (item < p.first) outer_item<DT0, NT, DT0 == MOE_BF16 ? TERMS : 2>(p, p.job[0], item, first);
+    else outer_item<DT1, NT, DT1 == MOE_BF16 ? TERMS : 2>(p, p.job[1], item - p.first, first);
 }
 
 // Sums of the chunks of adapters that have more than one, in their order.  blockIdx.y: the how manieth such adapter, blockIdx.z: the job.
@@ -199,7 +201,16 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(OuterArgs p)
             if (at >= size || first + chunks > job.slots) return;
             const float s = job.scale ? job.scale[e] : 1.0f;
             float4_t sum = {};
-            for (int i = 0; i < chunks; ++i) sum += *reinterpret_cast<const float4_t *>(job.part + (size_t)(first + i) * size + at);
+            const float *from = job.part + (size_t)first * size + at;
+            int i = 0;
+            for (; i + 8 <= chunks; i += 8) {                   // (eight requested together; added in their order)
+                float4_t v[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = *reinterpret_cast<const float4_t *>(from + (size_t)(i + q) * size);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) sum += v[q];
+            }
+            for (; i < chunks; ++i) sum += *reinterpret_cast<const float4_t *>(from + (size_t)i * size);
             const float v[4] = {sum[0] * s, sum[1] * s, sum[2] * s, sum[3] * s};
             store_gradient(job.out, p.out_dtype, (size_t)e * size + at, v);
             return;
@@ -226,19 +237,18 @@ int launch_adapter_outer(const OuterArgs &args, int dtype0, int dtype1, hipStrea
         }
     }
     if (blocks[0] + blocks[1] == 0) return MOE_OK;
-    if (blocks[0] + blocks[1] > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %ld workgroups exceed one launch", what, blocks[0] + blocks[1]);
-    p.first = (int)blocks[0];
+    p.first = (int)blocks[0], p.turns = p.rank <= 16 ? 1 : (p.rank + 31) / 32;
+    const long grid = (blocks[0] + blocks[1] + kXcds - 1) / kXcds * kXcds * p.turns;
+    if (grid > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %ld workgroups exceed one launch", what, grid);
     auto run = [&](auto d0, auto d1) {
         constexpr int D0 = decltype(d0)::value, D1 = decltype(d1)::value;
         auto start = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             const auto kernel = p.out_dtype == MOE_F32 ? &adapter_outer_kernel<D0, D1, NT, 3> : &adapter_outer_kernel<D0, D1, NT, 2>;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks[0] + blocks[1])), dim3(64), 0, s, p);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64), 0, s, p);
             return check_launch(what);
         };
-        using std::integral_constant;
-        return p.rank <= 16 ? start(integral_constant<int, 1>{}) : p.rank <= 32 ? start(integral_constant<int, 2>{}) : p.rank <= 64 ? start(integral_constant<int, 4>{})
-             : start(integral_constant<int, 8>{});
+        return p.rank <= 16 ? start(std::integral_constant<int, 1>{}) : start(std::integral_constant<int, 2>{});
     };
     const int rc = with_dtype(dtype1, [&](auto d1) {
         return dtype0 == MOE_F16 ? run(std::integral_constant<int, MOE_F16>{}, d1) : run(std::integral_constant<int, MOE_BF16>{}, d1);
