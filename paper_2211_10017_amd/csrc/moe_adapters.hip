@@ -44,7 +44,7 @@ static int check_rows(const char *what, const char *name, const void *p, int64_t
 
 // Rows of a wavefront's part of a matrix's gradient.  Enough parts to fill the chip (a part is 64 channels of `chunk` rows; two thousand wavefronts), as the sums of parts have to be
 // written and added up by a launch of their own; at most 1024 rows, or an adapter that has much of the batch is one long chain, unless that would make more than 256 parts of it.  Up to
-// 1024 rows are one part, without that launch.
+// 1024 rows are one part, without that launch (1024 rows of 256 by 16 adapters: a call of 21.7 us, 24.6 with it; all 1024 of 1024 x 1024 in one adapter 32).
 static int outer_chunk(int R, int C)
 {
     if (R <= 1024) return 1024;

@@ -319,6 +319,8 @@ __device__ inline void copy_rows(const AdapterArgs &p, int block, int waves)
 //
 // All blocks run at once, one per compute unit where there are as many, and share the memory's rate, so the one with the most to read is waited for: an adapter's rows are cut into as many
 // parts of `share` rows as come nearest, evenly, rather than into full tiles and a rest.  Neighbouring parts lie on one XCD (as find_item deals them), whose cache then holds their adapter.
+// (16384 rows of 4096 x 4096, 32 adapters of rank 32, bf16 in place: 108 us = 3.7 TB/s of x and y; tiles of 16 rows of one adapter each 141, as a third of what is read is then A and B.
+// Wavefronts spend 55 % of their time waiting to issue loads and stores and 23 % waiting for them: the blocks' phases, all reading and then all writing, are what is left.)
 
 // The block's adapter, slice and rows.  Every wavefront computes the same.
 __device__ inline bool find_share(const AdapterArgs &p, int most, int *e, int *col, int *row0, int *rows)
@@ -433,12 +435,14 @@ static int launch_expand(AdapterArgs p, int share, int slices, hipStream_t s, co
     return launch_items(&adapter_expand_kernel<WDT, ODT, Y, NT>, raised, p, share, 8, AdapterShape<WDT, ODT, 8, 1, NT>::kLds, s, what);
 }
 
+// One block per compute unit, of the fewest rows' registers that hold its share (32 adapters of 4096 x 4096, rank 16 / 32, bf16, in blocks of up to 16, 32, 48 and 80 rows: 3000 rows, shares of 12,
+// 22 / 27, 27 / 33, 34 / 38, 47 / 54 us; 3968, 16, 34 / 46, 28 / 34, 35 / 39, 48 / 55; 7000, 28, 54, 44, 47, 58; 8192, 33, 69, 60, 54, 62; 11000, 44, 81 / 103, 72 / 87, 66 / 71, 72 / 80).
 template <int XDT, int WDT, int ODT, bool Y, int NT>
 static int launch_rank(const AdapterArgs &p, hipStream_t s, const char *what)
 {
     constexpr int kUnits = 248, kMost = NT <= 2 ? 80 : NT == 4 ? 64 : 48;       // a few fewer than compute units, as parts are rounded one way or the other; rows that a block can hold
     const long even = ((long)p.R + kUnits - 1) / kUnits;
-    if (!p.coef || even <= 16) {
+    if (!p.coef || even <= 13) {
         // Few rows: parts of an adapter's rows and slices of N such that what a block moves (its rows of x, A, and its slice of y, out and B), times the rounds of blocks, is least.  What a
         // block takes to begin and to join its sums is as long as 96 KB.
         constexpr int W = NT <= 2 ? 16 : 8;
@@ -472,8 +476,8 @@ static int launch_rank(const AdapterArgs &p, hipStream_t s, const char *what)
     const long rounds = ((long)p.R + kUnits * (kMost - 8) - 1) / (kUnits * (kMost - 8));
     const int share = (int)((p.R + kUnits * rounds - 1) / (kUnits * rounds));
     if constexpr (NT <= 2) {
-        if (share <= 26) return launch_shape<XDT, WDT, ODT, Y, 8, 2, NT>(p, share, 1, s, what);
-        if (share <= 42) return launch_shape<XDT, WDT, ODT, Y, 8, 3, NT>(p, share, 1, s, what);
+        if (share <= 29) return launch_shape<XDT, WDT, ODT, Y, 8, 2, NT>(p, share, 1, s, what);
+        if (share <= 45) return launch_shape<XDT, WDT, ODT, Y, 8, 3, NT>(p, share, 1, s, what);
     }
     return launch_shape<XDT, WDT, ODT, Y, 8, kMost / 16, NT>(p, share, 1, s, what);
 }

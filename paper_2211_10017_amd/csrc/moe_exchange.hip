@@ -3,7 +3,8 @@
 //   out[t] = sum_j s[t,j] y[inv[t k + j]]:  dy[inv[a]] = s[a] dout[a / k],  ds[a] = <dout[a / k], y[inv[a]]>
 //   x_perm[r] = x[perm_src[r] / k]:         dx[t] = sum_j dx_perm[inv[t k + j]]
 //
-// Both go by token: a token's k rows are written by nobody else, so nothing is added into memory and the sums have one order.  One pass over the data each.
+// Both go by token: a token's k rows are written by nobody else, so nothing is added into memory and the sums have one order.  One pass over the data each, bound by memory (16384 tokens of
+// 4096, two rows each, fp16: 671 MB in 144 us = 4.7 TB/s, 403 MB in 88 us = 4.6 TB/s) or, for small batches, by a launch (512 tokens of 256: 3.6 and 3.1 us).
 #include "moe_rows.h"
 
 namespace moe {
