@@ -44,17 +44,19 @@ static int check_rows(const char *what, const char *name, const void *p, int64_t
 
 // Rows of a wavefront's part of a matrix's gradient.  Enough parts to fill the chip (a part is 64 channels of `chunk` rows; two thousand wavefronts), as the sums of parts have to be
 // written and added up by a launch of their own; at most 1024 rows, or an adapter that has much of the batch is one long chain, unless that would make more than 256 parts of it.  Up to
-// 1024 rows are one part, without that launch (1024 rows of 256 by 16 adapters: a call of 21.7 us, 24.6 with it; all 1024 of 1024 x 1024 in one adapter 32).
-static int outer_chunk(int R, int C)
+// 1024 rows, 256 for an adapter on average, are one part, without that launch: 1024 rows of 256 x 256 by 16 adapters take a call of 22.0 us, 24.5 with it.  Of a batch in which one adapter has all the
+// rows that is the slower one, which the host cannot see but where there are few adapters (1024 of 1024 x 1024 in one adapter: 31.9 us as one part, 24.5 in parts of 256).
+// More rows (a call in parts of 256, 512, 1024, 2048): 16384 by 64 adapters of 4096 x 4096 167, 156, 155, 154 us, 16384 by two 150, 146, 142, 158; 4096 by eight of 1024 x 1024 24.9, 31.2, 31.2.
+static int outer_chunk(int R, int C, int E)
 {
-    if (R <= 1024) return 1024;
+    if (R <= 1024 && R / 256 <= E) return 1024;
     const long even = (long)R * ((C + 63) / 64) / 2048, most = R / 256 > 1024 ? R / 256 : 1024;
     const long rows = even < 256 ? 256 : even > most ? most : even;
     return (int)((rows + 31) / 32 * 32);
 }
 
-static int part_slots(int R, int C) { return 2 * (R / outer_chunk(R, C)); }        // n rows in more than one chunk are at most 2 (n / chunk) of them
-static size_t part_bytes(int R, int C, int rank) { return (size_t)part_slots(R, C) * rank * C * sizeof(float); }
+static int part_slots(int R, int C, int E) { return 2 * (R / outer_chunk(R, C, E)); }        // n rows in more than one chunk are at most 2 (n / chunk) of them
+static size_t part_bytes(int R, int C, int E, int rank) { return (size_t)part_slots(R, C, E) * rank * C * sizeof(float); }
 
 }  // namespace moe
 
@@ -86,7 +88,7 @@ extern "C" size_t moe_adapters_backward_workspace_bytes(int R, int E, int K, int
 {
     using namespace moe;
     if (R <= 0 || E <= 0 || K <= 0 || N <= 0 || rank <= 0) return 0;
-    return round_up((size_t)R * rank * sizeof(float), 256) + round_up(part_bytes(R, K, rank), 256) + part_bytes(R, N, rank);
+    return round_up((size_t)R * rank * sizeof(float), 256) + round_up(part_bytes(R, K, E, rank), 256) + part_bytes(R, N, E, rank);
 }
 
 extern "C" int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_stride, const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k,
@@ -113,7 +115,7 @@ extern "C" int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_st
     const hipStream_t s = as_stream(stream);
     const RowMap tokens{perm_src, k, T, x_stride}, rows{by_assignment ? perm_src : nullptr, 1, R, dy_stride};
     float *u = (float *)workspace, *part0 = R > 0 ? (float *)((char *)workspace + round_up((size_t)R * rank * sizeof(float), 256)) : nullptr;
-    float *part1 = R > 0 ? (float *)((char *)part0 + round_up(part_bytes(R, K, rank), 256)) : nullptr;
+    float *part1 = R > 0 ? (float *)((char *)part0 + round_up(part_bytes(R, K, E, rank), 256)) : nullptr;
     if (R > 0 && (dx || da)) {
         AdapterArgs p{};
         p.offsets = expert_offsets, p.scale = scale, p.R = R, p.E = E, p.K = N, p.N = K, p.rank = rank;
@@ -125,7 +127,7 @@ extern "C" int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_st
     }
     OuterArgs p{};
     p.offsets = expert_offsets, p.R = R, p.E = E, p.rank = rank, p.out_dtype = grad_dtype;
-    p.job[0] = OuterJob{x, tokens, u, nullptr, da, K, 0, outer_chunk(R, K), part0, part_slots(R, K)};
-    p.job[1] = OuterJob{dy, rows, v, scale, db, N, 0, outer_chunk(R, N), part1, part_slots(R, N)};
+    p.job[0] = OuterJob{x, tokens, u, nullptr, da, K, 0, outer_chunk(R, K, E), part0, part_slots(R, K, E)};
+    p.job[1] = OuterJob{dy, rows, v, scale, db, N, 0, outer_chunk(R, N, E), part1, part_slots(R, N, E)};
     return launch_adapter_outer(p, dtype, dy_dtype, s, what);
 }

@@ -319,7 +319,7 @@ __device__ inline void copy_rows(const AdapterArgs &p, int block, int waves)
 //
 // All blocks run at once, one per compute unit where there are as many, and share the memory's rate, so the one with the most to read is waited for: an adapter's rows are cut into as many
 // parts of `share` rows as come nearest, evenly, rather than into full tiles and a rest.  Neighbouring parts lie on one XCD (as find_item deals them), whose cache then holds their adapter.
-// (16384 rows of 4096 x 4096, 32 adapters of rank 32, bf16 in place: 108 us = 3.7 TB/s of x and y; tiles of 16 rows of one adapter each 141, as a third of what is read is then A and B.
+// (16384 rows of 4096 x 4096, 32 adapters of rank 32, bf16 in place: 108 us = 3.7 TB/s of x and y; tiles of 16 rows of one adapter each 141: they read A and B, through the caches, twice as often as x and y.
 // Wavefronts spend 55 % of their time waiting to issue loads and stores and 23 % waiting for them: the blocks' phases, all reading and then all writing, are what is left.)
 
 // The block's adapter, slice and rows.  Every wavefront computes the same.

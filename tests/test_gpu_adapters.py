@@ -243,3 +243,20 @@ def test_replays_from_a_graph_and_on_a_side_stream():
             graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(g, w) for g, w in zip(results, want)), rep
+
+
+@pytest.mark.parametrize("R,E", [(256, 1), (511, 1), (512, 1), (700, 2), (768, 2), (1024, 3), (1024, 4), (1025, 4)])
+def test_gradients_of_few_adapters_with_all_the_rows(R, E):
+    """One part of an adapter's rows or several, around where that changes; the last adapter has every row, the others' gradients are 0."""
+    K, N, rank = 72, 136, 8
+    d = inputs(R, 1, E, K, N, rank, "even", BF16, BF16)
+    off = torch.tensor([0] * E + [R], dtype=torch.int32, device="cuda")
+    index = dict(perm_src=d["perm"], scale=d["scale"], by_assignment=True)
+    v = torch.empty((R, rank), device="cuda")
+    B.moe_adapters(d["x"], d["a"], d["b"], off, y=d["y"], v=v, **index)
+    want = adapters_ref(d["x"], d["a"], d["b"], off, d["perm"], 1, d["scale"], True, d["y"], d["dy"])
+    _, da, db = B.moe_adapters_backward(d["dy"], d["x"], d["a"], d["b"], v, off, **index)
+    torch.cuda.synchronize()
+    within(da, want["da"], want["da_mag"] + 2.0 ** -23 * want["da"].abs())
+    within(db, want["db"], want["db_mag"] + 2.0 ** -23 * want["db"].abs())
+    assert bool((da[:-1] == 0).all()) and bool((db[:-1] == 0).all())
