@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(ExchangeArgs p)
     constexpr int V = ODT == MOE_F32 || YDT == MOE_F32 ? 4 : 8, N = K ? K : 1;
     const int lane = threadIdx.x & 63, steps = p.d / V;
     const int active = min(p.active_rows ? *p.active_rows : p.R, p.R);
-    for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < p.T; t += gridDim.x * 4) {
+    for (uint32_t t = blockIdx.x * 4 + (threadIdx.x >> 6); t < (uint32_t)p.T; t += gridDim.x * 4) {       // (unsigned: T and a stride of up to 2^22 stay below 2^32)
         for (int j0 = 0; j0 < (K ? 1 : p.k); ++j0) {
             const size_t a = (size_t)t * (K ? K : p.k) + j0;
             int r[N];

@@ -167,3 +167,25 @@ def test_replays_from_a_graph_and_on_a_side_stream():
             graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((dy, ds, dx), want)), rep
+
+
+@pytest.mark.parametrize("T", [2 ** 22 * 4 + 5, 2 ** 31 - 1])
+def test_combine_backward_of_more_tokens_than_a_launch_has_wavefronts(T):
+    """The wavefronts' steps over the tokens end at T, also where T and a step together pass 2^31; every token has its dscale, the last one included."""
+    need = T * (16 + 4 + 4 + 4)
+    if torch.cuda.mem_get_info()[0] < need + (8 << 30):
+        pytest.skip("%d GB of memory needed" % (need >> 30))
+    dout = torch.empty((T, 8), dtype=torch.float16, device="cuda").fill_(0.5)
+    y = torch.full((4, 8), 2.0, dtype=torch.float16, device="cuda")
+    inv = torch.empty(T, dtype=torch.int32, device="cuda").fill_(-1)
+    inv[0], inv[T // 2], inv[T - 2], inv[T - 1] = 0, 1, 2, 3
+    scale = torch.empty((T, 1), device="cuda").fill_(0.25)
+    ds = torch.empty((T, 1), device="cuda").fill_(7.0)
+    dy, _ = B.moe_combine_backward(dout, y, inv, scale, out=(torch.zeros_like(y), ds))
+    torch.cuda.synchronize()
+    assert bool((dy == 0.125).all())
+    assert [float(ds[i]) for i in (0, T // 2, T - 2, T - 1)] == [8.0] * 4
+    ends = (ds[:1 << 23], ds[-(1 << 23):])
+    assert [int((t != 0).sum()) for t in ends] == [1, 2] and all(bool(((t == 0) | (t == 8)).all()) for t in ends)
+    del dout, inv, scale, ds, ends
+    torch.cuda.empty_cache()
