@@ -717,7 +717,7 @@ def moe_permute_backward(dx_perm, inv_perm, T: int, k: int, active_rows=None, ou
 
 def _rows(t, name, columns, dtypes):
     """(pointer, values from row to row) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.shape[1] != columns or not t.is_cuda or (t.stride(1) != 1 and columns > 1):
+    if t.dim() != 2 or t.shape[1] != columns or not t.is_cuda or (t.stride(1) != 1 and columns > 1 and t.shape[0]):
         raise MoeError("%s must be a [.., %d] CUDA tensor with contiguous rows" % (name, columns))
     if t.dtype not in dtypes:
         raise MoeError("%s has dtype %s, expected %s" % (name, t.dtype, dtypes))

@@ -27,8 +27,8 @@ static int check_adapters(const AdapterCall &c)
     if (c.K > 1 << 20 || c.N > 1 << 20) return fail(MOE_ERR_UNSUPPORTED, "%s: K and N of at most 2^20", what);
     if (c.dtype != MOE_F16 && c.dtype != MOE_BF16) return fail(MOE_ERR_UNSUPPORTED, "%s: x and the adapters must be fp16 or bf16", what);
     if (!known_dtype(c.other_dtype)) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
-    if (!c.perm_src && c.by_assignment) return fail(MOE_ERR_INVALID_ARG, "%s: rows by assignment need perm_src", what);
-    if (!c.perm_src && c.k != 1) return fail(MOE_ERR_INVALID_ARG, "%s: without perm_src there is one row per row of x (k=%d)", what, c.k);
+    if (c.R > 0 && !c.perm_src && c.by_assignment) return fail(MOE_ERR_INVALID_ARG, "%s: rows by assignment need perm_src", what);
+    if (c.R > 0 && !c.perm_src && c.k != 1) return fail(MOE_ERR_INVALID_ARG, "%s: without perm_src there is one row per row of x (k=%d)", what, c.k);
     if (c.R > 0 && (c.perm_src ? (long long)c.T * c.k != c.R : c.T < c.R)) return fail(MOE_ERR_INVALID_ARG, "%s: %d rows do not fit %d tokens, %d each", what, c.R, c.T, c.k);
     if (!c.offsets || !c.a || !c.b) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     if (!aligned16(c.a) || !aligned16(c.b)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);

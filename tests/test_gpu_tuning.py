@@ -4,6 +4,7 @@ import torch
 
 from paper_2211_10017_amd import (AdamW, LowRankAdapters, MoEExpertLayer, MoEMx4Layer, adapt, adapter_index, balance_loss, combine_tokens, permute_tokens)
 from paper_2211_10017_amd import binding as B
+from paper_2211_10017_amd.adapters import AdapterIndex
 from paper_2211_10017_amd.mx4_router_tuning import tune
 from tuning_ref import BF16, F16, F32, U, adapters_ref, generator, routing, sorted_index, within
 
@@ -306,3 +307,15 @@ def test_the_tuning_command_with_adapters_runs(optimizer):
     lines = []
     first, last, losses = tune(steps=3, T=64, d=128, F=128, E=8, adapter_rank=4, optimizer=optimizer, report=lines.append)
     assert len(losses) == 3 and all(0 < v < 100 for v in losses + [first, last]) and len(lines) == 2
+
+
+@pytest.mark.parametrize("k,by_assignment", [(1, True), (1, False), (2, False)])
+def test_no_tokens_at_all(k, by_assignment):
+    """An empty batch through the functions with gradients: empty rows, gradients of 0 for the matrices."""
+    a = LowRankAdapters(4, 8, 64, 72).requires_grad_()
+    x = torch.zeros((0, 64), dtype=F16, device="cuda", requires_grad=True)
+    rows = torch.empty(0, dtype=torch.int32, device="cuda")
+    out = a(x, None, AdapterIndex(rows, rows, torch.zeros(5, dtype=torch.int32, device="cuda"), k), by_assignment=by_assignment)
+    out.float().sum().backward()
+    torch.cuda.synchronize()
+    assert out.shape == (0, 72) and x.grad.shape == (0, 64) and bool((a.a.grad == 0).all()) and bool((a.b.grad == 0).all())

@@ -245,3 +245,13 @@ def test_objects_refuse_what_calls_would():
         one.load_state_dict(AdamW([p], bits=8).state_dict())
     with pytest.raises(B.MoeError, match="scale"):
         adapt(None, None, a.a, a.b, None, a.scale.requires_grad_())
+
+
+def test_adapters_of_no_rows_take_null_buffers():
+    """An empty batch's buffers are NULL, its index too, whatever k and the order are; gradients of the matrices are still written (as 0)."""
+    calls = []
+    for k, by_assignment in ((1, 0), (1, 1), (2, 0), (2, 1)):
+        calls += [("moe_adapters", [None, F16, [64], 0, None, k, PTR, 0, 4, 64, 64, 4, PTR, PTR, None, by_assignment, None, [64], None, [64], F16, None, None]),
+                  ("moe_adapters_backward", [None, F16, [64], None, F16, [64], 0, None, k, PTR, 0, 4, 64, 64, 4, PTR, PTR, None, by_assignment, None, None, [64], PTR, PTR, F32, None, [0], None])]
+    got = record(calls)
+    assert [c.rc for c in got] == [OK] * len(calls) and [len(c.launches) for c in got] == [0, 1] * (len(calls) // 2)
