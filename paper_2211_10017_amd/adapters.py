@@ -85,8 +85,10 @@ class LowRankAdapters:
         return adapter_index(adapter_idx, self.E)
 
     def add(self, x, y, index, by_assignment=None):
-        """y += the adapters' term, in place, without gradients.  Requests (k = 1): y in their order; an expert layer's rows: sorted."""
-        return B.moe_adapters(x, self.a.detach(), self.b.detach(), index.offsets, index.perm_src, index.k, self.scale, index.k == 1 if by_assignment is None else by_assignment, y=y, out=y)
+        """y += the adapters' term, in place, without gradients (for autograd y has been changed).  Requests (k = 1): y in their order; an expert layer's rows: sorted."""
+        B.moe_adapters(x, self.a.detach(), self.b.detach(), index.offsets, index.perm_src, index.k, self.scale, index.k == 1 if by_assignment is None else by_assignment, y=y, out=y)
+        torch.autograd.graph.increment_version(y)
+        return y
 
     def __call__(self, x, y, index, by_assignment=None):
         return adapt(x, y, self.a, self.b, index, self.scale, index.k == 1 if by_assignment is None else by_assignment)

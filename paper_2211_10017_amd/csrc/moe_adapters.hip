@@ -76,6 +76,7 @@ extern "C" int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, c
     if (y)
         if (const int rc = check_rows(what, "y", y, y_stride, N)) return rc;
     if (y == out && y_stride != out_stride) return fail(MOE_ERR_INVALID_ARG, "%s: in place the strides of y and out are one", what);
+    if (out == x) return fail(MOE_ERR_INVALID_ARG, "%s: out is x, which other blocks still read", what);
     AdapterArgs p{};
     p.offsets = expert_offsets, p.scale = scale, p.R = R, p.E = E, p.K = K, p.N = N, p.rank = rank;
     p.x = x, p.a = a, p.b = b, p.x_map = RowMap{perm_src, k, T, x_stride};
@@ -111,6 +112,7 @@ extern "C" int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_st
         const size_t need = moe_adapters_backward_workspace_bytes(R, E, K, N, rank);
         if (!workspace || workspace_bytes < need) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", what, need, workspace_bytes);
         if (!aligned16(workspace) || !aligned16(v)) return fail(MOE_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", what);
+        if (dx && (dx == dy || dx == x)) return fail(MOE_ERR_INVALID_ARG, "%s: dx is dy or x, which are still read", what);
     }
     const hipStream_t s = as_stream(stream);
     const RowMap tokens{perm_src, k, T, x_stride}, rows{by_assignment ? perm_src : nullptr, 1, R, dy_stride};

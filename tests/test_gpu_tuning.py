@@ -319,3 +319,22 @@ def test_no_tokens_at_all(k, by_assignment):
     out.float().sum().backward()
     torch.cuda.synchronize()
     assert out.shape == (0, 72) and x.grad.shape == (0, 64) and bool((a.a.grad == 0).all()) and bool((a.b.grad == 0).all())
+
+
+def test_adding_in_place_counts_as_a_change():
+    """Autograd must not take y's rows for those that it kept."""
+    gen, T = generator(7), 40
+    requests = LowRankAdapters(4, 8, 64, 64)
+    requests.b.normal_(generator=gen)
+    x, w = r(gen, T, 64).half(), r(gen, T, 64).half().requires_grad_()
+    index = requests.index(torch.zeros(T, dtype=torch.int32, device="cuda"))
+    y = w * 2.0
+    kept = y.square()
+    requests.add(x, y.detach(), index)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.float().sum().backward()
+    with torch.inference_mode():
+        z = torch.zeros((T, 64), dtype=F16, device="cuda")
+        assert requests.add(x, z, index) is z and bool((z != 0).any())
+    with pytest.raises(B.MoeError, match="out is x"):
+        requests.add(x, x, index)

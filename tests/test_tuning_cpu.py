@@ -198,10 +198,13 @@ def test_the_largest_batches_take_a_launch():
             assert got.rc == OK and len(got.launches) == 1 and 0 < got.launches[0].grid[0] * got.launches[0].block < 2 ** 32
 
 
+X, DX = 1 << 40, 1 << 41                                             # buffers of their own
+
+
 def _calls(T, k, E, K, N, rank, dt=F16, ydt=F16, v=PTR, y=PTR, out=PTR):
     R = T * k
-    forward = ("moe_adapters", [PTR, dt, [K], T, PTR, k, PTR, R, E, K, N, rank, PTR, PTR, None, 0, y, [N], out, [N], ydt, v, None])
-    backward = ("moe_adapters_backward", [PTR, ydt, [N], PTR, dt, [K], T, PTR, k, PTR, R, E, K, N, rank, PTR, PTR, None, 0, PTR, PTR, [K], PTR, PTR, F32, PTR, [1 << 40], None])
+    forward = ("moe_adapters", [X, dt, [K], T, PTR, k, PTR, R, E, K, N, rank, PTR, PTR, None, 0, y, [N], out, [N], ydt, v, None])
+    backward = ("moe_adapters_backward", [PTR, ydt, [N], PTR, dt, [K], T, PTR, k, PTR, R, E, K, N, rank, PTR, PTR, None, 0, PTR, DX, [K], PTR, PTR, F32, PTR, [1 << 40], None])
     return forward, backward
 
 
@@ -255,3 +258,11 @@ def test_adapters_of_no_rows_take_null_buffers():
                   ("moe_adapters_backward", [None, F16, [64], None, F16, [64], 0, None, k, PTR, 0, 4, 64, 64, 4, PTR, PTR, None, by_assignment, None, None, [64], PTR, PTR, F32, None, [0], None])]
     got = record(calls)
     assert [c.rc for c in got] == [OK] * len(calls) and [len(c.launches) for c in got] == [0, 1] * (len(calls) // 2)
+
+
+def test_adapters_refuse_to_write_what_they_read():
+    forward, backward = _calls(64, 1, 4, 64, 64, 8)
+    at = lambda call, **new: (call[0], [new.get("i%d" % i, a) for i, a in enumerate(call[1])])  # noqa: E731
+    assert forward[1][0] == X and forward[1][18] == PTR and [backward[1][i] for i in (0, 3, 20)] == [PTR, PTR, DX]
+    calls = [forward, backward, at(forward, i0=PTR), at(backward, i20=PTR), at(backward, i0=X, i20=X), at(backward, i3=DX), at(backward, i20=None)]
+    assert [c.rc for c in record(calls)] == [OK, OK, ARG, ARG, ARG, ARG, OK]
