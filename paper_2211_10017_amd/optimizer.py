@@ -31,13 +31,13 @@ class AdamW:
         self.exp_avg, self.exp_avg_sq = ([state(p) for p in self.params] for _ in range(2))
 
     def step(self, grad_scale: float = 1.0):
-        self.steps += 1
         groups = {}
         for i, p in enumerate(self.params):
             if p.grad is not None:
                 if p.grad.is_sparse:
                     raise B.MoeError("gradients must be dense")
                 groups.setdefault((p.dtype if self.masters[i] is not None else None, p.grad.dtype), []).append(i)
+        self.steps += 1                                     # (a refused gradient is no step)
         for (half, _), at in groups.items():
             params = [self.params[i].detach() for i in at]
             B.moe_adamw([self.masters[i] for i in at] if half else params, [self.params[i].grad.contiguous() for i in at], [self.exp_avg[i] for i in at], [self.exp_avg_sq[i] for i in at],

@@ -266,3 +266,12 @@ def test_adapters_refuse_to_write_what_they_read():
     assert forward[1][0] == X and forward[1][18] == PTR and [backward[1][i] for i in (0, 3, 20)] == [PTR, PTR, DX]
     calls = [forward, backward, at(forward, i0=PTR), at(backward, i20=PTR), at(backward, i0=X, i20=X), at(backward, i3=DX), at(backward, i20=None)]
     assert [c.rc for c in record(calls)] == [OK, OK, ARG, ARG, ARG, ARG, OK]
+
+
+def test_a_refused_gradient_is_no_step():
+    p = torch.zeros((4, 2), requires_grad=True)
+    one = AdamW([p])
+    p.grad = torch.zeros((4, 2)).to_sparse()
+    with pytest.raises(B.MoeError, match="dense"):
+        one.step()
+    assert one.steps == 0
