@@ -85,7 +85,7 @@ struct OuterArgs {
     const int32_t *offsets;
     int R, E, rank, out_dtype;
     OuterJob job[2];
-    int first;                  // blocks of job 0
+    int first, items;           // blocks of job 0, and of both (the grid is rounded up; a job without `out` has none)
     int turns;                  // parts of the rank
     int join;                   // adapters that can have more than one chunk
 };

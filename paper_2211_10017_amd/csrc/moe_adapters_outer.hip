@@ -178,6 +178,7 @@ template <int DT0, int DT1, int NT, int TERMS>
 __global__ __launch_bounds__(64, 3) void adapter_outer_kernel(OuterArgs p)
 {
     const int turn = blockIdx.x / kXcds, item = turn / p.turns * kXcds + blockIdx.x % kXcds, first = turn % p.turns * 16 * NT;
+    if (item >= p.items) return;
     if (item < p.first) outer_item<DT0, NT, DT0 == MOE_BF16 ? TERMS : 2>(p, p.job[0], item, first);
     else outer_item<DT1, NT, DT1 == MOE_BF16 ? TERMS : 2>(p, p.job[1], item - p.first, first);
 }
@@ -238,7 +239,7 @@ int launch_adapter_outer(const OuterArgs &args, int dtype0, int dtype1, hipStrea
         }
     }
     if (blocks[0] + blocks[1] == 0) return MOE_OK;
-    p.first = (int)blocks[0], p.turns = p.rank <= 16 ? 1 : (p.rank + 31) / 32;
+    p.first = (int)blocks[0], p.items = (int)(blocks[0] + blocks[1]), p.turns = p.rank <= 16 ? 1 : (p.rank + 31) / 32;
     const long grid = (blocks[0] + blocks[1] + kXcds - 1) / kXcds * kXcds * p.turns;
     if (grid > 0x3ffffff) return fail(MOE_ERR_UNSUPPORTED, "%s: %ld workgroups exceed one launch", what, grid);
     auto run = [&](auto d0, auto d1) {

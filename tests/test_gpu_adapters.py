@@ -260,3 +260,35 @@ def test_gradients_of_few_adapters_with_all_the_rows(R, E):
     within(da, want["da"], want["da_mag"] + 2.0 ** -23 * want["da"].abs())
     within(db, want["db"], want["db_mag"] + 2.0 ** -23 * want["db"].abs())
     assert bool((da[:-1] == 0).all()) and bool((db[:-1] == 0).all())
+
+
+@pytest.mark.parametrize("xt,yt", TYPES)
+@pytest.mark.parametrize("T,rank", [(3400, 50), (7000, 64), (8200, 33), (11800, 61), (3400, 127), (9000, 100), (10100, 128)])
+def test_blocks_of_a_high_rank(T, rank, xt, yt):
+    """Shares of rows that fill blocks of 32, 48 and 64 rows, with ranks above 32."""
+    test_forward_and_backward(T, 1, 5, 72, 136, rank, "even", xt, yt, True)
+
+
+@pytest.mark.parametrize("T,rank", [(3400, 16), (3400, 50), (8000, 60), (9000, 100)])
+def test_gradient_of_a_alone(T, rank):
+    """Coefficients that are wanted by themselves, in blocks of more than sixteen rows."""
+    d = inputs(T, 1, 5, 72, 136, rank, "pruned", BF16, F32)
+    index = dict(perm_src=d["perm"], scale=d["scale"], by_assignment=True)
+    want = adapters_ref(d["x"], d["a"], d["b"], d["offsets"], d["perm"], 1, d["scale"], True, d["y"], d["dy"])
+    dx, da, db = B.moe_adapters_backward(d["dy"], d["x"], d["a"], d["b"], None, d["offsets"], need=(False, True, False), **index)
+    torch.cuda.synchronize()
+    assert dx is None and db is None
+    within(da, want["da"], want["da_mag"] + 2.0 ** -23 * want["da"].abs())
+
+
+@pytest.mark.parametrize("E", range(1, 10))
+def test_one_matrix_of_any_number_of_adapters(E):
+    """The grid is rounded up to whole rounds of the eight XCDs: what is left over belongs to neither matrix, also where one of them is not wanted."""
+    d = inputs(40, 1, E, 64, 64, 8, "even", F16, F16)
+    index = dict(perm_src=d["perm"], scale=d["scale"])
+    v = torch.empty((40, 8), device="cuda")
+    B.moe_adapters(d["x"], d["a"], d["b"], d["offsets"], y=d["y"], v=v, **index)
+    _, da, db = B.moe_adapters_backward(d["dy"], d["x"], d["a"], d["b"], v, d["offsets"], **index)
+    for kept in (v, None):
+        assert torch.equal(B.moe_adapters_backward(d["dy"], d["x"], d["a"], d["b"], kept, d["offsets"], need=(False, True, False), **index)[1], da)
+    assert torch.equal(B.moe_adapters_backward(d["dy"], None, d["a"], d["b"], v, d["offsets"], need=(False, False, True), **index)[2], db)
