@@ -436,7 +436,8 @@ static int launch_expand(AdapterArgs p, int share, int slices, hipStream_t s, co
 }
 
 // One block per compute unit, of the fewest rows' registers that hold its share (32 adapters of 4096 x 4096, rank 16 / 32, bf16, in blocks of up to 16, 32, 48 and 80 rows: 3000 rows, shares of 12,
-// 22 / 27, 27 / 33, 34 / 38, 47 / 54 us; 3968, 16, 34 / 46, 28 / 34, 35 / 39, 48 / 55; 7000, 28, 54, 44, 47, 58; 8192, 33, 69, 60, 54, 62; 11000, 44, 81 / 103, 72 / 87, 66 / 71, 72 / 80).
+// 22 / 27, 27 / 33, 34 / 38, 47 / 54 us; 3968, 16, 34 / 46, 28 / 34, 35 / 39, 48 / 55; 7000, 28, 54, 44, 47, 58; 8192, 33, 69, 60, 54, 62; 11000, 44, 81 / 103, 72 / 87, 66 / 71, 72 / 80.
+// Rank 64 in blocks of up to 16, 32, 48 and 64 rows: 3968, 74, 52, 60, 68; 7000, 63 of 32, 71, 77; 8192, 110, 76, 82.  Rank 128, 16, 32 and 48: 3968, 133, 82, 97; 7000, 93 of 32, 105.)
 template <int XDT, int WDT, int ODT, bool Y, int NT>
 static int launch_rank(const AdapterArgs &p, hipStream_t s, const char *what)
 {
@@ -475,8 +476,8 @@ static int launch_rank(const AdapterArgs &p, hipStream_t s, const char *what)
     }
     const long rounds = ((long)p.R + kUnits * (kMost - 8) - 1) / (kUnits * (kMost - 8));
     const int share = (int)((p.R + kUnits * rounds - 1) / (kUnits * rounds));
-    if constexpr (NT <= 2) {
-        if (share <= 29) return launch_shape<XDT, WDT, ODT, Y, 8, 2, NT>(p, share, 1, s, what);
+    if (share <= 29) return launch_shape<XDT, WDT, ODT, Y, 8, 2, NT>(p, share, 1, s, what);
+    if constexpr (NT <= 4) {
         if (share <= 45) return launch_shape<XDT, WDT, ODT, Y, 8, 3, NT>(p, share, 1, s, what);
     }
     return launch_shape<XDT, WDT, ODT, Y, 8, kMost / 16, NT>(p, share, 1, s, what);
