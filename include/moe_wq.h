@@ -472,6 +472,9 @@ int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_stride, const
  *   state_bits 32: m and v are fp32 [n].  state_bits 8: m holds codes of m, v codes of sqrt(v), n bytes each, e4m3 numbers in units of 2^(scale - 127), a byte of
  *   m_scales / v_scales for each 32 neighbouring values ([ceil(n/32)]): with amax the largest magnitude of the 32, scale = floor(log2(amax)) - 7 + 127, at least 0; nearest code,
  *   ties to the even one, but for sqrt(v) > 0 at least the smallest number; 255 for a block with an infinity or a NaN, which then reads as NaN.  All zero bytes: zeros.
+ *   state_bits 8 | MOE_ADAMW_RANDOM: the same states, but each code is one of the two next to its value, the upper one with probability (value - lower) / (upper - lower), by a fixed
+ *   function of t and the value's index: equal calls give equal states, and the mean of what is held is the value.  A run of steps takes this one.  To the nearest code a moment that changes
+ *   by less than half the distance of two codes stays where it is, sqrt(v) for good at the usual beta2, and steps become several times too large.
  *   tensors: HOST array (read before the call returns); its pointers are device pointers, aligned for their types (16-byte alignment is the fast way).  No two tensors overlap.
  *   step_ptr: t on the device instead of `step` (a captured step then counts on; numbers below 1 count as 1), or NULL.
  * moe_adamw_state: the values of n codes, [n] in out_dtype.
@@ -484,6 +487,7 @@ typedef struct {
     void *copy;
     int64_t n;
 } moe_adamw_tensor;
+enum { MOE_ADAMW_RANDOM = 256 };
 int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2,
               double eps, double weight_decay, double grad_scale, int step, const int32_t *step_ptr, void *stream);
 int moe_adamw_state(const void *codes, const void *scales, int64_t n, void *out, int out_dtype, void *stream);

@@ -18,6 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoe_wq.so")
 
 MOE_F16, MOE_BF16, MOE_F32 = 0, 1, 2
+MOE_ADAMW_RANDOM = 256
 _DT = {torch.float16: MOE_F16, torch.bfloat16: MOE_BF16, torch.float32: MOE_F32}
 
 EXPORTS = ["moe_last_error", "moe_last_ffn_kernels", "moe_device_info", "moe_abi_version", "moe_quantize_experts", "moe_gate_topk",
@@ -815,17 +816,21 @@ def _pairs(states):
     return [s[0] for s in states], [s[1] for s in states]
 
 
-def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, copies=None):
+def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, copies=None,
+              rounding: str = "nearest"):
     """An AdamW step over lists of tensors, in place (include/moe_wq.h).
 
     params of one type, grads of one type.  exp_avg and exp_avg_sq: fp32 tensors, or pairs (codes uint8 [n], scales uint8 [ceil(n/32)]) for states in 8 bits, of the moment and
-    of the second one's root.  step: the step's number from 1 on, or an int32 CUDA tensor that holds it.  copies: 16-bit copies of fp32 params to be written as well."""
+    of the second one's root.  step: the step's number from 1 on, or an int32 CUDA tensor that holds it.  copies: 16-bit copies of fp32 params to be written as well.
+    rounding of states in 8 bits: "nearest", which is one step's best but over many steps keeps the second moment from falling, or "random", whose mean is the value: a program's steps take it."""
     count = len(params)
     if not count == len(grads) == len(exp_avg) == len(exp_avg_sq) or (copies is not None and len(copies) != count):
         raise MoeError("params, grads, exp_avg, exp_avg_sq and copies must be lists of one length")
     if not count:
         return
     bits = 8 if isinstance(exp_avg[0], (tuple, list)) else 32
+    if rounding not in ("nearest", "random"):
+        raise MoeError("rounding is nearest or random, not %r" % (rounding,))
     pd, gd, cd = params[0].dtype, grads[0].dtype, copies[0].dtype if copies is not None else None
     if pd not in _DT or gd not in _DT or (cd is not None and cd not in (torch.float16, torch.bfloat16)):
         raise MoeError("parameters and gradients must be fp16, bf16 or fp32, copies fp16 or bf16")
@@ -868,7 +873,7 @@ def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=
         if step.numel() != 1:
             raise MoeError("step must be one number")
         _check_device(step)
-    rc = load().moe_adamw(table.buffer_info()[0], count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits, lr, betas[0], betas[1], eps, weight_decay, grad_scale,
+    rc = load().moe_adamw(table.buffer_info()[0], count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits | (MOE_ADAMW_RANDOM if bits == 8 and rounding == "random" else 0), lr, betas[0], betas[1], eps, weight_decay, grad_scale,
                           1 if on_device else step, _ptr(step, torch.int32, "step") if on_device else None, _stream())
     _check(rc, "moe_adamw")
 

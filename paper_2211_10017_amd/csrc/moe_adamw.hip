@@ -7,6 +7,10 @@
 // 32 neighbouring values: the largest then lies in [128, 256) and every rounding stays below e4m3's largest number; values 2^-17 of it and less become 0, but a positive r at least
 // the smallest number, 2^-9 units: an r of 0 beside an m that is not would make a step of m / eps.  The root, as its range is half that of v in powers of two.
 // The step itself uses m and v as they are before they are rounded to 8 bits.
+//
+// To the nearest number r cannot follow its average: with b2 = 0.999 it falls by 0.05 % a step at most, half the distance to the next number is 3 to 6 %, so it stays where it is (as does m, with
+// b1 = 0.9, up to 1.6 times short of a constant gradient).  RANDOM: up or down by chance, so that the mean of what is held is the number itself, of m and of r, whatever their change in a step.
+// r then wanders about its average, by 4 % under constant gradients and 14 % under normal ones, its mean and that of 1 / r move by less than 2 %.
 #include <math.h>
 
 #include "moe_rows.h"
@@ -24,6 +28,7 @@ struct AdamTensors {
     float rate, root;                                           // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
     double lr, beta1, beta2;
     const int32_t *step;                                        // [1] or null: t on the device, rate and root come from it
+    int number;                                                 // t where the host knows it
 };
 
 // b^t by squaring, in products alone: the host's bits and the device's are the same, whichever of them knows t.
@@ -57,9 +62,25 @@ __device__ inline int scale_byte(float amax)
 
 __device__ inline float scale_value(int byte) { return byte == 255 ? NAN : pow2(byte - 127); }
 
-// Four values in 8 bits.  ROOT: of r = sqrt(v), which stays above 0.
-template <bool ROOT>
-__device__ inline uint32_t encode(const float (&v)[4], int byte)
+// 32 bits for a number of 32: products with odd numbers (the fractions of the golden ratio and of the root of 2), each between shifts that bring the upper half to the lower one.
+__device__ inline uint32_t mixed(uint32_t x)
+{
+    x = (x ^ x >> 16) * 0x9e3779b1u;
+    x = (x ^ x >> 15) * 0x6a09e667u;
+    return x ^ x >> 16;
+}
+
+// a >= 0 to one of the two e4m3 numbers beside it: up where the 20 bits behind the third of the mantissa and 20 random ones together carry.  Numbers below 2^-6, whose steps are all 2^-9, are
+// brought into [2^-6, 2^-5), where the steps are the same.
+__device__ inline float rounded_by(float a, uint32_t random)
+{
+    const float up = a < 0x1p-6f ? 0x1p-6f : 0.0f;
+    return __uint_as_float((__float_as_uint(a + up) + (random >> 12)) & 0xfff00000u) - up;
+}
+
+// Four values in 8 bits.  ROOT: of r = sqrt(v), which stays above 0.  RANDOM: by each value's 32 random bits, of which r takes the upper and m the lower ones (in reverse).
+template <bool ROOT, bool RANDOM>
+__device__ inline uint32_t encode(const float (&v)[4], int byte, const uint32_t (&random)[4])
 {
     if (byte == 255) return 0;
     const float inv = pow2(127 - byte);
@@ -67,6 +88,7 @@ __device__ inline uint32_t encode(const float (&v)[4], int byte)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         q[i] = v[i] * inv;
+        if constexpr (RANDOM) q[i] = ROOT ? rounded_by(q[i], random[i]) : copysignf(rounded_by(fabsf(q[i]), __brev(random[i])), q[i]);
         if (ROOT && v[i] > 0.0f) q[i] = fmaxf(q[i], 0x1p-9f);
     }
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
@@ -132,19 +154,20 @@ __device__ inline void store_codes(uint8_t *base, int64_t at, int n, uint32_t w)
         if (i < n) base[at + i] = (uint8_t)(w >> (8 * i));
 }
 
-// Bound by memory: 134 million values with states in 8 bits, bf16 gradients and copies 16.1 bytes each, 405 us = 5.3 TB/s; 25 million with fp32 states 28 bytes each, 139 us = 5.1 TB/s.
+// Bound by memory: 134 million values with states in 8 bits, bf16 gradients and copies 16.1 bytes each, 405 us = 5.3 TB/s (a call of 417 to the nearest, 419 RANDOM); 25 million with fp32 states 28 bytes each, 139 us = 5.1 TB/s.
 // The products and sums of m and v are rounded one by one (no fused multiply-adds): the definition is then the same on every path.
-template <int PDT, int GDT, int CDT, int BITS, bool WIDE>
+template <int PDT, int GDT, int CDT, int STATES, bool WIDE>
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTensors a)
 {
 #pragma clang fp contract(off)
+    constexpr int BITS = STATES & 0xff;
+    constexpr bool RANDOM = (STATES & MOE_ADAMW_RANDOM) != 0;
     __shared__ float from_step[2];
     float rate = a.rate, root = a.root;
+    int number = a.number;
     if (a.step) {
-        if (threadIdx.x == 0) {
-            const int t = max(*a.step, 1);
-            from_step[0] = step_rate(a.lr, a.beta1, t), from_step[1] = step_root(a.beta2, t);
-        }
+        number = max(*a.step, 1);
+        if (threadIdx.x == 0) from_step[0] = step_rate(a.lr, a.beta1, number), from_step[1] = step_root(a.beta2, number);
         __syncthreads();
         rate = from_step[0], root = from_step[1];
     }
@@ -152,6 +175,8 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTensors a)
     while (i + 1 < a.count && (int)blockIdx.x >= a.first[i + 1]) ++i;
     const moe_adamw_tensor &t = a.t[i];
     const int64_t start = (int64_t)((int)blockIdx.x - a.first[i]) * a.chunk, end = min(t.n, start + (int64_t)a.chunk);
+    // (a value's random bits come from the step's number and its place alone; a block has one upper half of places)
+    const uint32_t seed = RANDOM ? mixed((uint32_t)number ^ mixed((uint32_t)(start >> 32))) : 0;
     for (int64_t at = start + threadIdx.x * 4; at < (end + 31) / 32 * 32; at += kAdamThreads * 4) {      // (whole blocks of 32: their eight lanes stay together)
         const int n = (int)min((int64_t)4, max((int64_t)0, end - at));
         float p[4], g[4], m[4], v[4], r[4];
@@ -187,8 +212,13 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTensors a)
             }
             if (!fine) ma = ra = INFINITY;
             const int mb = scale_byte(max_of_8_lanes(ma)), rb = scale_byte(max_of_8_lanes(ra));
-            store_codes<WIDE>((uint8_t *)t.m, at, n, encode<false>(m, mb));
-            store_codes<WIDE>((uint8_t *)t.v, at, n, encode<true>(r, rb));
+            uint32_t random[4] = {};
+            if constexpr (RANDOM) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) random[q] = mixed(((uint32_t)at + q) ^ seed);
+            }
+            store_codes<WIDE>((uint8_t *)t.m, at, n, encode<false, RANDOM>(m, mb, random));
+            store_codes<WIDE>((uint8_t *)t.v, at, n, encode<true, RANDOM>(r, rb, random));
             if ((threadIdx.x & 7) == 0) t.m_scales[at >> 5] = (uint8_t)mb, t.v_scales[at >> 5] = (uint8_t)rb;
         } else {
             store4<MOE_F32, WIDE>(t.m, at, n, m);
@@ -244,7 +274,7 @@ extern "C" int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype
     if (count < 0 || (count > 0 && !tensors)) return fail(MOE_ERR_INVALID_ARG, "%s: no tensors", what);
     if (!known_dtype(p_dtype) || !known_dtype(g_dtype) || (copy_dtype != -1 && copy_dtype != MOE_F16 && copy_dtype != MOE_BF16)) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
     if (copy_dtype != -1 && p_dtype != MOE_F32) return fail(MOE_ERR_UNSUPPORTED, "%s: a copy belongs to fp32 parameters", what);
-    if (state_bits != 32 && state_bits != 8) return fail(MOE_ERR_UNSUPPORTED, "%s: states of %d bits", what, state_bits);
+    if (state_bits != 32 && state_bits != 8 && state_bits != (8 | MOE_ADAMW_RANDOM)) return fail(MOE_ERR_UNSUPPORTED, "%s: states of %d bits", what, state_bits);
     if (!step_ptr && step < 1) return fail(MOE_ERR_INVALID_ARG, "%s: steps are counted from 1", what);
     if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1)) return fail(MOE_ERR_INVALID_ARG, "%s: 0 <= beta < 1 required", what);
     if (!(lr >= 0) || !(eps >= 0) || !(weight_decay >= 0) || !isfinite(lr) || !isfinite(eps) || !isfinite(weight_decay) || !isfinite(grad_scale))
@@ -255,9 +285,9 @@ extern "C" int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype
         if (t.n < 0) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d has %lld values", what, i, (long long)t.n);
         if (t.n == 0) continue;
         if (t.n > (int64_t)kAdamChunk << 22) return fail(MOE_ERR_UNSUPPORTED, "%s: tensor %d exceeds one launch", what, i);
-        if (!t.p || !t.g || !t.m || !t.v || (state_bits == 8 && (!t.m_scales || !t.v_scales)) || (copy_dtype != -1 && !t.copy))
+        if (!t.p || !t.g || !t.m || !t.v || (state_bits != 32 && (!t.m_scales || !t.v_scales)) || (copy_dtype != -1 && !t.copy))
             return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer in tensor %d", what, i);
-        const int state = state_bits == 8 ? 1 : 4;
+        const int state = state_bits == 32 ? 4 : 1;
         if (!aligned(t.p, size_of(p_dtype)) || !aligned(t.g, size_of(g_dtype)) || !aligned(t.m, state) || !aligned(t.v, state) || (copy_dtype != -1 && !aligned(t.copy, 2)))
             return fail(MOE_ERR_INVALID_ARG, "%s: a pointer of tensor %d is not aligned for its type", what, i);
         wide = wide && aligned(t.p, 4 * size_of(p_dtype)) && aligned(t.g, 4 * size_of(g_dtype)) && aligned(t.m, 4 * state) && aligned(t.v, 4 * state)
@@ -266,7 +296,7 @@ extern "C" int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype
     AdamTensors a;
     a.b1 = (float)beta1, a.b2 = (float)beta2, a.c1 = (float)(1.0 - beta1), a.c2 = (float)(1.0 - beta2), a.eps = (float)eps;
     a.decay = (float)(1.0 - lr * weight_decay), a.grad_scale = (float)grad_scale;
-    a.lr = lr, a.beta1 = beta1, a.beta2 = beta2, a.step = step_ptr;
+    a.lr = lr, a.beta1 = beta1, a.beta2 = beta2, a.step = step_ptr, a.number = step;
     a.rate = step_ptr ? 0.0f : step_rate(lr, beta1, step), a.root = step_ptr ? 0.0f : step_root(beta2, step);
     int64_t most = 0;
     for (int i = 0; i < count; ++i) most = tensors[i].n > most ? tensors[i].n : most;
@@ -292,7 +322,8 @@ extern "C" int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype
                 };
                 auto with_width = [&](auto cd, auto bits) { return wide ? run(cd, bits, std::true_type{}) : run(cd, bits, std::false_type{}); };
                 auto with_bits = [&](auto cd) {
-                    return state_bits == 8 ? with_width(cd, std::integral_constant<int, 8>{}) : with_width(cd, std::integral_constant<int, 32>{});
+                    if (state_bits == 32) return with_width(cd, std::integral_constant<int, 32>{});
+                    return state_bits == 8 ? with_width(cd, std::integral_constant<int, 8>{}) : with_width(cd, std::integral_constant<int, 8 | MOE_ADAMW_RANDOM>{});
                 };
                 if constexpr (P == MOE_F32) {
                     if (copy_dtype == MOE_F16) return with_bits(std::integral_constant<int, MOE_F16>{});

@@ -10,7 +10,7 @@ _HALVES = (torch.float16, torch.bfloat16)
 
 class AdamW:
     """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass.  step() takes the gradients that are there; a parameter
-    without one stays as it is."""
+    without one stays as it is.  States in 8 bits are rounded up or down by chance, the same in every run: to the nearest number they could not follow their averages."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, bits=32):
         self.params = list(params)
@@ -41,7 +41,7 @@ class AdamW:
         for (half, _), at in groups.items():
             params = [self.params[i].detach() for i in at]
             B.moe_adamw([self.masters[i] for i in at] if half else params, [self.params[i].grad.contiguous() for i in at], [self.exp_avg[i] for i in at], [self.exp_avg_sq[i] for i in at],
-                        self.steps, self.lr, self.betas, self.eps, self.weight_decay, grad_scale, copies=params if half else None)
+                        self.steps, self.lr, self.betas, self.eps, self.weight_decay, grad_scale, copies=params if half else None, rounding="random")
             # (written through pointers: a backward pass that still needs the old values raises)
             torch.autograd.graph.increment_version(params)
 

@@ -1,0 +1,183 @@
+"""States in 8 bits that are rounded up or down by chance: the definition code by code, what many steps make of it beside states in 32 bits, and that nothing but the step's number and a
+value's place decides."""
+import math
+
+import pytest
+import torch
+
+from paper_2211_10017_amd import AdamW
+from paper_2211_10017_amd import binding as B
+from tuning_ref import BF16, F16, F32, generator
+
+pytestmark = pytest.mark.gpu
+
+
+def mixed(x):
+    """The 32 bits that belong to a number of 32 (int64 tensors of values below 2^32)."""
+    x = ((x ^ (x >> 16)) * 0x9E3779B1) & 0xFFFFFFFF
+    x = ((x ^ (x >> 15)) * 0x6A09E667) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def random_bits(index, t):
+    """Twenty bits each for m and for the root, of the values at `index` in step t."""
+    whole = lambda v: torch.tensor([v], dtype=torch.int64, device="cuda")  # noqa: E731
+    w = mixed((index & 0xFFFFFFFF) ^ mixed(whole(t) ^ mixed(index >> 32)))
+    back = torch.zeros_like(w)
+    for i in range(32):
+        back |= ((w >> i) & 1) << (31 - i)
+    return back >> 12, w >> 12
+
+
+def rounded(v, bits, root):
+    """The values that v (64 bits, of fp32 numbers) is held as, and the scales."""
+    n = v.numel()
+    b, w = (torch.nn.functional.pad(t, (0, -n % 32)).view(-1, 32) for t in (v, bits.double()))
+    top = b.abs().amax(1, keepdim=True)
+    e = torch.where(top > 0, torch.frexp(top)[1] - 8, -127).clamp(min=-127)
+    a = b.abs() * torch.exp2(-e.double())
+    step = torch.exp2((torch.frexp(a)[1] - 4).clamp(min=-9).double())
+    lower = torch.floor(a / step)
+    # (a number below 2^-6 units has more bits than twenty behind the step's: they are rounded to twenty)
+    q = (lower + (torch.round((a / step - lower) * 2 ** 20) + w >= 2 ** 20)) * step
+    if root:
+        q = torch.where(a > 0, q.clamp(min=2.0 ** -9), q)
+    return (torch.sign(b) * q * torch.exp2(e.double())).view(-1)[:n], (e + 127).view(-1)
+
+
+def held(codes, scales):
+    return codes.view(torch.float8_e4m3fn).double() * torch.exp2(scales.double() - 127).repeat_interleave(32)[:codes.numel()]
+
+
+def states(n, offset=0):
+    zeros = lambda k: torch.zeros(k + offset, dtype=torch.uint8, device="cuda")[offset:]  # noqa: E731
+    return zeros(n), zeros((n + 31) // 32)
+
+
+@pytest.mark.parametrize("t", [1, 7, 2 ** 31 - 1])
+@pytest.mark.parametrize("n,offset", [(1, 0), (33, 1), (4096, 0), (70001, 0), (70001, 1)])
+def test_codes_are_the_definitions(n, offset, t):
+    """A step that leaves a chosen m behind (beta1 = 0: m = g, beta2 = 0.5: the root of g^2 / 2), values of all sizes in a block."""
+    print(f"adamw random n={n} +{offset} t={t}", flush=True)
+    gen = generator(n)
+    g = torch.randn(n, generator=gen, device="cuda") * torch.exp2(torch.randint(-20, 3, (n,), generator=gen, device="cuda").float())
+    g[torch.rand(n, generator=gen, device="cuda") < 0.02] = 0.0
+    sm, sv, nm, nv = states(n, offset), states(n, offset), states(n), states(n)
+    kw = dict(betas=(0.0, 0.5))
+    B.moe_adamw([torch.zeros(n, device="cuda")], [g], [sm], [sv], t, rounding="random", **kw)
+    B.moe_adamw([torch.zeros(n, device="cuda")], [g], [nm], [nv], t, **kw)
+    torch.cuda.synchronize()
+    bits_m, bits_r = random_bits(torch.arange(n, device="cuda"), t)
+    for got, nearest, v, bits, root in ((sm, nm, g.double(), bits_m, False), (sv, nv, torch.sqrt(g * g * 0.5).double(), bits_r, True)):
+        value, scale = rounded(v, bits, root)
+        assert torch.equal(got[1].long(), scale.long()) and torch.equal(got[1], nearest[1])
+        assert torch.equal(held(*got), value)
+        if n > 4096:
+            # as often up as the value is far up: the mean error of n values, each at most a step (an eighth of it) off, is below 4 / sqrt(n) of that
+            off = ((held(*got) - v) / v.abs().clamp(min=1e-30))[v.abs() > 2.0 ** -6 * torch.exp2(got[1].double() - 127).repeat_interleave(32)[:n]]
+            assert abs(float(off.mean())) <= 4 / math.sqrt(off.numel()) / 8
+
+
+def test_a_place_past_32_bits():
+    n = (1 << 32) + 4096
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("40 GB of memory needed")
+    p, g = torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
+    part = torch.randn(4096, generator=generator(2), device="cuda").to(BF16)
+    g[:4096], g[-4096:] = part, part
+    m, v = states(n), states(n)
+    B.moe_adamw([p], [g], [m], [v], 3, betas=(0.0, 0.5), rounding="random")
+    torch.cuda.synchronize()
+    for at in (0, 1 << 32):
+        bits_m, _ = random_bits(torch.arange(at, at + 4096, device="cuda"), 3)
+        assert torch.equal(held(m[0][at:at + 4096], m[1][at // 32:at // 32 + 128]), rounded(part.double(), bits_m, False)[0])
+    assert not torch.equal(m[0][:4096], m[0][-4096:])
+
+
+# Rounding by chance adds (distance to the lower number) x (distance to the upper one) to a moment's variance in each step, at most |change| x an eighth of the value.  Of the root: it changes
+# by (1 - b2) / 2 |g^2 / v - 1| of itself, under normal gradients by 0.48 (1 - b2) in the mean, and forgets by 1 - b2 a step, so its relative variance is at most 0.48 / 8 / 2 = 1/33; while a
+# constant gradient still builds it up (a change of 1 / (2 t), forgotten as (t' / t)^2) sum 1 / (16 t') (t' / t)^2 = 1/32.  The mean of the root is then off by at most half that, the
+# mean of a step, m / root, by at most that much; the tests allow twice.  Means are over 2^17 values, which adds 0.2 / sqrt(2^17), nothing beside it.
+_VARIANCE = 1 / 32
+_N = 1 << 17
+
+
+def _run(gradients, steps, at, kw):
+    """Parameters and roots of states in 8 and in 32 bits after the steps in `at`."""
+    ours, theirs = (torch.zeros(_N, device="cuda", requires_grad=True) for _ in range(2))
+    one, two = AdamW([ours], bits=8, **kw), AdamW([theirs], bits=32, **kw)
+    got = {}
+    for t in range(1, steps + 1):
+        ours.grad = theirs.grad = gradients(t)
+        one.step()
+        two.step()
+        if t in at:
+            roots = B.moe_adamw_state(*one.exp_avg_sq[0]).double(), two.exp_avg_sq[0].double().sqrt()
+            got[t] = tuple(x.detach().double().clone() for x in (ours, theirs)) + roots
+    return got
+
+
+@pytest.mark.parametrize("kind", ["constant", "normal"])
+def test_many_steps_follow_states_in_32_bits(kind):
+    gen = generator(4)
+    g = torch.ones(_N, device="cuda")
+    gradients = (lambda t: g) if kind == "constant" else (lambda t: g.normal_(generator=gen))
+    got = _run(gradients, 3000, (10, 100, 1000, 3000), dict(lr=1e-3, betas=(0.9, 0.999), weight_decay=0.0))
+    for t, (p, want, root, root32) in got.items():
+        assert abs(float(root.mean() / root32.mean()) - 1) <= _VARIANCE, t
+        assert abs(float((p * want).sum() / (want * want).sum()) - 1) <= 2 * _VARIANCE, t
+
+
+def test_gradients_that_become_small():
+    """A hundredth of the gradients from step 1000 on: the root falls as it does in 32 bits.  (Its variance grows by 0.0005 / 8 a step meanwhile, to 1/32 + 5000 / 16000 at the end; a step's
+    mean, 1 / root, by up to exp of that, 1.41.  Of the way in 32 bits, 958 rates up to step 1000 and 273 from then on, that is (958 (1 + 1/32) + 273 x 1.41) / 1231 = 1.12.)"""
+    gen = generator(6)
+    g = torch.empty(_N, device="cuda")
+    got = _run(lambda t: g.normal_(generator=gen).mul_(0.3).add_(1.0).mul_(1.0 if t <= 1000 else 0.01), 6000, (1000, 2000, 6000), dict(lr=1e-3, betas=(0.9, 0.999), weight_decay=0.0))
+    for t, (p, want, root, root32) in got.items():
+        assert abs(float(root.mean() / root32.mean()) - 1) <= _VARIANCE, t
+        assert 1 - 2 * _VARIANCE <= float((p * want).sum() / (want * want).sum()) <= 1.125, t
+
+
+def test_moments_of_values_without_gradients_go_to_zero():
+    """Beside a value whose gradient stays large.  In the mean a step leaves 0.9 of m: of some 27 of the smallest numbers 27 x 0.9^395 after 395 steps, 1e-14 over all of the 512 blocks."""
+    n = 32 * 512
+    p = torch.zeros(n, device="cuda", requires_grad=True)
+    optimiser = AdamW([p], lr=1e-3, weight_decay=0.0, bits=8)
+    for t in range(400):
+        p.grad = torch.zeros(n, device="cuda")
+        p.grad[::32] = 1.0
+        if t < 5:
+            p.grad[1::32] = 1e-3
+        optimiser.step()
+    m = B.moe_adamw_state(*optimiser.exp_avg[0]).view(-1, 32)
+    assert bool((m[:, 1:] == 0).all()) and bool((m[:, 0] > 0.5).all())
+
+
+@pytest.mark.parametrize("pd,gd,copy", [(F32, F16, F16), (F32, BF16, BF16), (F16, F16, None), (BF16, F32, None)])
+def test_equal_calls_give_equal_states(pd, gd, copy):
+    """In any list, from any alignment, with the step's number here or on the device (captured and replayed); parameters as with states rounded to nearest, in a step from the same states."""
+    sizes = [5000, 33, 1]
+    make = lambda: [torch.randn(n, generator=generator(n), device="cuda").to(pd) for n in sizes]  # noqa: E731
+    grads = [torch.randn(n, generator=generator(n + 1), device="cuda").to(gd) for n in sizes]
+    copies = lambda: [torch.empty(n, dtype=copy, device="cuda") for n in sizes] if copy else None  # noqa: E731
+    together, alone, captured, nearest = ([make(), [states(n, i == 1) for n in sizes], [states(n, i == 1) for n in sizes], copies()] for i in range(4))
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.add_(1)
+        B.moe_adamw(captured[0], grads, captured[1], captured[2], step, copies=captured[3], rounding="random")
+    for t in range(1, 5):
+        B.moe_adamw(together[0], grads, together[1], together[2], t, copies=together[3], rounding="random")
+        for i in range(len(sizes)):
+            B.moe_adamw(alone[0][i:i + 1], grads[i:i + 1], alone[1][i:i + 1], alone[2][i:i + 1], t, copies=alone[3][i:i + 1] if copy else None, rounding="random")
+        graph.replay()
+        torch.cuda.synchronize()
+        if t == 1:
+            B.moe_adamw(nearest[0], grads, nearest[1], nearest[2], t, copies=nearest[3])
+            assert all(torch.equal(a, b) for a, b in zip(together[0], nearest[0]))
+        for other in (alone, captured):
+            flat = lambda s: s[0] + [x for pair in s[1] + s[2] for x in pair] + (s[3] or [])  # noqa: E731
+            assert all(torch.equal(a, b) for a, b in zip(flat(together), flat(other))), t
+        grads[0].mul_(0.9)

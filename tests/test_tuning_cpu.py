@@ -275,3 +275,23 @@ def test_a_refused_gradient_is_no_step():
     with pytest.raises(B.MoeError, match="dense"):
         one.step()
     assert one.steps == 0
+
+
+def test_how_states_are_rounded(lib, on_host, monkeypatch):
+    """The binding asks for rounding by chance where it is wanted, and AdamW with states in 8 bits wants it."""
+    asked = []
+    monkeypatch.setattr(B, "load", lambda: type("Library", (), {"moe_adamw": staticmethod(lambda *args: asked.append(args[5]) or 0)}))
+    z, u8 = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt), torch.uint8  # noqa: E731
+    eight = lambda: [(z(40, u8), z(2, u8))]  # noqa: E731
+    for kw, states in ((dict(), eight), (dict(rounding="random"), eight), (dict(rounding="random"), lambda: [z(40)])):
+        B.moe_adamw([z(40)], [z(40)], states(), states(), 1, **kw)
+    with pytest.raises(B.MoeError, match="rounding"):
+        B.moe_adamw([z(40)], [z(40)], eight(), eight(), 1, rounding="up")
+    for bits in (8, 32):
+        p = z(40).requires_grad_()
+        p.grad = z(40)
+        AdamW([p], bits=bits).step()
+    assert asked == [8, 8 | B.MOE_ADAMW_RANDOM, 32, 8 | B.MOE_ADAMW_RANDOM, 32]
+    t = Tensor(*[0x1000] * 7, 64)
+    for bits in (32 | B.MOE_ADAMW_RANDOM, B.MOE_ADAMW_RANDOM, 9):
+        assert lib.moe_adamw(ctypes.byref(t), 1, F32, F32, -1, bits, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1.0, 1, None, None) == UNSUPPORTED
