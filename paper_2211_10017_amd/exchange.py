@@ -57,7 +57,8 @@ class _Combine(torch.autograd.Function):
         T, k = expert_scale.shape
         inv_perm = inv_perm.clone()                                         # (a layer routes the next batch into the same buffers, through pointers that torch does not see)
         active = None if active_rows is None else active_rows[:1].clone()
-        ctx.save_for_backward(y_perm, expert_scale, inv_perm, active)
+        # (the gate's scales are such a buffer too; where they carry a gradient they are the program's own, and stay in its graph)
+        ctx.save_for_backward(y_perm, expert_scale if ctx.needs_input_grad[1] else expert_scale.clone(), inv_perm, active)
         return B.moe_combine(y_perm, inv_perm, expert_scale, T, k, out_dtype=out_dtype, active_rows=active)
 
     @staticmethod
@@ -69,7 +70,7 @@ class _Combine(torch.autograd.Function):
 
 
 def combine_tokens(y_perm, inv_perm, expert_scale, active_rows=None, out_dtype=torch.float32):
-    """moe_combine with gradients for y_perm [T * k, d] and expert_scale fp32 [T, k].  The index may be written again before the backward pass; y_perm may not (torch raises; so it does
+    """moe_combine with gradients for y_perm [T * k, d] and expert_scale fp32 [T, k].  The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not (torch raises; so it does
     for a layer's own buffer, whose next call counts as a change)."""
     if not y_perm.is_contiguous() or not expert_scale.is_contiguous():
         y_perm, expert_scale = y_perm.contiguous(), expert_scale.contiguous()

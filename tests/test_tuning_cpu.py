@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from launches import P as PTR, record
-from paper_2211_10017_amd import AdamW, LowRankAdapters, adapt
+from paper_2211_10017_amd import AdamW, LowRankAdapters, adapt, combine_tokens
 from paper_2211_10017_amd import binding as B
 
 P, ODD = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1008)          # never dereferenced: validation fails first
@@ -295,3 +295,14 @@ def test_how_states_are_rounded(lib, on_host, monkeypatch):
     t = Tensor(*[0x1000] * 7, 64)
     for bits in (32 | B.MOE_ADAMW_RANDOM, B.MOE_ADAMW_RANDOM, 9):
         assert lib.moe_adamw(ctypes.byref(t), 1, F32, F32, -1, bits, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1.0, 1, None, None) == UNSUPPORTED
+
+
+def test_combine_keeps_scales_that_carry_no_gradient(on_host, monkeypatch):
+    """The scales that its backward pass uses are a copy (a layer's gate writes its own again through a pointer), the program's own where they learn."""
+    used = []
+    library = type("Library", (), {"moe_combine": staticmethod(lambda *args: 0), "moe_combine_backward": staticmethod(lambda *args: used.append(args[5]) or 0)})
+    monkeypatch.setattr(B, "load", lambda: library)
+    for learns in (False, True):
+        y, scale = torch.zeros(8, 64).requires_grad_(), torch.ones(4, 2).requires_grad_(learns)
+        combine_tokens(y, torch.arange(8, dtype=torch.int32), scale).sum().backward()
+        assert (used.pop() == scale.data_ptr()) == learns
