@@ -70,8 +70,8 @@ class _Combine(torch.autograd.Function):
 
 
 def combine_tokens(y_perm, inv_perm, expert_scale, active_rows=None, out_dtype=torch.float32):
-    """moe_combine with gradients for y_perm [T * k, d] and expert_scale fp32 [T, k].  The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not (torch raises; so it does
-    for a layer's own buffer, whose next call counts as a change)."""
+    """moe_combine with gradients for y_perm [T * k, d] and expert_scale fp32 [T, k].  The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not
+    (torch raises; so it does for a buffer of a layer, of either kind, whose next call counts as a change, but where that call is a replay of a captured graph)."""
     if not y_perm.is_contiguous() or not expert_scale.is_contiguous():
         y_perm, expert_scale = y_perm.contiguous(), expert_scale.contiguous()
     return _Combine.apply(y_perm, expert_scale, inv_perm, active_rows, out_dtype)

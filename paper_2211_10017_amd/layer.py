@@ -8,6 +8,11 @@ import torch
 from . import binding as B
 
 
+# Buffers that the calls of a plan write, through pointers: a graph that still needs the last call's values has to raise.
+_WRITTEN = {"moe_gate_topk": ("expert_idx", "expert_scale"), "moe_permute": ("perm_src", "inv_perm", "expert_offsets", "x_perm"),
+            "moe_grouped_ffn_wq": ("perm_src", "inv_perm", "expert_offsets", "y_perm", "out"), "moe_combine": ("out",)}
+
+
 class MoEExpertLayer:
     def __init__(self, T, d, F, E, k, bits, group_size=0, act_dtype=torch.float16, renormalize=True,
                  y_dtype=None, out_dtype=torch.float32, device="cuda:0", fuse_routing=True, activation="relu"):
@@ -93,6 +98,7 @@ class MoEExpertLayer:
                 rc = fn(*args)
                 if rc != 0:
                     B._check(rc, what)
+        torch.autograd.graph.increment_version([getattr(self, n) for n in _WRITTEN[name]])
 
     def gate(self, x, finished=None):
         self._step("moe_gate_topk", x, finished)
@@ -118,6 +124,7 @@ class MoEExpertLayer:
         rc = fn(*bare[1])
         if rc != 0:
             B._check(rc, what)
+        torch.autograd.graph.increment_version([self.perm_src, self.inv_perm, self.expert_offsets])
 
     def combine(self, x, finished=None):
         self._step("moe_combine", x, finished)       # nothing to do when fc2 stored the output itself
@@ -135,6 +142,8 @@ class MoEExpertLayer:
             rc = fn(*args)
             if rc != 0:
                 B._check(rc, name)
+        # (0.3 us of a call's 12 to 13 on the host)
+        torch.autograd.graph.increment_version([self.expert_idx, self.expert_scale, self.x_perm, self.perm_src, self.inv_perm, self.expert_offsets, self.y_perm, self.out])
         return self.out
 
     def _plan(self, x, finished):

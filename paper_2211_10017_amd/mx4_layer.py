@@ -51,6 +51,8 @@ class MoEMx4Layer:
             raise B.MoeError("finished must be a contiguous uint8 [T] CUDA tensor")
         B.moe_gate_topk(x, self.wg, self.gate_bias, self.k, self.renormalize, out=(self.expert_idx, self.expert_scale), finished=finished)
         B.moe_permute_index(self.expert_idx, self.E, self.d, x.dtype, self.perm_src, self.inv_perm, self.expert_offsets, self.ws_permute)
+        # (written through pointers, here and below: a backward pass that still needs the last call's values raises)
+        torch.autograd.graph.increment_version([self.expert_idx, self.expert_scale, self.perm_src, self.inv_perm, self.expert_offsets])
 
     def experts(self, x):
         """y of every assignment, [T * k, d], in the sorted order of the last route()."""
@@ -58,7 +60,6 @@ class MoEMx4Layer:
                               activation=self.activation, max_rows_per_expert=self.T, workspace=self.ws_ffn)
         if self.adapters is not None:
             self.adapters.add(x, self.y_perm, self.index(), by_assignment=False)
-        # (written through a pointer: a backward pass that still needs the last call's rows raises)
         torch.autograd.graph.increment_version(self.y_perm)
         return self.y_perm
 
@@ -69,5 +70,7 @@ class MoEMx4Layer:
     def forward(self, x, finished=None):
         self.route(x, finished)
         self.experts(x)
-        return B.moe_combine(self.y_perm, self.inv_perm, self.expert_scale, self.T, self.k, out=self.out, out_dtype=self.out.dtype,
-                             active_rows=self.expert_offsets[self.E:])
+        B.moe_combine(self.y_perm, self.inv_perm, self.expert_scale, self.T, self.k, out=self.out, out_dtype=self.out.dtype,
+                      active_rows=self.expert_offsets[self.E:])
+        torch.autograd.graph.increment_version(self.out)
+        return self.out

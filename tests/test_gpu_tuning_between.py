@@ -46,3 +46,32 @@ def test_the_scales_of_a_router_that_does_not_learn(kind):
     layer.forward(other)
     assert not torch.equal(scales, layer.expert_scale)
     assert all(torch.equal(a, b) for a, b in zip(grads(out), want))
+
+
+@pytest.mark.parametrize("kind", ["mx4", "int4"])
+def test_a_layers_next_call_counts_as_a_change(kind):
+    """What a graph keeps of a layer's buffers (rows, output, scales, the index) is not taken from the next call: the backward pass raises."""
+    gen = generator(2)
+    layer = a_layer(kind, gen)
+    x, other = r(gen, T, D).half(), r(gen, T, D).half()
+    weight, scale = r(gen, D).requires_grad_(), torch.rand((T, K), generator=gen, device="cuda").requires_grad_()
+    layer.forward(x)
+    rows = torch.zeros((T * K, 4), device="cuda", requires_grad=True)
+    uses = [lambda: combine_tokens(layer.y_perm, layer.inv_perm, scale, active_rows=layer.expert_offsets[E:]), lambda: layer.out * weight, lambda: layer.expert_scale * scale,
+            lambda: rows.index_select(0, layer.inv_perm), lambda: rows.index_select(0, layer.perm_src)]
+    for i, use in enumerate(uses):
+        out = use()
+        out.sum().backward()                                                # (nothing written in between)
+        out = use()
+        layer.forward(other)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.sum().backward()
+    # ... nor from one of its steps
+    steps = ([layer.gate, layer.permute, layer.ffn, layer.combine] if kind == "int4" else [layer.route, layer.route, layer.experts])
+    for step, use in zip(steps, [uses[2], uses[3], uses[0], uses[1]]):
+        out = use()
+        step(x)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.sum().backward()
+    with torch.inference_mode():
+        assert layer.forward(x) is layer.out
