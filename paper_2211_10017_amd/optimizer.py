@@ -10,7 +10,7 @@ _HALVES = (torch.float16, torch.bfloat16)
 
 class AdamW:
     """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass.  step() takes the gradients that are there; a parameter
-    without one stays as it is.  States in 8 bits are rounded up or down by chance, the same in every run: to the nearest number they could not follow their averages."""
+    without one stays as it is, and its steps are counted from its own first one on (`counts`).  States in 8 bits are rounded up or down by chance, the same in every run: to the nearest number they could not follow their averages."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, bits=32):
         self.params = list(params)
@@ -20,7 +20,8 @@ class AdamW:
             raise B.MoeError("parameters must be contiguous tensors of fp16, bf16 or fp32")
         if len({p.data_ptr() for p in self.params if p.numel()}) < sum(p.numel() > 0 for p in self.params):
             raise B.MoeError("a parameter is in the list twice")
-        self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.steps = lr, tuple(betas), eps, weight_decay, bits, 0
+        self.lr, self.betas, self.eps, self.weight_decay, self.bits = lr, tuple(betas), eps, weight_decay, bits
+        self.counts = [0] * len(self.params)                # steps that each parameter has taken: its moments begin at 0, whenever that is
         self.masters = [p.detach().float() if p.dtype in _HALVES else None for p in self.params]
 
         def state(p):
@@ -30,20 +31,26 @@ class AdamW:
 
         self.exp_avg, self.exp_avg_sq = ([state(p) for p in self.params] for _ in range(2))
 
+    @property
+    def steps(self):
+        """The most steps that a parameter has taken."""
+        return max(self.counts)
+
     def step(self, grad_scale: float = 1.0):
         groups = {}
         for i, p in enumerate(self.params):
             if p.grad is not None:
                 if p.grad.is_sparse:
                     raise B.MoeError("gradients must be dense")
-                groups.setdefault((p.dtype if self.masters[i] is not None else None, p.grad.dtype), []).append(i)
-        self.steps += 1                                     # (a refused gradient is no step)
-        for (half, _), at in groups.items():
+                groups.setdefault((p.dtype if self.masters[i] is not None else None, p.grad.dtype, self.counts[i] + 1), []).append(i)
+        for (half, _, number), at in groups.items():
             params = [self.params[i].detach() for i in at]
             B.moe_adamw([self.masters[i] for i in at] if half else params, [self.params[i].grad.contiguous() for i in at], [self.exp_avg[i] for i in at], [self.exp_avg_sq[i] for i in at],
-                        self.steps, self.lr, self.betas, self.eps, self.weight_decay, grad_scale, copies=params if half else None, rounding="random")
+                        number, self.lr, self.betas, self.eps, self.weight_decay, grad_scale, copies=params if half else None, rounding="random")
             # (written through pointers: a backward pass that still needs the old values raises)
             torch.autograd.graph.increment_version(params)
+            for i in at:
+                self.counts[i] = number
 
     def zero_grad(self, set_to_none: bool = True):
         for p in self.params:
@@ -54,15 +61,16 @@ class AdamW:
                     p.grad.zero_()
 
     def state_dict(self):
-        return dict(steps=self.steps, bits=self.bits, masters=self.masters, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq)
+        return dict(steps=list(self.counts), bits=self.bits, masters=self.masters, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq)
 
     def load_state_dict(self, state):
         if state["bits"] != self.bits or len(state["exp_avg"]) != len(self.params):
             raise B.MoeError("the state belongs to other parameters, or has other bits")
         flat = lambda s: [t for x in s for t in (x if isinstance(x, tuple) else (x,)) if t is not None]  # noqa: E731
         mine, theirs = (flat(s["masters"]) + flat(s["exp_avg"]) + flat(s["exp_avg_sq"]) for s in (self.state_dict(), state))
-        if [t.shape for t in mine] != [t.shape for t in theirs]:
+        steps = [state["steps"]] * len(self.params) if isinstance(state["steps"], int) else list(state["steps"])      # (one number: a state of one count for all)
+        if len(steps) != len(self.params) or [t.shape for t in mine] != [t.shape for t in theirs]:
             raise B.MoeError("the state belongs to other parameters")
         for m, t in zip(mine, theirs):
             m.copy_(t)
-        self.steps = state["steps"]
+        self.counts = steps

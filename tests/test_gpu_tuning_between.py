@@ -75,3 +75,25 @@ def test_a_layers_next_call_counts_as_a_change(kind):
             out.sum().backward()
     with torch.inference_mode():
         assert layer.forward(x) is layer.out
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_parameter_that_learns_later(bits):
+    """Its first gradients come after many steps of the others: the steps are the formula's from t = 1 on."""
+    gen, lr = generator(3), 0.01
+    early, late = (r(gen, 1000).requires_grad_() for _ in range(2))
+    optimiser = AdamW([early, late], lr=lr, betas=(0.9, 0.999), weight_decay=0.0, bits=bits)
+    for _ in range(100):
+        early.grad = r(gen, 1000)
+        optimiser.step()
+    m, v = torch.zeros(1000, dtype=torch.float64, device="cuda"), torch.zeros(1000, dtype=torch.float64, device="cuda")
+    for t in (1, 2):
+        early.grad, late.grad = r(gen, 1000), r(gen, 1000)
+        g, old = late.grad.double(), late.detach().double()
+        m, v = 0.9 * m + 0.1 * g, 0.999 * v + 0.001 * g * g
+        optimiser.step()
+        want = old - lr / (1 - 0.9 ** t) * m / ((v / (1 - 0.999 ** t)).sqrt() + 1e-8)
+        # 32 roundings of a step of up to (t = 2) 1.5 rates, and one of the value
+        assert bool(((late.detach().double() - want).abs() <= 32 * 2.0 ** -24 * 1.5 * lr + 2.0 ** -24 * (old.abs() + 1.5 * lr)).all()), t
+        if bits == 8:
+            break                                                           # (the second step's moments have been rounded)

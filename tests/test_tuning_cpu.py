@@ -306,3 +306,34 @@ def test_combine_keeps_scales_that_carry_no_gradient(on_host, monkeypatch):
         y, scale = torch.zeros(8, 64).requires_grad_(), torch.ones(4, 2).requires_grad_(learns)
         combine_tokens(y, torch.arange(8, dtype=torch.int32), scale).sum().backward()
         assert (used.pop() == scale.data_ptr()) == learns
+
+
+def _steps_asked(monkeypatch):
+    """The parameters (their number) and the step's number of each call of the library."""
+    asked = []
+    monkeypatch.setattr(B, "load", lambda: type("Library", (), {"moe_adamw": staticmethod(lambda *args: asked.append((args[1], args[12])) or 0)}))
+    return asked
+
+
+def test_a_parameters_steps_are_its_own(on_host, monkeypatch):
+    asked = _steps_asked(monkeypatch)
+    early, late, never = (torch.zeros(4, requires_grad=True) for _ in range(3))
+    one = AdamW([early, late, never])
+    one.step()                                                              # (no gradient anywhere: no step)
+    assert asked == [] and one.steps == 0
+    early.grad = torch.zeros(4)
+    one.step(), one.step()
+    late.grad = torch.zeros(4)
+    one.step()
+    early.grad = None
+    one.step()
+    assert asked == [(1, 1), (1, 2), (1, 3), (1, 1), (1, 2)] and one.counts == [3, 2, 0] and one.steps == 3
+    other = AdamW([torch.zeros(4) for _ in range(3)])
+    other.load_state_dict(one.state_dict())
+    one.step()
+    assert other.counts == [3, 2, 0]
+    other.load_state_dict(dict(one.state_dict(), steps=7))                  # a state with one count for all
+    assert other.counts == [7, 7, 7]
+    with pytest.raises(B.MoeError):
+        other.load_state_dict(dict(one.state_dict(), steps=[1, 2]))
+    assert other.counts == [7, 7, 7]
