@@ -477,6 +477,7 @@ int moe_adapters_backward(const void *dy, int dy_dtype, int64_t dy_stride, const
  *   by less than half the distance of two codes stays where it is, sqrt(v) for good at the usual beta2, and steps become several times too large.
  *   tensors: HOST array (read before the call returns); its pointers are device pointers, aligned for their types (16-byte alignment is the fast way).  No two tensors overlap.
  *   step_ptr: t on the device instead of `step` (a captured step then counts on; numbers below 1 count as 1), or NULL.
+ * moe_adamw_check: what moe_adamw would refuse, without a step (where several calls are one step: none of them is made if one would be refused).
  * moe_adamw_state: the values of n codes, [n] in out_dtype.
  */
 typedef struct {
@@ -490,6 +491,8 @@ typedef struct {
 enum { MOE_ADAMW_RANDOM = 256 };
 int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2,
               double eps, double weight_decay, double grad_scale, int step, const int32_t *step_ptr, void *stream);
+int moe_adamw_check(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2,
+                    double eps, double weight_decay, double grad_scale, int step, const int32_t *step_ptr);
 int moe_adamw_state(const void *codes, const void *scales, int64_t n, void *out, int out_dtype, void *stream);
 
 #ifdef __cplusplus

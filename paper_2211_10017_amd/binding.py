@@ -33,7 +33,7 @@ EXPORTS = ["moe_last_error", "moe_last_ffn_kernels", "moe_device_info", "moe_abi
            "moe_grouped_ffn_mx4_workspace_bytes", "moe_grouped_ffn_mx4",
            "moe_balance_loss_workspace_bytes", "moe_balance_loss", "moe_balance_loss_backward",
            "moe_combine_backward", "moe_permute_backward", "moe_adapters", "moe_adapters_backward_workspace_bytes", "moe_adapters_backward",
-           "moe_adamw", "moe_adamw_state"]
+           "moe_adamw", "moe_adamw_check", "moe_adamw_state"]
 
 LAYER_MAX_EXPERTS = 256   # experts of a whole layer call: moe_gate_topk's limit (moe_permute: 1024, the FFN: 4096)
 
@@ -147,6 +147,8 @@ def load():
     d = ctypes.c_double
     lib.moe_adamw.restype = i
     lib.moe_adamw.argtypes = [vp, i, i, i, i, i, d, d, d, d, d, d, i, vp, vp]
+    lib.moe_adamw_check.restype = i
+    lib.moe_adamw_check.argtypes = lib.moe_adamw.argtypes[:-1]
     lib.moe_adamw_state.restype = i
     lib.moe_adamw_state.argtypes = [vp, vp, i64, vp, i, vp]
     _lib = lib
@@ -816,18 +818,13 @@ def _pairs(states):
     return [s[0] for s in states], [s[1] for s in states]
 
 
-def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, copies=None,
-              rounding: str = "nearest"):
-    """An AdamW step over lists of tensors, in place (include/moe_wq.h).
-
-    params of one type, grads of one type.  exp_avg and exp_avg_sq: fp32 tensors, or pairs (codes uint8 [n], scales uint8 [ceil(n/32)]) for states in 8 bits, of the moment and
-    of the second one's root.  step: the step's number from 1 on, or an int32 CUDA tensor that holds it.  copies: 16-bit copies of fp32 params to be written as well.
-    rounding of states in 8 bits: "nearest", which is one step's best but over many steps keeps the second moment from falling, or "random", whose mean is the value: a program's steps take it."""
+def adamw_arguments(params, grads, exp_avg, exp_avg_sq, step, lr, betas, eps, weight_decay, grad_scale, copies, rounding):
+    """moe_adamw's checks: the library's arguments, and what they point to (to be kept until the call); None for empty lists."""
     count = len(params)
     if not count == len(grads) == len(exp_avg) == len(exp_avg_sq) or (copies is not None and len(copies) != count):
         raise MoeError("params, grads, exp_avg, exp_avg_sq and copies must be lists of one length")
     if not count:
-        return
+        return None
     bits = 8 if isinstance(exp_avg[0], (tuple, list)) else 32
     if rounding not in ("nearest", "random"):
         raise MoeError("rounding is nearest or random, not %r" % (rounding,))
@@ -873,9 +870,20 @@ def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=
         if step.numel() != 1:
             raise MoeError("step must be one number")
         _check_device(step)
-    rc = load().moe_adamw(table.buffer_info()[0], count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits | (MOE_ADAMW_RANDOM if bits == 8 and rounding == "random" else 0), lr, betas[0], betas[1], eps, weight_decay, grad_scale,
-                          1 if on_device else step, _ptr(step, torch.int32, "step") if on_device else None, _stream())
-    _check(rc, "moe_adamw")
+    return (table.buffer_info()[0], count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits | (MOE_ADAMW_RANDOM if bits == 8 and rounding == "random" else 0), lr, betas[0], betas[1],
+            eps, weight_decay, grad_scale, 1 if on_device else step, _ptr(step, torch.int32, "step") if on_device else None), (table, buffers)
+
+
+def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, copies=None,
+              rounding: str = "nearest"):
+    """An AdamW step over lists of tensors, in place (include/moe_wq.h).
+
+    params of one type, grads of one type.  exp_avg and exp_avg_sq: fp32 tensors, or pairs (codes uint8 [n], scales uint8 [ceil(n/32)]) for states in 8 bits, of the moment and
+    of the second one's root.  step: the step's number from 1 on, or an int32 CUDA tensor that holds it.  copies: 16-bit copies of fp32 params to be written as well.
+    rounding of states in 8 bits: "nearest", which is one step's best but over many steps keeps the second moment from falling, or "random", whose mean is the value: a program's steps take it."""
+    call = adamw_arguments(params, grads, exp_avg, exp_avg_sq, step, lr, betas, eps, weight_decay, grad_scale, copies, rounding)
+    if call is not None:
+        _check(load().moe_adamw(*call[0], _stream()), "moe_adamw")
 
 
 def moe_adamw_state(codes, scales, dtype=torch.float32, out=None):

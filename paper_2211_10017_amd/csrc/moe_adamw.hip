@@ -264,12 +264,10 @@ __global__ __launch_bounds__(256) void adamw_state_kernel(const uint8_t *codes, 
 
 static bool aligned(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
-}  // namespace moe
-
-extern "C" int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2,
-                         double eps, double weight_decay, double grad_scale, int step, const int32_t *step_ptr, void *stream)
+// What a step takes; wide: every buffer is aligned for whole loads.
+static int check_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2, double eps,
+                       double weight_decay, double grad_scale, int step, const int32_t *step_ptr, bool *wide_out)
 {
-    using namespace moe;
     const char *what = "moe_adamw";
     if (count < 0 || (count > 0 && !tensors)) return fail(MOE_ERR_INVALID_ARG, "%s: no tensors", what);
     if (!known_dtype(p_dtype) || !known_dtype(g_dtype) || (copy_dtype != -1 && copy_dtype != MOE_F16 && copy_dtype != MOE_BF16)) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
@@ -293,6 +291,26 @@ extern "C" int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype
         wide = wide && aligned(t.p, 4 * size_of(p_dtype)) && aligned(t.g, 4 * size_of(g_dtype)) && aligned(t.m, 4 * state) && aligned(t.v, 4 * state)
             && (copy_dtype == -1 || aligned(t.copy, 8));
     }
+    *wide_out = wide;
+    return MOE_OK;
+}
+
+}  // namespace moe
+
+extern "C" int moe_adamw_check(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2, double eps,
+                               double weight_decay, double grad_scale, int step, const int32_t *step_ptr)
+{
+    bool wide;
+    return moe::check_adamw(tensors, count, p_dtype, g_dtype, copy_dtype, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, step, step_ptr, &wide);
+}
+
+extern "C" int moe_adamw(const moe_adamw_tensor *tensors, int count, int p_dtype, int g_dtype, int copy_dtype, int state_bits, double lr, double beta1, double beta2,
+                         double eps, double weight_decay, double grad_scale, int step, const int32_t *step_ptr, void *stream)
+{
+    using namespace moe;
+    const char *what = "moe_adamw";
+    bool wide;
+    if (const int rc = check_adamw(tensors, count, p_dtype, g_dtype, copy_dtype, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, step, step_ptr, &wide)) return rc;
     AdamTensors a;
     a.b1 = (float)beta1, a.b2 = (float)beta2, a.c1 = (float)(1.0 - beta1), a.c2 = (float)(1.0 - beta2), a.eps = (float)eps;
     a.decay = (float)(1.0 - lr * weight_decay), a.grad_scale = (float)grad_scale;

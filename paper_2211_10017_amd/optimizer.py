@@ -43,10 +43,18 @@ class AdamW:
                 if p.grad.is_sparse:
                     raise B.MoeError("gradients must be dense")
                 groups.setdefault((p.dtype if self.masters[i] is not None else None, p.grad.dtype, self.counts[i] + 1), []).append(i)
+        lib, calls = B.load(), []
         for (half, _, number), at in groups.items():
             params = [self.params[i].detach() for i in at]
-            B.moe_adamw([self.masters[i] for i in at] if half else params, [self.params[i].grad.contiguous() for i in at], [self.exp_avg[i] for i in at], [self.exp_avg_sq[i] for i in at],
-                        number, self.lr, self.betas, self.eps, self.weight_decay, grad_scale, copies=params if half else None, rounding="random")
+            calls.append((at, number, params, *B.adamw_arguments([self.masters[i] for i in at] if half else params, [self.params[i].grad.contiguous() for i in at], [self.exp_avg[i] for i in at],
+                                                                 [self.exp_avg_sq[i] for i in at], number, self.lr, self.betas, self.eps, self.weight_decay, grad_scale,
+                                                                 params if half else None, "random")))
+        # (a refusal leaves everything as it was, so all calls are checked before the first is made; one alone is by itself)
+        if len(calls) > 1:
+            for call in calls:
+                B._check(lib.moe_adamw_check(*call[3]), "moe_adamw")
+        for at, number, params, arguments, _ in calls:
+            B._check(lib.moe_adamw(*arguments, B._stream()), "moe_adamw")
             # (written through pointers: a backward pass that still needs the old values raises)
             torch.autograd.graph.increment_version(params)
             for i in at:

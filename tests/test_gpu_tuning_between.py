@@ -97,3 +97,23 @@ def test_a_parameter_that_learns_later(bits):
         assert bool(((late.detach().double() - want).abs() <= 32 * 2.0 ** -24 * 1.5 * lr + 2.0 ** -24 * (old.abs() + 1.5 * lr)).all()), t
         if bits == 8:
             break                                                           # (the second step's moments have been rounded)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_refused_step_leaves_every_parameter(bits):
+    """A parameter elsewhere, in the last of the groups: the first ones are as they were, and so are their states, and the step after it is the first."""
+    gen = generator(5)
+    a, b = r(gen, 500).requires_grad_(), r(gen, 64).half().requires_grad_()
+    elsewhere = torch.zeros(64, dtype=BF16, requires_grad=True)
+    optimiser = AdamW([a, b, elsewhere], lr=0.1, weight_decay=0.0, bits=bits)
+    for p in (a, b, elsewhere):
+        p.grad = torch.ones_like(p)
+    flat = lambda: [t for s in optimiser.exp_avg + optimiser.exp_avg_sq for t in (s if bits == 8 else (s,))] + [a.detach(), b.detach(), optimiser.masters[1]]  # noqa: E731
+    before, versions = [t.clone() for t in flat()], (a._version, b._version)
+    with pytest.raises(B.MoeError, match="device"):
+        optimiser.step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(flat(), before)) and versions == (a._version, b._version) and optimiser.counts == [0, 0, 0]
+    elsewhere.grad = None
+    optimiser.step()
+    assert optimiser.counts == [1, 1, 0] and bool((((a.detach() - before[-3]) + 0.1).abs() <= 1e-6).all())

@@ -311,7 +311,7 @@ def test_combine_keeps_scales_that_carry_no_gradient(on_host, monkeypatch):
 def _steps_asked(monkeypatch):
     """The parameters (their number) and the step's number of each call of the library."""
     asked = []
-    monkeypatch.setattr(B, "load", lambda: type("Library", (), {"moe_adamw": staticmethod(lambda *args: asked.append((args[1], args[12])) or 0)}))
+    monkeypatch.setattr(B, "load", lambda: type("Library", (), {"moe_adamw": staticmethod(lambda *args: asked.append((args[1], args[12])) or 0), "moe_adamw_check": lambda *_: 0})())
     return asked
 
 
@@ -337,3 +337,38 @@ def test_a_parameters_steps_are_its_own(on_host, monkeypatch):
     with pytest.raises(B.MoeError):
         other.load_state_dict(dict(one.state_dict(), steps=[1, 2]))
     assert other.counts == [7, 7, 7]
+
+
+def test_a_refused_step_changes_nothing(lib, on_host, monkeypatch):
+    """Whatever refuses it, in the first group of parameters or the last: no call is made, no step counted, no version moved; the next step is the first."""
+    asked = []
+    library = type("Library", (), {"moe_adamw": staticmethod(lambda *args: asked.append(args[12]) or lib.moe_adamw_check(*args[:-1])), "moe_adamw_check": lib.moe_adamw_check,
+                                   "moe_last_error": lib.moe_last_error})
+    monkeypatch.setattr(B, "load", lambda: library)
+    for halves in (False, True):
+        params = [torch.zeros(4, requires_grad=True)] + [torch.zeros(4, dtype=torch.float16, requires_grad=True)] * halves
+        one = AdamW(params)
+
+        def refused(match, grad_scale=1.0):
+            before = one.counts, [p._version for p in params]
+            with pytest.raises(B.MoeError, match=match):
+                one.step(grad_scale)
+            assert (asked == [] or not halves) and one.steps == 0 and before == (one.counts, [p._version for p in params])
+            asked.clear()
+
+        for p in params:
+            p.grad = torch.zeros_like(p)
+        for scale in (float("inf"), float("nan")):
+            refused("finite", scale)
+        one.eps = -1.0
+        refused("eps")
+        one.eps = 1e-8
+        state = one.exp_avg_sq[-1]
+        one.exp_avg_sq[-1] = torch.zeros(5)
+        refused("moment")
+        one.exp_avg_sq[-1] = torch.frombuffer(bytearray(20), dtype=torch.uint8)[1:17].view(torch.uint8)
+        refused("moment")
+        one.exp_avg_sq[-1] = state
+        one.step()
+        assert one.counts == [1] * len(params) and asked == [1] * len(params)
+        asked.clear()
