@@ -37,6 +37,8 @@ class AdamW:
         return max(self.counts)
 
     def step(self, grad_scale: float = 1.0):
+        if self.params[0].device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            raise B.MoeError("a captured step would have the same number in every replay: capture moe_adamw, with the step's number on the device")
         groups = {}
         for i, p in enumerate(self.params):
             if p.grad is not None:

@@ -117,3 +117,23 @@ def test_a_refused_step_leaves_every_parameter(bits):
     elsewhere.grad = None
     optimiser.step()
     assert optimiser.counts == [1, 1, 0] and bool((((a.detach() - before[-3]) + 0.1).abs() <= 1e-6).all())
+
+
+def test_a_captured_step_of_the_class_is_refused():
+    """Its number is the host's: each replay would take the captured one again.  (moe_adamw takes it from the device.)"""
+    p = torch.zeros(64, device="cuda", requires_grad=True)
+    p.grad = torch.ones(64, device="cuda")
+    optimiser = AdamW([p], lr=0.1, weight_decay=0.0)
+    done = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        done.add_(1)
+        with pytest.raises(B.MoeError, match="captured"):
+            optimiser.step()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert float(done) == 3 and bool((p == 0).all()) and optimiser.steps == 0
+    optimiser.step()
+    assert bool(((p + 0.1).abs() <= 1e-6).all()) and optimiser.steps == 1
