@@ -8,8 +8,13 @@ from . import binding as B
 _HALVES = (torch.float16, torch.bfloat16)
 
 
+def _version(p):
+    return -1 if p.is_inference() else p._version           # (inference tensors have none)
+
+
 class AdamW:
-    """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass.  step() takes the gradients that are there; a parameter
+    """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass; what
+    others write into one between two steps (not through .data, which torch does not count) goes into its master.  step() takes the gradients that are there; a parameter
     without one stays as it is, and its steps are counted from its own first one on (`counts`).  States in 8 bits are rounded up or down by chance, the same in every run: to the nearest number they could not follow their averages."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, bits=32):
@@ -23,6 +28,7 @@ class AdamW:
         self.lr, self.betas, self.eps, self.weight_decay, self.bits = lr, tuple(betas), eps, weight_decay, bits
         self.counts = [0] * len(self.params)                # steps that each parameter has taken: its moments begin at 0, whenever that is
         self.masters = [p.detach().float() if p.dtype in _HALVES else None for p in self.params]
+        self._seen = [_version(p) for p in self.params]     # as the masters know them
 
         def state(p):
             if bits == 32:
@@ -56,11 +62,19 @@ class AdamW:
             for call in calls:
                 B._check(lib.moe_adamw_check(*call[3]), "moe_adamw")
         for at, number, params, arguments, _ in calls:
+            for i in at:
+                if self.masters[i] is not None and _version(self.params[i]) != self._seen[i]:
+                    self._take_over(i)
             B._check(lib.moe_adamw(*arguments, B._stream()), "moe_adamw")
             # (written through pointers: a backward pass that still needs the old values raises)
             torch.autograd.graph.increment_version(params)
             for i in at:
-                self.counts[i] = number
+                self.counts[i], self._seen[i] = number, _version(self.params[i])
+
+    def _take_over(self, i):
+        """A parameter's new values into its master; where the parameter is still the master's rounding, the master stays."""
+        master, p = self.masters[i], self.params[i].detach()
+        master.copy_(torch.where(master.to(p.dtype) == p, master, p.float()))
 
     def zero_grad(self, set_to_none: bool = True):
         for p in self.params:

@@ -137,3 +137,21 @@ def test_a_captured_step_of_the_class_is_refused():
     assert float(done) == 3 and bool((p == 0).all()) and optimiser.steps == 0
     optimiser.step()
     assert bool(((p + 0.1).abs() <= 1e-6).all()) and optimiser.steps == 1
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_parameters_that_are_written_between_steps(dtype):
+    """The next step goes on from what was written, and elsewhere from the master's bits."""
+    gen = generator(6)
+    p, q = (r(generator(7), 1000).to(dtype).requires_grad_() for _ in range(2))
+    ours, theirs = (AdamW([t], lr=0.01, weight_decay=0.0) for t in (p, q))
+    for t in range(4):
+        p.grad = r(gen, 1000).to(dtype)
+        q.grad = p.grad.clone()
+        ours.step(), theirs.step()
+        if t == 1:
+            with torch.no_grad():
+                p[:100] = 0.5
+                theirs.masters[0][:100] = 0.5
+    assert torch.equal(ours.masters[0], theirs.masters[0]) and torch.equal(p, q) and bool(((p[:100] - 0.5).abs() < 0.03).all())
+    assert not torch.equal(ours.masters[0], p.detach().float())

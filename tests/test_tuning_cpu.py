@@ -372,3 +372,26 @@ def test_a_refused_step_changes_nothing(lib, on_host, monkeypatch):
         one.step()
         assert one.counts == [1] * len(params) and asked == [1] * len(params)
         asked.clear()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_what_others_write_into_a_parameter_goes_into_its_master(on_host, dtype):
+    p = torch.tensor([1.0, 2.0, 3.0, float("nan")]).to(dtype).requires_grad_()
+    p.grad = torch.zeros_like(p)
+    one = AdamW([p])
+    with torch.no_grad():
+        one.masters[0][:2] += 2.0 ** -14                                    # (what 16 bits do not show)
+        one.step()
+        assert one.masters[0][:3].tolist() == [1.0 + 2.0 ** -14, 2.0 + 2.0 ** -14, 3.0]
+        p[1] = -5.0
+        p.clamp_(max=2.5)
+        one.step()
+    assert one.masters[0][:3].tolist() == [1.0 + 2.0 ** -14, -5.0, 2.5] and bool(one.masters[0][3].isnan())
+    with torch.no_grad():                                                   # a state, and then the parameters that belong to it: the state's masters stay
+        other = torch.zeros(4, dtype=dtype)
+        two = AdamW([other])
+        two.load_state_dict(one.state_dict())
+        other.grad = torch.zeros_like(other)
+        other.copy_(p)
+        two.step()
+    assert two.masters[0][:3].tolist() == one.masters[0][:3].tolist()
