@@ -6,7 +6,7 @@ from collections import namedtuple
 import torch
 
 from . import binding as B
-from .exchange import gradient
+from .exchange import gradient, whole
 
 # The sorted index of rows by adapter (moe_permute): k rows per token.
 AdapterIndex = namedtuple("AdapterIndex", "perm_src inv_perm offsets k")
@@ -47,7 +47,7 @@ class _Adapt(torch.autograd.Function):
 
         dx = da = db = None
         if need_x or need_a or need_b:
-            rows = dout if dout.stride(-1) == 1 and dout.stride(0) % 8 == 0 and dout.stride(0) >= dout.shape[1] and dout.data_ptr() % 16 == 0 else dout.contiguous()
+            rows = dout if dout.stride(-1) == 1 and dout.stride(0) % 8 == 0 and dout.stride(0) >= dout.shape[1] and dout.data_ptr() % 16 == 0 else whole(dout)
             dx, da, db = gradient(call, "adapt", rows, x, a, b)
         return dx, dout if need_y else None, da, db, None, None, None, None
 

@@ -24,6 +24,12 @@ def gradient(call, name, *tensors):
     return Once.apply(call, name, *tensors) if torch.is_grad_enabled() else call(*tensors)
 
 
+def whole(t):
+    """A gradient as the library reads it: contiguous, on 16 bytes.  (torch may hand over a part of a larger one, contiguous wherever it begins.)"""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 class _Permute(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, expert_idx, E):
@@ -43,7 +49,7 @@ class _Permute(torch.autograd.Function):
     def backward(ctx, dx_perm, *_):
         inv_perm, active = ctx.saved_tensors
         call = lambda g: B.moe_permute_backward(g, inv_perm, *ctx.sizes, active_rows=active)  # noqa: E731
-        return gradient(call, "permute_tokens", dx_perm.contiguous()), None, None
+        return gradient(call, "permute_tokens", whole(dx_perm)), None, None
 
 
 def permute_tokens(x, expert_idx, E: int):
@@ -66,7 +72,7 @@ class _Combine(torch.autograd.Function):
         y_perm, expert_scale, inv_perm, active = ctx.saved_tensors
         need = ctx.needs_input_grad[:2]
         call = lambda g, y, s: B.moe_combine_backward(g, y, inv_perm, s, active_rows=active, need=need)  # noqa: E731
-        return (*gradient(call, "combine_tokens", dout.contiguous(), y_perm, expert_scale), None, None, None)
+        return (*gradient(call, "combine_tokens", whole(dout), y_perm, expert_scale), None, None, None)
 
 
 def combine_tokens(y_perm, inv_perm, expert_scale, active_rows=None, out_dtype=torch.float32):

@@ -155,3 +155,37 @@ def test_parameters_that_are_written_between_steps(dtype):
                 theirs.masters[0][:100] = 0.5
     assert torch.equal(ours.masters[0], theirs.masters[0]) and torch.equal(p, q) and bool(((p[:100] - 0.5).abs() < 0.03).all())
     assert not torch.equal(ours.masters[0], p.detach().float())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("name", ["combine", "permute", "adapt"])
+def test_gradients_that_begin_anywhere(name, dtype):
+    """A gradient that is a part of a larger one is contiguous but does not begin on 16 bytes; others are transposed, expanded, or every second column."""
+    gen = generator(8)
+    perm, inv, offsets = sorted_index(routing(gen, T, K, E, "pruned"), E)
+    idx = routing(generator(9), T, K, E, "pruned")
+    if name == "combine":
+        leaf, scale = r(gen, T * K, 72), torch.rand((T, K), generator=gen, device="cuda")
+        call = lambda x: combine_tokens(x, inv, scale, active_rows=offsets[E:], out_dtype=dtype)  # noqa: E731
+    elif name == "permute":
+        leaf = r(gen, T, 72).to(dtype)
+        call = lambda x: permute_tokens(x, idx, E)[0]  # noqa: E731
+    else:
+        x, b = r(gen, T, 64).half(), r(gen, E, 4, 72).half()
+        leaf = r(gen, E, 4, 64).half()
+        call = lambda a: adapt(x, None, a, b, AdapterIndex(perm, inv, offsets, K), y_dtype=dtype)  # noqa: E731
+
+    def grad(use):
+        mine = leaf.clone().requires_grad_()
+        use(call(mine)).backward()
+        return mine.grad
+
+    w = r(gen, 1 + call(leaf).numel()).to(dtype)
+    shape = call(leaf).shape
+    plain = grad(lambda out: (out * w[1:].view(shape)).sum())
+    one = torch.ones(1, dtype=dtype, device="cuda", requires_grad=True)
+    assert torch.equal(grad(lambda out: (torch.cat([one, out.flatten()]) * w).sum()), plain)
+    tr = w[1:].view(shape).t().contiguous()
+    assert torch.equal(grad(lambda out: (out.t() * tr).sum()), plain)
+    assert torch.equal(grad(lambda out: (torch.stack([out, out], 2)[:, :, 0] * w[1:].view(shape)).sum()), plain)
+    assert torch.equal(grad(lambda out: out.sum()), grad(lambda out: (out * torch.ones_like(out)).sum()))

@@ -395,3 +395,13 @@ def test_what_others_write_into_a_parameter_goes_into_its_master(on_host, dtype)
         other.copy_(p)
         two.step()
     assert two.masters[0][:3].tolist() == one.masters[0][:3].tolist()
+
+
+def test_gradients_that_begin_between_16_bytes_are_copied():
+    from paper_2211_10017_amd.exchange import whole
+    room = torch.arange(200.0).half()
+    at = next(i for i in range(8) if room[i:].data_ptr() % 16)
+    part = room[at:at + 64].view(8, 8)
+    assert part.is_contiguous() and whole(part).data_ptr() % 16 == 0 and torch.equal(whole(part), part)
+    aligned = torch.zeros(8, 8)
+    assert whole(aligned).data_ptr() == aligned.data_ptr() and whole(aligned.t()).is_contiguous()
