@@ -453,7 +453,7 @@ int moe_permute_backward(const void *dx_perm, int perm_dtype, const int32_t *inv
  *   da[e] = sum_r u[r] x[t]^T,  db[e] = scale[e] * sum_r v[r] dy[r]^T  in grad_dtype, 0 for adapters without rows; sums over rows in a fixed order
  *   dx, da, db may each be NULL (x is read for da only, v for db only).  Workspace of moe_adapters_backward_workspace_bytes; calls that overlap in time need one each.
  * But for y == out nothing that is written overlaps anything else of the call (out == x, dx == dy and dx == x are refused).
- * Products are summed in fp32, v and u kept in it.  Strides and K, N are multiples of 8, K and N at most 2^20, 1 <= rank <= 128, E <= 4096.  expert_offsets and
+ * Products are summed in fp32, v and u kept in it.  Strides and K, N are multiples of 8, K and N at most 2^20, 1 <= rank <= 128, E <= 4096, R <= 2^30.  expert_offsets and
  * perm_src are forced into range: wrong contents give wrong results but no stray access.
  */
 int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k, const int32_t *expert_offsets, int R, int E, int K, int N, int rank,

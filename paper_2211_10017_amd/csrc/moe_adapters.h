@@ -6,6 +6,7 @@
 namespace moe {
 
 constexpr int kAdapterMostRank = 128, kAdapterMostAdapters = 4096;
+constexpr int kAdapterMostRows = 1 << 30;           // a row's number and the steps that are requested ahead of it (two of 32 rows, or the next part's) stay below 2^31
 constexpr int kAdapterRowsWithoutV = 512;           // more rows take two launches, between which the coefficients are in memory
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));

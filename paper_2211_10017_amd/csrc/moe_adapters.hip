@@ -25,6 +25,7 @@ static int check_adapters(const AdapterCall &c)
     if (c.rank > kAdapterMostRank) return fail(MOE_ERR_UNSUPPORTED, "%s: rank %d above %d", what, c.rank, kAdapterMostRank);
     if (c.E > kAdapterMostAdapters) return fail(MOE_ERR_UNSUPPORTED, "%s: %d adapters, above %d", what, c.E, kAdapterMostAdapters);
     if (c.K > 1 << 20 || c.N > 1 << 20) return fail(MOE_ERR_UNSUPPORTED, "%s: K and N of at most 2^20", what);
+    if (c.R > kAdapterMostRows) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows, above %d", what, c.R, kAdapterMostRows);
     if (c.dtype != MOE_F16 && c.dtype != MOE_BF16) return fail(MOE_ERR_UNSUPPORTED, "%s: x and the adapters must be fp16 or bf16", what);
     if (!known_dtype(c.other_dtype)) return fail(MOE_ERR_UNSUPPORTED, "%s: unknown dtype", what);
     if (c.R > 0 && !c.perm_src && c.by_assignment) return fail(MOE_ERR_INVALID_ARG, "%s: rows by assignment need perm_src", what);

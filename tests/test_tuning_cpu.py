@@ -405,3 +405,15 @@ def test_gradients_that_begin_between_16_bytes_are_copied():
     assert part.is_contiguous() and whole(part).data_ptr() % 16 == 0 and torch.equal(whole(part), part)
     aligned = torch.zeros(8, 8)
     assert whole(aligned).data_ptr() == aligned.data_ptr() and whole(aligned.t()).is_contiguous()
+
+
+def test_rows_of_adapters_are_counted_in_32_bits():
+    """Above 2^30 rows a row's number and what is requested ahead of it could pass 2^31: refused, db alone among them, which needs no launch for the rows themselves."""
+    def db(R):
+        name, args = _calls(R, 1, 1, 64, 8, 16)[1]
+        args[19] = PTR
+        args[20] = args[22] = None                                          # no dx, no da
+        return name, args
+    assert [c.rc for c in record([db(2 ** 31 - 1), db(2 ** 30 + 1), _calls(2 ** 30 + 1, 1, 1, 64, 64, 16)[0]])] == [UNSUPPORTED] * 3
+    got = record([db(2 ** 30)])[0]
+    assert got.rc == OK and len(got.launches) == 2 and all(0 < l.grid[0] * l.block < 2 ** 32 for l in got.launches)
