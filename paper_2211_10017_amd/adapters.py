@@ -8,8 +8,16 @@ import torch
 from . import binding as B
 from .exchange import gradient, whole
 
-# The sorted index of rows by adapter (moe_permute): k rows per token.
-AdapterIndex = namedtuple("AdapterIndex", "perm_src inv_perm offsets k")
+class AdapterIndex(namedtuple("AdapterIndex", "perm_src inv_perm offsets k")):
+    """The sorted index of rows by adapter (moe_permute): k rows per token."""
+    __slots__ = ()
+    by_assignment = property(lambda self: self.k == 1)      # how y lies unless a call says so: one row per request, in the requests' order
+
+
+class LayerIndex(AdapterIndex):
+    """An expert layer's: y is sorted by expert, also with one expert per token."""
+    __slots__ = ()
+    by_assignment = False
 
 
 def adapter_index(adapter_idx, E: int):
@@ -85,10 +93,10 @@ class LowRankAdapters:
         return adapter_index(adapter_idx, self.E)
 
     def add(self, x, y, index, by_assignment=None):
-        """y += the adapters' term, in place, without gradients (for autograd y has been changed).  Requests (k = 1): y in their order; an expert layer's rows: sorted."""
-        B.moe_adapters(x, self.a.detach(), self.b.detach(), index.offsets, index.perm_src, index.k, self.scale, index.k == 1 if by_assignment is None else by_assignment, y=y, out=y)
+        """y += the adapters' term, in place, without gradients (for autograd y has been changed).  Requests (k = 1): y in their order; an expert layer's rows (its index()): sorted."""
+        B.moe_adapters(x, self.a.detach(), self.b.detach(), index.offsets, index.perm_src, index.k, self.scale, index.by_assignment if by_assignment is None else by_assignment, y=y, out=y)
         torch.autograd.graph.increment_version(y)
         return y
 
     def __call__(self, x, y, index, by_assignment=None):
-        return adapt(x, y, self.a, self.b, index, self.scale, index.k == 1 if by_assignment is None else by_assignment)
+        return adapt(x, y, self.a, self.b, index, self.scale, index.by_assignment if by_assignment is None else by_assignment)

@@ -5,7 +5,7 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
-from .adapters import AdapterIndex
+from .adapters import LayerIndex
 
 
 class MoEMx4Layer:
@@ -65,7 +65,7 @@ class MoEMx4Layer:
 
     def index(self):
         """The last route()'s index, as adapters take it; the next one writes it again."""
-        return AdapterIndex(self.perm_src, self.inv_perm, self.expert_offsets, self.k)
+        return LayerIndex(self.perm_src, self.inv_perm, self.expert_offsets, self.k)
 
     def forward(self, x, finished=None):
         self.route(x, finished)

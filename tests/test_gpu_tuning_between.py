@@ -189,3 +189,22 @@ def test_gradients_that_begin_anywhere(name, dtype):
     assert torch.equal(grad(lambda out: (out.t() * tr).sum()), plain)
     assert torch.equal(grad(lambda out: (torch.stack([out, out], 2)[:, :, 0] * w[1:].view(shape)).sum()), plain)
     assert torch.equal(grad(lambda out: out.sum()), grad(lambda out: (out * torch.ones_like(out)).sum()))
+
+
+@pytest.mark.parametrize("k", [1, 2])
+def test_a_layers_index_says_how_its_rows_lie(k):
+    """With one expert per token as well: sorted, not in the tokens' order."""
+    gen = generator(10)
+    layer = a_layer("mx4", gen, k)
+    x = r(gen, T, D).half()
+    adapters = LowRankAdapters(E, 4, D, D, generator=gen)
+    adapters.b.normal_(generator=gen)
+    layer.forward(x)
+    want = adapters(x, layer.y_perm, layer.index(), by_assignment=False)
+    assert torch.equal(adapters(x, layer.y_perm, layer.index()), want)
+    assert torch.equal(adapters.add(x, layer.y_perm.clone(), layer.index()), want)
+    perm_src, inv_perm, offsets, rows = layer.index()
+    assert rows == k and torch.equal(layer.index().perm_src, perm_src)
+    if k == 1:
+        requests = AdapterIndex(perm_src, inv_perm, offsets, 1)
+        assert torch.equal(adapters(x, layer.y_perm, requests), adapters(x, layer.y_perm, requests, by_assignment=True)) and not torch.equal(adapters(x, layer.y_perm, requests), want)

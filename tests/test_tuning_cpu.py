@@ -417,3 +417,9 @@ def test_rows_of_adapters_are_counted_in_32_bits():
     assert [c.rc for c in record([db(2 ** 31 - 1), db(2 ** 30 + 1), _calls(2 ** 30 + 1, 1, 1, 64, 64, 16)[0]])] == [UNSUPPORTED] * 3
     got = record([db(2 ** 30)])[0]
     assert got.rc == OK and len(got.launches) == 2 and all(0 < l.grid[0] * l.block < 2 ** 32 for l in got.launches)
+
+
+def test_which_order_an_index_stands_for():
+    from paper_2211_10017_amd.adapters import AdapterIndex, LayerIndex
+    assert AdapterIndex(1, 2, 3, 1).by_assignment and not AdapterIndex(1, 2, 3, 2).by_assignment
+    assert not LayerIndex(1, 2, 3, 1).by_assignment and LayerIndex(1, 2, 3, 1) == (1, 2, 3, 1) and isinstance(LayerIndex(1, 2, 3, 1)._replace(k=2), LayerIndex)
