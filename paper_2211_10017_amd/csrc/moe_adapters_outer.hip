@@ -102,13 +102,21 @@ __device__ inline void outer_item(const OuterArgs &p, const OuterJob &job, int i
         } else {
             float back = 1.0f;
             if constexpr (DT == MOE_F16) {
-                float most = 0.0f;
+                auto largest = [&](auto finite_c) {
+                    float most = 0.0f;
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(f[B][n][i]));
+                        for (int i = 0; i < 8; ++i) {
+                            const float a = fabsf(f[B][n][i]);
+                            most = decltype(finite_c)::value && a == INFINITY ? most : fmaxf(most, a);
+                        }
 #pragma unroll
-                for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+                    for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+                    return most;
+                };
+                float most = largest(std::false_type{});
+                if (most == INFINITY) most = largest(std::true_type{});             // (an infinity is its own rank's alone: the others' numbers need their unit)
                 const int ex = split_exponent(most);
                 if (ex > unit) {
                     const float down = ex - unit > 126 ? 0.0f : exp2i(unit - ex);       // (past that only what was 0 anyway)
