@@ -130,7 +130,7 @@ struct Split {
         using T = std::conditional_t<DT == MOE_BF16, __bf16, _Float16>;
         const T h = (T)c;
         c -= (float)h;
-        c = c == c ? c : 0.0f;                                  // (an infinity leaves none)
+        c = __builtin_isfinite(c) ? c : 0.0f;                   // (an infinity leaves none, nor does a number that becomes one in bf16)
         return __builtin_bit_cast(uint16_t, h);
     }
 };

@@ -34,3 +34,20 @@ def test_a_coefficient_that_is_not_finite_is_its_ranks_alone(rows, rank, dtype, 
         assert not bool(torch.isfinite(got[0][1]).any()) and bool((got[1] == 0).all())
         if dtype == BF16:
             assert torch.equal(got[0][others], plain[0][others])
+
+
+@pytest.mark.parametrize("value,want", [(3.395e38, 3.395e38), (3.4e38, float("inf"))])
+def test_coefficients_about_the_largest_bf16_number(value, want):
+    """The largest bf16 number is (2 - 2^-7) 2^127 = 3.3895e38; up to half a step above it, (2 - 2^-8) 2^127 = 3.3962e38, numbers are rounded to it and the other terms hold the rest.  Above that, where
+    only fp32 is finite, they count as infinite (what is left of them, minus an infinity, would make a NaN of every sum)."""
+    offsets = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    a, b, dy = (torch.ones(s, dtype=BF16, device="cuda") for s in ((1, 2, 64), (1, 2, 64), (1, 64)))
+    v = torch.tensor([[value, 1.0]], device="cuda")
+    want = torch.tensor(want, device="cuda")
+    near = lambda t: bool((t == want).all() if torch.isinf(want) else ((t - want).abs() <= 2.0 ** -22 * want).all())  # noqa: E731
+    db = B.moe_adapters_backward(dy, None, a, b, v, offsets, need=(False, False, True), grad_dtype=F32)[2]
+    assert near(db[0, 0]) and bool((db[0, 1] == 1).all())
+    x = torch.zeros((1, 64), dtype=BF16, device="cuda")
+    x[0, 0] = 1.0
+    a[0, 1] = 0.0
+    assert near(B.moe_adapters(x, a, b, offsets, scale=torch.tensor([value], device="cuda"), y_dtype=F32))
