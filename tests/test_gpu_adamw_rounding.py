@@ -7,7 +7,7 @@ import torch
 
 from paper_2211_10017_amd import AdamW
 from paper_2211_10017_amd import binding as B
-from tuning_ref import BF16, F16, F32, generator
+from tuning_ref import BF16, F16, F32, generator, half_step
 
 pytestmark = pytest.mark.gpu
 
@@ -181,3 +181,51 @@ def test_equal_calls_give_equal_states(pd, gd, copy):
             flat = lambda s: s[0] + [x for pair in s[1] + s[2] for x in pair] + (s[3] or [])  # noqa: E731
             assert all(torch.equal(a, b) for a, b in zip(flat(together), flat(other))), t
         grads[0].mul_(0.9)
+
+
+def nearest(v, root):
+    """The values that v (64 bits, of fp32 numbers) is held as to the nearest number, ties to the even one."""
+    n = v.numel()
+    b = torch.nn.functional.pad(v, (0, -n % 32)).view(-1, 32)
+    top = b.abs().amax(1, keepdim=True)
+    unit = torch.exp2(torch.where(top > 0, torch.frexp(top)[1] - 8, -127).clamp(min=-127).double())
+    a = b.abs() / unit
+    step = torch.exp2((torch.frexp(a)[1] - 4).clamp(min=-9).double())
+    q = torch.round(a / step) * step
+    q = torch.where(a > 0, q.clamp(min=2.0 ** -9), q) if root else q
+    return (torch.sign(b) * q * unit).view(-1)[:n]
+
+
+@pytest.mark.parametrize("rounding", ["nearest", "random"])
+@pytest.mark.parametrize("pd,gd,copy", [(F32, F16, F16), (F32, F16, None), (BF16, F16, None), (F16, F16, None), (F32, F32, BF16), (F32, BF16, F16), (F16, BF16, None)])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_steps_in_every_type(pd, gd, copy, offset, rounding):
+    """Several steps: the moments are fp32 sums of rounded products, which torch's operations repeat bit by bit, and are held as the definition says; p within 16 roundings of a step in 64 bits."""
+    print(f"adamw 8 {pd} {gd} {copy} +{offset} {rounding}", flush=True)
+    gen, sizes = generator(11), [1, 31, 4096, 70001]
+    place = lambda t: torch.cat([t.new_zeros(offset), t])[offset:]  # noqa: E731
+    p = [place((torch.randn(n, generator=gen, device="cuda") * 0.1).to(pd)) for n in sizes]
+    sm, sv = ([states(n, offset) for n in sizes] for _ in range(2))
+    copies = [place(torch.zeros(n, dtype=copy, device="cuda")) for n in sizes] if copy else None
+    b1, b2, lr, eps, wd, gs = 0.9, 0.99, 1e-2, 1e-6, 0.1, 0.5
+    c1, c2 = 1.0 - b1, 1.0 - b2
+    for t in (1, 2, 3, 50):
+        g = [place((torch.randn(n, generator=gen, device="cuda") * torch.exp(torch.randn(n, generator=gen, device="cuda"))).to(gd)) for n in sizes]
+        old = [(held(*a).float(), held(*b).float(), q.double()) for a, b, q in zip(sm, sv, p)]
+        B.moe_adamw(p, g, sm, sv, t, lr=lr, betas=(b1, b2), eps=eps, weight_decay=wd, grad_scale=gs, copies=copies, rounding=rounding)
+        torch.cuda.synchronize()
+        for i, (m, root, before) in enumerate(old):
+            h = g[i].float() * gs
+            m = m * b1 + h * c1
+            v = root * root * b2 + h * h * c2
+            root = torch.sqrt(v)
+            bits = random_bits(torch.arange(sizes[i], device="cuda"), t)
+            for state, new, w, is_root in ((sm[i], m, bits[0], False), (sv[i], root, bits[1], True)):
+                want = rounded(new.double(), w, is_root)[0] if rounding == "random" else nearest(new.double(), is_root)
+                assert torch.equal(held(*state), want), (t, i, is_root)
+            move = lr / (1 - b1 ** t) * m.double() / (v.double().sqrt() / math.sqrt(1 - b2 ** t) + eps)
+            want = before * (1 - lr * wd) - move
+            slack = 16 * 2.0 ** -24 * (move.abs() + before.abs())
+            assert bool(((p[i].double() - want).abs() <= slack + half_step(want.abs() + slack, pd)).all()), (t, i)
+            if copy:
+                assert torch.equal(copies[i], p[i].to(copy))

@@ -423,3 +423,14 @@ def test_which_order_an_index_stands_for():
     from paper_2211_10017_amd.adapters import AdapterIndex, LayerIndex
     assert AdapterIndex(1, 2, 3, 1).by_assignment and not AdapterIndex(1, 2, 3, 2).by_assignment
     assert not LayerIndex(1, 2, 3, 1).by_assignment and LayerIndex(1, 2, 3, 1) == (1, 2, 3, 1) and isinstance(LayerIndex(1, 2, 3, 1)._replace(k=2), LayerIndex)
+
+
+def test_which_blocks_the_rows_go_through():
+    """The sizes that the tests compare reach every block of adapter_kernel with eight wavefronts: <x, matrices, y, adds y, 8, sixteens of rows, sixteens of the rank>."""
+    sizes = {(4700, 16): (2, 1), (4700, 24): (2, 2), (9001, 9): (3, 1), (9001, 32): (3, 2), (14999, 16): (5, 1), (14999, 20): (5, 2), (24000, 32): (5, 2), (17800, 5): (5, 1), (14000, 64): (2, 4),
+             (9001, 64): (3, 4), (13500, 64): (4, 4), (14000, 100): (2, 8), (9900, 100): (3, 8)}
+    calls = [c for R, rank in sizes for c in _calls(R, 1, 7, 72, 136, rank)]
+    got = record(calls)
+    for i, ((R, rank), (rows, ranks)) in enumerate(sizes.items()):
+        for call, adds_y in zip(got[2 * i:2 * i + 2], ("true", "false")):
+            assert call.rc == OK and call.launches[0].kernel == "adapter_kernel<0, 0, 0, %s, 8, %d, %d>" % (adds_y, rows, ranks), (R, rank, call.launches[0])
