@@ -85,7 +85,8 @@ class AdamW:
                     p.grad.zero_()
 
     def state_dict(self):
-        return dict(steps=list(self.counts), bits=self.bits, masters=self.masters, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq)
+        """The optimiser's own tensors and counts, which later steps change: to keep them, copy or save them."""
+        return dict(steps=self.counts, bits=self.bits, masters=self.masters, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq)
 
     def load_state_dict(self, state):
         if state["bits"] != self.bits or len(state["exp_avg"]) != len(self.params):
@@ -97,4 +98,4 @@ class AdamW:
             raise B.MoeError("the state belongs to other parameters")
         for m, t in zip(mine, theirs):
             m.copy_(t)
-        self.counts = steps
+        self.counts[:] = steps

@@ -434,3 +434,19 @@ def test_which_blocks_the_rows_go_through():
     for i, ((R, rank), (rows, ranks)) in enumerate(sizes.items()):
         for call, adds_y in zip(got[2 * i:2 * i + 2], ("true", "false")):
             assert call.rc == OK and call.launches[0].kernel == "adapter_kernel<0, 0, 0, %s, 8, %d, %d>" % (adds_y, rows, ranks), (R, rank, call.launches[0])
+
+
+def test_a_state_that_was_not_copied_stays_whole(on_host, monkeypatch):
+    """A state dict holds the optimiser's tensors as they are, and so it does the counts: loaded back after further steps it is the present state, not old counts beside new moments."""
+    _steps_asked(monkeypatch)
+    p = torch.zeros(4, requires_grad=True)
+    p.grad = torch.zeros(4)
+    one = AdamW([p])
+    one.step()
+    state = one.state_dict()
+    one.step()
+    assert state["steps"] == [2] and state["exp_avg"][0] is one.exp_avg[0]
+    one.load_state_dict(state)
+    assert one.counts == [2]
+    one.step()
+    assert state["steps"] == [3]
