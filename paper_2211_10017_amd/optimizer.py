@@ -8,10 +8,6 @@ from . import binding as B
 _HALVES = (torch.float16, torch.bfloat16)
 
 
-def _version(p):
-    return -1 if p.is_inference() else p._version           # (inference tensors have none)
-
-
 class AdamW:
     """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass; what
     others write into one between two steps (not through .data, which torch does not count) goes into its master.  step() takes the gradients that are there; a parameter
@@ -28,7 +24,7 @@ class AdamW:
         self.lr, self.betas, self.eps, self.weight_decay, self.bits = lr, tuple(betas), eps, weight_decay, bits
         self.counts = [0] * len(self.params)                # steps that each parameter has taken: its moments begin at 0, whenever that is
         self.masters = [p.detach().float() if p.dtype in _HALVES else None for p in self.params]
-        self._seen = [_version(p) for p in self.params]     # as the masters know them
+        self._seen = [None if p.is_inference() else p._version for p in self.params]        # as the masters know them (inference tensors have no version)
 
         def state(p):
             if bits == 32:
@@ -46,30 +42,39 @@ class AdamW:
         if self.params[0].device.type == "cuda" and torch.cuda.is_current_stream_capturing():
             raise B.MoeError("a captured step would have the same number in every replay: capture moe_adamw, with the step's number on the device")
         groups = {}
-        for i, p in enumerate(self.params):
-            if p.grad is not None:
-                if p.grad.is_sparse:
+        for i, (p, master, count) in enumerate(zip(self.params, self.masters, self.counts)):
+            g = p.grad
+            if g is not None:
+                if g.is_sparse:
                     raise B.MoeError("gradients must be dense")
-                groups.setdefault((p.dtype if self.masters[i] is not None else None, p.grad.dtype, self.counts[i] + 1), []).append(i)
+                key = None if master is None else p.dtype, g.dtype, count + 1
+                if key not in groups:
+                    groups[key] = [], [], []
+                for to, what in zip(groups[key], (i, p, g.contiguous())):
+                    to.append(what)
         lib, calls = B.load(), []
-        for (half, _, number), at in groups.items():
-            params = [self.params[i].detach() for i in at]
-            calls.append((at, number, params, *B.adamw_arguments([self.masters[i] for i in at] if half else params, [self.params[i].grad.contiguous() for i in at], [self.exp_avg[i] for i in at],
-                                                                 [self.exp_avg_sq[i] for i in at], number, self.lr, self.betas, self.eps, self.weight_decay, grad_scale,
-                                                                 params if half else None, "random")))
+        for (half, _, number), (at, params, grads) in groups.items():
+            masters = [self.masters[i] for i in at] if half else None
+            call = B.adamw_arguments(masters or params, grads, [self.exp_avg[i] for i in at], [self.exp_avg_sq[i] for i in at], number, self.lr, self.betas, self.eps, self.weight_decay, grad_scale,
+                                     params if half else None, "random")
+            calls.append((at, params, number, half, *call))
         # (a refusal leaves everything as it was, so all calls are checked before the first is made; one alone is by itself)
         if len(calls) > 1:
             for call in calls:
-                B._check(lib.moe_adamw_check(*call[3]), "moe_adamw")
-        for at, number, params, arguments, _ in calls:
-            for i in at:
-                if self.masters[i] is not None and _version(self.params[i]) != self._seen[i]:
-                    self._take_over(i)
+                B._check(lib.moe_adamw_check(*call[4]), "moe_adamw")
+        for at, params, number, half, arguments, _ in calls:
+            if half:
+                for i, p in zip(at, params):
+                    if not p.is_inference() and p._version != self._seen[i]:
+                        self._take_over(i)
             B._check(lib.moe_adamw(*arguments, B._stream()), "moe_adamw")
             # (written through pointers: a backward pass that still needs the old values raises)
             torch.autograd.graph.increment_version(params)
             for i in at:
-                self.counts[i], self._seen[i] = number, _version(self.params[i])
+                self.counts[i] = number
+            if half:
+                for i, p in zip(at, params):
+                    self._seen[i] = None if p.is_inference() else p._version
 
     def _take_over(self, i):
         """A parameter's new values into its master; where the parameter is still the master's rounding, the master stays."""
