@@ -54,6 +54,9 @@ class _Permute(torch.autograd.Function):
 
 def permute_tokens(x, expert_idx, E: int):
     """x [T, d], expert_idx int32 [T, k] (E: a pruned row) -> (x_perm [T * k, d], perm_src, inv_perm, expert_offsets); x_perm carries gradients, its rows behind the last expert's are 0."""
+    if x.dim() != 2 or expert_idx.dim() != 2 or expert_idx.shape[0] != x.shape[0]:
+        raise B.MoeError("x must be [T, d] and expert_idx [T, k], not %s and %s" % (tuple(x.shape), tuple(expert_idx.shape)))
+    B._check_device(x, expert_idx)
     return _Permute.apply(x, expert_idx, E)
 
 
@@ -78,6 +81,9 @@ class _Combine(torch.autograd.Function):
 def combine_tokens(y_perm, inv_perm, expert_scale, active_rows=None, out_dtype=torch.float32):
     """moe_combine with gradients for y_perm [T * k, d] and expert_scale fp32 [T, k].  The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not
     (torch raises; so it does for a buffer of a layer, of either kind, whose next call counts as a change, but where that call is a replay of a captured graph)."""
+    if y_perm.dim() != 2 or expert_scale.dim() != 2 or not y_perm.shape[0] == inv_perm.numel() == expert_scale.numel() or (active_rows is not None and active_rows.numel() < 1):
+        raise B.MoeError("expert_scale must be [T, k], inv_perm [T * k] and y_perm [T * k, d], not %s, %s and %s" % tuple(tuple(t.shape) for t in (expert_scale, inv_perm, y_perm)))
+    B._check_device(y_perm, inv_perm, expert_scale, active_rows)
     if not y_perm.is_contiguous() or not expert_scale.is_contiguous():
         y_perm, expert_scale = y_perm.contiguous(), expert_scale.contiguous()
     return _Combine.apply(y_perm, expert_scale, inv_perm, active_rows, out_dtype)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from launches import P as PTR, record
-from paper_2211_10017_amd import AdamW, LowRankAdapters, adapt, combine_tokens
+from paper_2211_10017_amd import AdamW, LowRankAdapters, adapt, combine_tokens, permute_tokens
 from paper_2211_10017_amd import binding as B
 
 P, ODD = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1008)          # never dereferenced: validation fails first
@@ -450,3 +450,24 @@ def test_a_state_that_was_not_copied_stays_whole(on_host, monkeypatch):
     assert one.counts == [2]
     one.step()
     assert state["steps"] == [3]
+
+
+def test_tokens_and_rows_that_do_not_fit(on_host, monkeypatch):
+    """permute_tokens and combine_tokens: the library knows neither how many rows there are nor how long the index is."""
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt)  # noqa: E731
+    i32 = torch.int32
+    permute_tokens(z(4, 64), z(4, 2, dt=i32), 8)
+    for bad in ((z(3, 64), z(4, 2, dt=i32)), (z(5, 64), z(4, 2, dt=i32)), (z(64), z(4, 2, dt=i32)), (z(4, 64), z(4, dt=i32))):
+        with pytest.raises(B.MoeError, match=r"\[T, k\]"):
+            permute_tokens(*bad, 8)
+    fine = dict(y_perm=z(8, 64), inv_perm=z(8, dt=i32), expert_scale=z(4, 2), active_rows=z(1, dt=i32))
+    combine_tokens(**fine)
+    for bad in (dict(y_perm=z(7, 64)), dict(y_perm=z(8 * 64)), dict(inv_perm=z(7, dt=i32)), dict(inv_perm=z(9, dt=i32)), dict(expert_scale=z(5, 2)), dict(expert_scale=z(8)), dict(active_rows=z(0, dt=i32))):
+        with pytest.raises(B.MoeError, match=r"\[T \* k"):
+            combine_tokens(**dict(fine, **bad))
+    called = len(on_host)
+    monkeypatch.setattr(B, "_raw_device", lambda: 1)
+    for call in (lambda: combine_tokens(**fine), lambda: permute_tokens(z(4, 64), z(4, 2, dt=i32), 8)):
+        with pytest.raises(B.MoeError, match="device"):
+            call()
+    assert len(on_host) == called
