@@ -22,6 +22,7 @@ class LayerIndex(AdapterIndex):
 
 def adapter_index(adapter_idx, E: int):
     """Index of requests: adapter_idx int32 [T] on the device, E for a request without an adapter (E <= 1024, moe_permute's limit).  Worth keeping while the batch is the same."""
+    B._check_device(adapter_idx)
     T, dev = adapter_idx.numel(), adapter_idx.device
     index = AdapterIndex(*(torch.empty(n, dtype=torch.int32, device=dev) for n in (T, T, E + 1)), 1)
     workspace = torch.empty(B.moe_permute_workspace_bytes(T, 1, E), dtype=torch.uint8, device=dev)

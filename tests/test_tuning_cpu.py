@@ -471,3 +471,14 @@ def test_tokens_and_rows_that_do_not_fit(on_host, monkeypatch):
         with pytest.raises(B.MoeError, match="device"):
             call()
     assert len(on_host) == called
+
+
+def test_an_index_is_made_where_the_call_runs(on_host, monkeypatch):
+    adapters, idx = LowRankAdapters(2, 4, 64, 64, device="cpu"), torch.zeros(4, dtype=torch.int32)
+    monkeypatch.setattr(B, "moe_permute_workspace_bytes", lambda *_: 16)
+    assert adapters.index(idx).offsets.numel() == 3
+    monkeypatch.setattr(B, "_raw_device", lambda: 1)
+    with pytest.raises(B.MoeError, match="device"):
+        adapters.index(idx)
+    with pytest.raises(B.MoeError, match="device"):
+        adapters.index(idx.long())
