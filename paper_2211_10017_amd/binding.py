@@ -826,32 +826,33 @@ def adamw_arguments(params, grads, exp_avg, exp_avg_sq, step, lr, betas, eps, we
     if not count:
         return None
     bits = 8 if isinstance(exp_avg[0], (tuple, list)) else 32
-    if rounding not in ("nearest", "random"):
+    state = bits
+    if rounding == "random":
+        state = bits | MOE_ADAMW_RANDOM if bits == 8 else bits
+    elif rounding != "nearest":
         raise MoeError("rounding is nearest or random, not %r" % (rounding,))
     pd, gd, cd = params[0].dtype, grads[0].dtype, copies[0].dtype if copies is not None else None
     if pd not in _DT or gd not in _DT or (cd is not None and cd not in (torch.float16, torch.bfloat16)):
         raise MoeError("parameters and gradients must be fp16, bf16 or fp32, copies fp16 or bf16")
     # All buffers in one list, kind by kind, and each check over all of it: with a hundred small tensors the checks are most of a step.
     sizes = list(map(_numel, params))
-    names, buffers, want, types = ["parameter", "gradient"], [*params, *grads], sizes * 2, [pd] * count + [gd] * count
+    buffers, want, types = [*params, *grads], sizes * 2, [pd] * count + [gd] * count
     if bits == 8:
         (m, ms), (v, vs) = _pairs(exp_avg), _pairs(exp_avg_sq)
-        names += ["codes", "codes", "scales", "scales"]
         buffers += [*m, *v, *ms, *vs]
         want += sizes * 2 + [(n + 31) // 32 for n in sizes] * 2
         types += [torch.uint8] * (4 * count)
     else:
-        names += ["moment", "moment"]
         buffers += [*exp_avg, *exp_avg_sq]
         want += sizes * 2
         types += [torch.float32] * (2 * count)
     if copies is not None:
-        names.append("copy")
         buffers += copies
         want += sizes
         types += [cd] * count
     here = torch.cuda.current_device() if _raw_device is None else _raw_device()
     if list(map(_numel, buffers)) != want or list(map(_dtype, buffers)) != types or set(map(_device, buffers)) != {here} or not all(map(_contiguous, buffers)):
+        names = ["parameter", "gradient"] + (["codes", "codes", "scales", "scales"] if bits == 8 else ["moment", "moment"]) + ["copy"]
         for i, t in enumerate(buffers):
             if t.numel() != want[i] or t.dtype is not types[i] or t.get_device() != here or not t.is_contiguous():
                 raise MoeError("%s of tensor %d must be contiguous, on the current CUDA device, of %s with %d values, not %s with %d" % (names[i // count], i % count, types[i], want[i], t.dtype, t.numel()))
@@ -865,13 +866,14 @@ def adamw_arguments(params, grads, exp_avg, exp_avg_sq, step, lr, betas, eps, we
     if copies is not None:
         table[6::8] = array.array("q", at[-count:])
     table[7::8] = array.array("q", sizes)
-    on_device = isinstance(step, torch.Tensor)
-    if on_device:
+    number, on_device = step, None
+    if type(step) is not int and isinstance(step, torch.Tensor):
         if step.numel() != 1:
             raise MoeError("step must be one number")
         _check_device(step)
-    return (table.buffer_info()[0], count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], bits | (MOE_ADAMW_RANDOM if bits == 8 and rounding == "random" else 0), lr, betas[0], betas[1],
-            eps, weight_decay, grad_scale, 1 if on_device else step, _ptr(step, torch.int32, "step") if on_device else None), (table, buffers)
+        number, on_device = 1, _ptr(step, torch.int32, "step")
+    return (table.buffer_info()[0], count, _DT[pd], _DT[gd], -1 if cd is None else _DT[cd], state, lr, betas[0], betas[1],
+            eps, weight_decay, grad_scale, number, on_device), (table, buffers)
 
 
 def moe_adamw(params, grads, exp_avg, exp_avg_sq, step, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, copies=None,
