@@ -123,14 +123,15 @@ struct Split {
     uint16_t hi, lo, rest;
     __device__ inline explicit Split(float c)
     {
-        hi = take(c), lo = take(c), rest = DT == MOE_BF16 ? take(c) : 0;
+        hi = take(c);
+        c = __builtin_isfinite(c) ? c : 0.0f;                   // (an infinity leaves none, nor does a number that becomes one in bf16; what finite numbers leave is finite)
+        lo = take(c), rest = DT == MOE_BF16 ? take(c) : 0;
     }
     __device__ static inline uint16_t take(float &c)
     {
         using T = std::conditional_t<DT == MOE_BF16, __bf16, _Float16>;
         const T h = (T)c;
         c -= (float)h;
-        c = __builtin_isfinite(c) ? c : 0.0f;                   // (an infinity leaves none, nor does a number that becomes one in bf16)
         return __builtin_bit_cast(uint16_t, h);
     }
 };
