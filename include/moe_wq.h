@@ -449,11 +449,12 @@ int moe_permute_backward(const void *dx_perm, int perm_dtype, const int32_t *inv
  *   Rows of no adapter (at or past expert_offsets[E]) are y's; in place they are neither read nor written.
  *   v [R,rank] fp32: what the backward pass needs of this one, in sorted order (rows of no adapter are not written); of at most 512 rows it may be NULL.
  * Backward, of dy [R,N] dy_dtype (ordered as y):  u[r] = scale[e] * B[e] dy[r],
- *   dx[r] = u[r] A[e] in dtype, ordered as y, 0 for rows of no adapter (with more than one row per token moe_permute_backward adds them up)
+ *   dx[r] = u[r] A[e] in dtype, ordered as y, 0 for rows of no adapter (with more than one row per token moe_permute_backward adds up the rounded rows)
  *   da[e] = sum_r u[r] x[t]^T,  db[e] = scale[e] * sum_r v[r] dy[r]^T  in grad_dtype, 0 for adapters without rows; sums over rows in a fixed order
  *   dx, da, db may each be NULL (x is read for da only, v for db only).  Workspace of moe_adapters_backward_workspace_bytes; calls that overlap in time need one each.
  * But for y == out nothing that is written overlaps anything else of the call (out == x, dx == dy and dx == x are refused).
- * Products are summed in fp32, v and u kept in it.  Strides and K, N are multiples of 8, K and N at most 2^20, 1 <= rank <= 128, E <= 4096, R <= 2^30.  expert_offsets and
+ * Products are summed in fp32, v and u kept in it.  Where they meet 16-bit numbers they enter the products as 16-bit terms: in bf16 two, off by 2^-16, or three (2^-24) where the result is
+ * fp32; in fp16 two, off by 2^-22, or by 2^-39 of the row's largest one (for da and db, of 32 rows' and up to 32 ranks') if that is more.  An infinity may come out as NaN.  Strides and K, N are multiples of 8, K and N at most 2^20, 1 <= rank <= 128, E <= 4096, R <= 2^30.  expert_offsets and
  * perm_src are forced into range: wrong contents give wrong results but no stray access.
  */
 int moe_adapters(const void *x, int dtype, int64_t x_stride, int T, const int32_t *perm_src, int k, const int32_t *expert_offsets, int R, int E, int K, int N, int rank,

@@ -1,4 +1,4 @@
-// moe_adamw, moe_adamw_state: an AdamW step over many tensors in one launch, moments in fp32 or in 8 bits.
+// moe_adamw, moe_adamw_state: an AdamW step over many tensors, forty in a launch, moments in fp32 or in 8 bits.
 //
 //   g = grad grad_scale;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
 //   p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)

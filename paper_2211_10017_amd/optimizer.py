@@ -1,4 +1,4 @@
-"""AdamW over many tensors in one launch, states in 32 or 8 bits (moe_adamw, include/moe_wq.h)."""
+"""AdamW over many tensors, forty in a launch, states in 32 or 8 bits (moe_adamw, include/moe_wq.h)."""
 from __future__ import annotations
 
 import torch
