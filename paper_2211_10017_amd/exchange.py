@@ -65,7 +65,8 @@ class _Combine(torch.autograd.Function):
     def forward(ctx, y_perm, expert_scale, inv_perm, active_rows, out_dtype):
         T, k = expert_scale.shape
         inv_perm = inv_perm.clone()                                         # (a layer routes the next batch into the same buffers, through pointers that torch does not see)
-        active = None if active_rows is None else active_rows[:1].clone()
+        # (rows past y_perm's last are never read, whatever the index says)
+        active = None if active_rows is None else active_rows[:1].clamp(max=y_perm.shape[0])
         # (the gate's scales are such a buffer too; where they carry a gradient they are the program's own, and stay in its graph)
         ctx.save_for_backward(y_perm, expert_scale if ctx.needs_input_grad[1] else expert_scale.clone(), inv_perm, active)
         return B.moe_combine(y_perm, inv_perm, expert_scale, T, k, out_dtype=out_dtype, active_rows=active)
@@ -79,10 +80,12 @@ class _Combine(torch.autograd.Function):
 
 
 def combine_tokens(y_perm, inv_perm, expert_scale, active_rows=None, out_dtype=torch.float32):
-    """moe_combine with gradients for y_perm [T * k, d] and expert_scale fp32 [T, k].  The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not
+    """moe_combine with gradients for y_perm [R, d] and expert_scale fp32 [T, k]: of all tokens (R = T * k), of some of them (rows of others get 0), or of the active rows alone.  The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not
     (torch raises; so it does for a buffer of a layer, of either kind, whose next call counts as a change, but where that call is a replay of a captured graph)."""
-    if y_perm.dim() != 2 or expert_scale.dim() != 2 or not y_perm.shape[0] == inv_perm.numel() == expert_scale.numel() or (active_rows is not None and active_rows.numel() < 1):
-        raise B.MoeError("expert_scale must be [T, k], inv_perm [T * k] and y_perm [T * k, d], not %s, %s and %s" % tuple(tuple(t.shape) for t in (expert_scale, inv_perm, y_perm)))
+    if y_perm.dim() != 2 or expert_scale.dim() != 2 or inv_perm.numel() != expert_scale.numel() or (active_rows is not None and active_rows.numel() < 1):
+        raise B.MoeError("expert_scale must be [T, k], inv_perm [T * k] and y_perm [R, d], not %s, %s and %s" % tuple(tuple(t.shape) for t in (expert_scale, inv_perm, y_perm)))
+    if active_rows is None and y_perm.shape[0] < inv_perm.numel():
+        raise B.MoeError("y_perm must have the rows of all %d assignments, or active_rows say how many there are" % inv_perm.numel())
     B._check_device(y_perm, inv_perm, expert_scale, active_rows)
     if not y_perm.is_contiguous() or not expert_scale.is_contiguous():
         y_perm, expert_scale = y_perm.contiguous(), expert_scale.contiguous()

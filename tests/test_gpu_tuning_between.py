@@ -208,3 +208,30 @@ def test_a_layers_index_says_how_its_rows_lie(k):
     if k == 1:
         requests = AdapterIndex(perm_src, inv_perm, offsets, 1)
         assert torch.equal(adapters(x, layer.y_perm, requests), adapters(x, layer.y_perm, requests, by_assignment=True)) and not torch.equal(adapters(x, layer.y_perm, requests), want)
+
+
+@pytest.mark.parametrize("k", [1, 2])
+def test_some_tokens_and_the_active_rows_alone(k):
+    """Rows of a whole batch with some of its tokens, and rows without those of pruned tokens: outputs and gradients are the whole call's."""
+    gen = generator(12)
+    perm, inv, offsets = sorted_index(routing(gen, T, k, E, "pruned"), E)
+    n = int(offsets[E])
+    y, scale, w = r(gen, T * k, 72), torch.rand((T, k), generator=gen, device="cuda"), r(gen, T, 72)
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    ys, ss = leaf(y), leaf(scale)
+    out = combine_tokens(ys, inv, ss, active_rows=offsets[E:])
+    (out * w).sum().backward()
+    part = slice(10, 30)
+    few = inv.view(T, k)[part].reshape(-1).contiguous()
+    yp, sp = leaf(y), leaf(scale[part])
+    got = combine_tokens(yp, few, sp, active_rows=offsets[E:])
+    (got * w[part]).sum().backward()
+    named = torch.zeros(T * k, dtype=torch.bool, device="cuda")
+    named[few.long()] = True
+    assert torch.equal(got, out[part]) and torch.equal(sp.grad, ss.grad[part]) and torch.equal(yp.grad, torch.where(named[:, None], ys.grad, 0.0))
+    ya, sa = leaf(y[:n]), leaf(scale)
+    got = combine_tokens(ya, inv, sa, active_rows=offsets[E:])
+    (got * w).sum().backward()
+    assert torch.equal(got, out) and torch.equal(sa.grad, ss.grad) and torch.equal(ya.grad, ys.grad[:n])
+    fewer = combine_tokens(y[:n - 5], inv, scale, active_rows=offsets[E:])     # (rows that are not there count as pruned)
+    assert torch.equal(fewer, combine_tokens(y, inv, scale, active_rows=offsets[E:] - 5))

@@ -462,7 +462,11 @@ def test_tokens_and_rows_that_do_not_fit(on_host, monkeypatch):
             permute_tokens(*bad, 8)
     fine = dict(y_perm=z(8, 64), inv_perm=z(8, dt=i32), expert_scale=z(4, 2), active_rows=z(1, dt=i32))
     combine_tokens(**fine)
-    for bad in (dict(y_perm=z(7, 64)), dict(y_perm=z(8 * 64)), dict(inv_perm=z(7, dt=i32)), dict(inv_perm=z(9, dt=i32)), dict(expert_scale=z(5, 2)), dict(expert_scale=z(8)), dict(active_rows=z(0, dt=i32))):
+    combine_tokens(**dict(fine, y_perm=z(5, 64)))                           # (the active rows alone)
+    combine_tokens(**dict(fine, y_perm=z(20, 64), active_rows=None))        # (some of a batch's tokens)
+    with pytest.raises(B.MoeError, match="active_rows"):
+        combine_tokens(**dict(fine, y_perm=z(7, 64), active_rows=None))
+    for bad in (dict(y_perm=z(8 * 64)), dict(inv_perm=z(7, dt=i32)), dict(inv_perm=z(9, dt=i32)), dict(expert_scale=z(5, 2)), dict(expert_scale=z(8)), dict(active_rows=z(0, dt=i32))):
         with pytest.raises(B.MoeError, match=r"\[T \* k"):
             combine_tokens(**dict(fine, **bad))
     called = len(on_host)
