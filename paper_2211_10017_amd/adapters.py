@@ -63,14 +63,15 @@ class _Adapt(torch.autograd.Function):
 
 def adapt(x, y, a, b, index, scale=None, by_assignment: bool = False, y_dtype=None):
     """moe_adapters as a function with gradients for x [T, K], y, a [E, rank, K] and b [E, rank, N]: y[r] + scale[e] * (A[e] x[t]) B[e], in a tensor of its own (y None: the second term).
-    The index may be written again before the backward pass; the others may not.  scale takes no gradient.  x's gradient is rounded to its type row by row before a token's rows are added."""
+    The index may be written again before the backward pass; the others may not.  scale takes no gradient.  x's gradient is rounded to its type row by row, before a token's are added."""
     if scale is not None and scale.requires_grad:
         raise B.MoeError("an adapter's scale takes no gradient")
     return _Adapt.apply(x, y, a, b, scale, index, by_assignment, y_dtype)
 
 
 class LowRankAdapters:
-    """E adapters from K to N channels (index() makes one of up to 1024, moe_permute's limit; a layer's or a caller's own serves up to 4096).  a starts as normal numbers, b as 0: an adapter begins by changing nothing."""
+    """E adapters from K to N channels (index() makes one of up to 1024, moe_permute's limit; a caller's own serves up to 4096).  a starts as normal numbers, b as 0: an adapter begins by
+    changing nothing."""
 
     def __init__(self, E, rank, K, N, dtype=torch.float16, alpha=None, device="cuda:0", generator=None):
         if not (1 <= E <= 4096 and 1 <= rank <= 128) or K <= 0 or N <= 0 or K % 8 or N % 8:

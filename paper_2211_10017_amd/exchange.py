@@ -80,8 +80,9 @@ class _Combine(torch.autograd.Function):
 
 
 def combine_tokens(y_perm, inv_perm, expert_scale, active_rows=None, out_dtype=torch.float32):
-    """moe_combine with gradients for y_perm [R, d] and expert_scale fp32 [T, k]: of all tokens (R = T * k), of some of them (rows of others get 0), or of the active rows alone.  The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not
-    (torch raises; so it does for a buffer of a layer, of either kind, whose next call counts as a change, but where that call is a replay of a captured graph)."""
+    """moe_combine with gradients for y_perm [R, d] and expert_scale fp32 [T, k]: of all tokens (R = T * k), of some of them (rows of others get 0), or of the active rows alone.
+    The index, and scales that carry no gradient, may be written again before the backward pass; y_perm may not (torch raises; so it does for a buffer of a layer, of either kind, whose next
+    call counts as a change, but where that call is a replay of a captured graph)."""
     if y_perm.dim() != 2 or expert_scale.dim() != 2 or inv_perm.numel() != expert_scale.numel() or (active_rows is not None and active_rows.numel() < 1):
         raise B.MoeError("expert_scale must be [T, k], inv_perm [T * k] and y_perm [R, d], not %s, %s and %s" % tuple(tuple(t.shape) for t in (expert_scale, inv_perm, y_perm)))
     if active_rows is None and y_perm.shape[0] < inv_perm.numel():

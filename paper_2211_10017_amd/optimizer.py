@@ -9,9 +9,9 @@ _HALVES = (torch.float16, torch.bfloat16)
 
 
 class AdamW:
-    """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass; what
-    others write into one between two steps (not through .data, which torch does not count) goes into its master.  step() takes the gradients that are there; a parameter
-    without one stays as it is, and its steps are counted from its own first one on (`counts`).  States in 8 bits are rounded up or down by chance, the same in every run: to the nearest number they could not follow their averages."""
+    """16-bit parameters are kept in fp32 beside themselves (`masters`) and written as copies of that in the same pass; what others write into one between
+    two steps (not through .data, which torch does not count) goes into its master.  step() takes the gradients that are there; a parameter without one stays as it is, and its steps are counted
+    from its own first one on (`counts`).  States in 8 bits are rounded up or down by chance, the same in every run: to the nearest number they could not follow their averages."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, bits=32):
         self.params = list(params)
@@ -37,6 +37,10 @@ class AdamW:
     def steps(self):
         """The most steps that a parameter has taken."""
         return max(self.counts)
+
+    @steps.setter
+    def steps(self, number):
+        self.counts[:] = [int(number)] * len(self.params)
 
     def step(self, grad_scale: float = 1.0):
         if self.params[0].device.type == "cuda" and torch.cuda.is_current_stream_capturing():

@@ -486,3 +486,13 @@ def test_an_index_is_made_where_the_call_runs(on_host, monkeypatch):
         adapters.index(idx)
     with pytest.raises(B.MoeError, match="device"):
         adapters.index(idx.long())
+
+
+def test_the_number_of_steps_can_be_set(on_host, monkeypatch):
+    asked = _steps_asked(monkeypatch)
+    p = torch.zeros(4, requires_grad=True)
+    p.grad = torch.zeros(4)
+    one = AdamW([p])
+    one.steps = 10                                                          # (a program that goes on with moments of its own)
+    one.step()
+    assert asked == [(1, 11)] and one.steps == 11
