@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from launches import P as PTR, record
-from paper_2211_10017_amd import AdamW, LowRankAdapters, adapt, combine_tokens, permute_tokens
+from paper_2211_10017_amd import AdamW, LowRankAdapters, adapt
+from paper_2211_10017_amd import combine_tokens, permute_tokens
 from paper_2211_10017_amd import binding as B
 
 P, ODD = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1008)          # never dereferenced: validation fails first
